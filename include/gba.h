@@ -369,6 +369,227 @@ gba_status gba_bias_act_f16(int64_t M, int64_t N, void *C, int64_t ldc, const vo
 gba_status gba_add_f16(int64_t M, int64_t N, void *C, int64_t ldc, const void *X, int64_t ldx,
                        gba_stream_t stream);
 
+/*
+ * ---------------------------------------------------------------------------
+ * A decoding step: weights in 4 bits, a paged key/value cache, and the
+ * attention of the new tokens of each request over it.  The conventions at
+ * the top of this file hold.  Elements are fp16 or bf16, one type a call;
+ * sums and softmax statistics are held in fp32 and every result is rounded
+ * once to its type.
+ *
+ * The cache keeps the keys and values of a request's tokens in blocks of
+ * block_size tokens that may lie anywhere in it.  Row r of the block table
+ * names the blocks of request r in the order of its tokens: position p of
+ * the request is token p % block_size of block table[r * width + p / block_size].
+ * A slot is block * block_size + token.
+ */
+typedef enum { GBA_F16 = 0, GBA_BF16 = 1 } gba_dtype;
+
+/*
+ * gba_q4_weight -- a K x N matrix in 4 bits with one scale, and if zeros is
+ * not NULL one zero point, for every `group` consecutive k of a column:
+ *
+ *     W(k,j) = scale(k / group, j) * (code(k,j) - zero(k / group, j))
+ *
+ * with codes 0..15 and zero 8 where zeros is NULL.  Storage:
+ *   codes   32-bit words [ceil(N/16)][ceil(K/128)][64][4]: word (nb, kb, l, i)
+ *           holds column 16 nb + l % 16 and the eight k from
+ *           128 kb + 32 i + 8 (l / 16) on, the e-th of them in the four bits
+ *           from 4 (e / 2) + 16 (e % 2) on.  What stands beyond K or N is
+ *           not used.
+ *   scales, zeros   elements [ceil(N/16)][ceil(K/group)][16] of type dtype:
+ *           (nb, g, c) belongs to column 16 nb + c.
+ * 16-byte aligned codes; group 32, 64 or 128.
+ */
+typedef struct gba_q4_weight {
+    gba_dtype dtype;
+    int group;
+    int64_t K, N;
+    const void *codes;
+    const void *scales;
+    const void *zeros;
+} gba_q4_weight;
+
+/*
+ * gba_q4_pack -- the stored form of the codes of a K x N matrix: reads one
+ * code a byte (its low four bits), codes[k * ld + j], ld >= N, and writes the
+ * ceil(N/16) * ceil(K/128) * 256 words that gba_q4_weight describes (zeros
+ * beyond K and N).
+ * Errors: GBA_EINVAL for negative sizes, ld < N, or a NULL pointer with a
+ * non-empty matrix; GBA_EUNSUPPORTED for K or N above 2^31-1 or packed not
+ * 16-byte aligned; GBA_EHIP if the launch fails.
+ */
+gba_status gba_q4_pack(int64_t K, int64_t N, const void *codes, int64_t ld, void *packed,
+                       gba_stream_t stream);
+
+/*
+ * gba_q4_linear -- C = act(A*W + bias) over a few rows: for 0<=i<M, 0<=j<N
+ *     C[i*ldc + j] = act( sum_k A[i*lda + k] * W(k,j) + (bias ? bias[j] : 0) )
+ * A (row-major, lda >= K), bias (N, or NULL) and C (row-major, ldc >= N) are
+ * of the weight's dtype.  Products are exact and summed in fp32; scales are
+ * applied to each group's fp32 sum.  Meant for up to 64 rows, which share one
+ * pass over the weights; more rows run as blocks of 64.
+ * A and C need the alignment of an element only.
+ * M == 0 or N == 0: nothing is launched.  K == 0: C = act(bias).
+ * Errors: GBA_EINVAL for w == NULL, a bad enum or group, negative sizes, a
+ * leading dimension below its extent, a NULL pointer that is read or written;
+ * GBA_EUNSUPPORTED for sizes above 2^31-1, codes not 16-byte aligned or
+ * another pointer not 2-byte aligned, or M above 64 * 65535; GBA_EHIP if the
+ * launch fails.
+ */
+gba_status gba_q4_linear(const gba_q4_weight *w, int64_t M, const void *A, int64_t lda, const void *bias,
+                         gba_act act, void *C, int64_t ldc, gba_stream_t stream);
+
+/*
+ * gba_block_tables -- the block tables of a batch and the stack of blocks
+ * that no request holds.  All arrays are on the device and the caller's:
+ * table[requests * width], held[requests] (blocks a request holds: the first
+ * held[r] entries of its row), free_blocks[num_blocks], free_count[1] (the
+ * stack is free_blocks[0 .. free_count), its top last).  Entries of a row past
+ * held are -1.
+ */
+typedef struct gba_block_tables {
+    int64_t requests, width, num_blocks;
+    int64_t block_size;
+    int32_t *table;
+    int32_t *held;
+    int32_t *free_blocks;
+    int32_t *free_count;
+} gba_block_tables;
+
+/*
+ * gba_tables_step -- make room for the next tokens of every request, give
+ * back what it no longer needs, and say where each new token goes.
+ *
+ * lens[r] tokens of request r stay in the cache and count[r] new ones come
+ * after them (both 0 for a request that has ended; negative ones count as 0).
+ * With need = ceil((lens + count) / block_size):
+ *   1. A request that holds more than need gives its last blocks back: in
+ *      request order, and within one in table order, they are pushed on the
+ *      stack of free blocks and their entries become -1.
+ *   2. Requests that need more take them from the top of the stack, in request
+ *      order and in table order, as long as the whole rest of one still fits;
+ *      the first one that does not fit and those after it that want any get
+ *      none.
+ * Outputs (slots and positions may be NULL):
+ *   offsets[requests + 1]   where a request's new tokens begin: the running
+ *                           sum of count, at most `tokens`
+ *   slots[tokens]           slot of each new token (position lens + i of its
+ *                           request for its i-th); -1 where status is not 0
+ *   positions[tokens]       lens + i, or lens + the token's depth in its tree
+ *   status[requests]        0; 1: not enough free blocks; 2: need > width;
+ *                           3: more new tokens than fit `tokens`, or a tree of
+ *                           more than 64 -- the last two take no blocks
+ *   mask[tokens]            bit j: the token is the j-th new token of its
+ *                           request or descends from it
+ * Entries past the last request's tokens are -1, -1 and 0, and so are those of
+ * a tree of more than 64.
+ * parents (NULL: every token follows the one before it, and mask is not
+ * written) gives each new token's parent as an index among the new tokens of
+ * its request; a value below 0, or not below the token's own index, makes it a
+ * root (depth 0).
+ * Sums are of 64 bits; a step is the same whatever order its threads run in.
+ *
+ * Errors: GBA_EINVAL for tables == NULL, negative sizes, block_size < 1, a
+ * NULL table, held, free_blocks, free_count, lens, count, offsets or status
+ * with requests > 0, parents without mask; GBA_EUNSUPPORTED for more than
+ * GBA_MAX_REQUESTS requests, num_blocks * block_size, tokens or requests *
+ * width above 2^31-1 or a pointer not aligned to its elements;
+ * GBA_EHIP if a launch fails.
+ */
+#define GBA_MAX_REQUESTS 4096
+gba_status gba_tables_step(const gba_block_tables *tables, const int32_t *lens, const int32_t *count,
+                           const int32_t *parents, int64_t tokens, int32_t *offsets, int32_t *slots,
+                           int32_t *positions, int32_t *status, uint64_t *mask, gba_stream_t stream);
+
+/*
+ * gba_paged_cache -- keys and values of num_blocks * block_size tokens, heads
+ * of dim elements each.  Strides are in elements; dim is contiguous.
+ */
+typedef struct gba_paged_cache {
+    gba_dtype dtype;
+    int64_t num_blocks, block_size, heads, dim;
+    void *k, *v;
+    int64_t k_block, k_token, k_head;
+    int64_t v_block, v_token, v_head;
+} gba_paged_cache;
+
+/*
+ * gba_cache_store -- write new keys and values into the cache: for each token
+ * t with 0 <= slots[t] < num_blocks * block_size, head h and element d
+ *     K(slots[t], h, d) = k[t*k_token + h*k_head + d], and V from v likewise.
+ * Tokens with any other slot are left out.  Two tokens with one slot leave
+ * either's row.  k and v are of the cache's dtype (strides in elements).
+ * Errors: GBA_EINVAL for cache == NULL, a bad enum, negative sizes, block_size
+ * < 1, a NULL pointer that is read or written; GBA_EUNSUPPORTED for
+ * num_blocks * block_size, tokens or heads * dim above 2^31-1, or an array of
+ * elements not 2-byte aligned; GBA_EHIP if the launch fails.
+ */
+gba_status gba_cache_store(const gba_paged_cache *cache, int64_t tokens, const void *k, int64_t k_token,
+                           int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
+                           const int32_t *slots, gba_stream_t stream);
+
+/*
+ * gba_attention -- one request of gba_tree_attention.  q and out: rows of
+ * query heads, element d of head h of token t at t*q_token + h*q_head + d
+ * (out likewise), of the cache's dtype.
+ */
+typedef struct gba_attention {
+    gba_paged_cache cache;
+    int64_t requests, width;      /* rows and row length of the block table */
+    int64_t tokens;               /* rows of q, out and mask */
+    int64_t max_new;              /* no request has more new tokens than this */
+    int64_t q_heads;              /* a multiple of cache.heads */
+    float scale;
+    const void *q;
+    int64_t q_token, q_head;
+    void *out;
+    int64_t out_token, out_head;
+    const int32_t *table;         /* [requests][width] */
+    const int32_t *lens;          /* [requests]: cached tokens before the new ones */
+    const int32_t *offsets;       /* [requests + 1]: rows of q of each request */
+    const uint64_t *mask;         /* [tokens], or NULL */
+    void *workspace;
+    size_t workspace_bytes;
+} gba_attention;
+
+/*
+ * gba_tree_attention -- attention of each request's new tokens over the cache.
+ *
+ * Request r has T = offsets[r+1] - offsets[r] new tokens, rows offsets[r] ...
+ * of q, whose keys and values are already in the cache at positions lens[r]
+ * ... lens[r] + T - 1.  Its i-th new token sees every position below lens[r],
+ * and position lens[r] + j for j < T if bit j of its mask is set (j < 64), or
+ * with mask == NULL if j <= i (a chain; T == 1 is ordinary decoding).  With
+ * query head h reading key head h / (q_heads / heads):
+ *     s_p = scale * q . K_p            p over the positions that it sees
+ *     out = sum_p exp(s_p - m) V_p / sum_p exp(s_p - m),   m = max_p s_p
+ * and zeros where it sees none.  The weights exp(s_p - m) are rounded to the
+ * cache's dtype for the second product, as its matrix instructions take them,
+ * and their sum is that of the rounded ones.
+ * What the cache holds at other positions is never used, whatever it is (a
+ * position whose block is outside the cache counts as not seen).  Rows of out
+ * that belong to no request are not written; neither are those of a request
+ * past max_new.
+ *
+ * Workspace: with at least gba_tree_attention_workspace_size bytes, 256-byte
+ * aligned, long requests are split across workgroups and joined by a second
+ * kernel; with less each request and head is one workgroup's work.  It need
+ * not be cleared, and calls that may overlap need separate ones.
+ *
+ * dim a multiple of 8 up to 256; q, out, K and V 16-byte aligned with strides
+ * that are multiples of 8 (out: 4).
+ * Errors: GBA_EINVAL for desc == NULL, a bad enum, negative sizes, block_size
+ * < 1, q_heads no multiple of heads, heads == 0 with tokens, a NULL pointer
+ * that is read or written, a workspace not 256-byte aligned;
+ * GBA_EUNSUPPORTED for other dims, alignments or strides, num_blocks *
+ * block_size, requests * width, width * block_size or tokens above 2^31-1,
+ * more than GBA_MAX_REQUESTS requests, or max_new > 64 with a mask; GBA_EHIP
+ * if a launch fails.
+ */
+gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t stream);
+gba_status gba_tree_attention_workspace_size(const gba_attention *desc, size_t *bytes);
+
 /* Static, human-readable name of a status code. */
 const char *gba_status_string(gba_status status);
 

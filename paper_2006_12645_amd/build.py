@@ -1,9 +1,10 @@
 """Build libgba.so (gfx950 only) in-tree with hipcc.
 
-The entry points (csrc/gba_api.hip) and one kernel-instantiation unit per
+The entry points (csrc/gba_api.hip), one kernel-instantiation unit per
 operand-layout pair and kernel variant (csrc/gba_gemm_unit.hip compiled with
-GBA_LA, GBA_LB, GBA_PRO, GBA_DUAL set) are compiled in parallel, then linked
-into ``paper_2006_12645_amd/libgba.so``.  Every hipcc line carries
+GBA_LA, GBA_LB, GBA_PRO, GBA_DUAL set) and the operators of a decoding step
+(csrc/decode, one unit each) are compiled in parallel, then linked into
+``paper_2006_12645_amd/libgba.so``.  Every hipcc line carries
 ``-Xclang -target-feature -Xclang -packed-fp32-ops`` so the device compiler
 never forms packed fp32 instructions.
 """
@@ -27,7 +28,9 @@ UNITS = [("gba_api.hip", [], "gba_api.o"), ("gba_thin_unit.hip", [], "gba_thin.o
     ("gba_gemm_unit.hip",
      [f"-DGBA_LA={la}", f"-DGBA_LB={lb}", f"-DGBA_PRO={pro}", f"-DGBA_DUAL={dual}"],
      f"gba_gemm_{'RC'[la]}{'RC'[lb]}_p{pro}d{dual}.o")
-    for la in (0, 1) for lb in (0, 1) for pro in (0, 1) for dual in (0, 1)]
+    for la in (0, 1) for lb in (0, 1) for pro in (0, 1) for dual in (0, 1)] + [
+    (os.path.join("decode", f"gba_{name}.hip"), [], f"gba_{name}.o")
+    for name in ("q4", "tables", "cache", "tree_attention")]
 HIPCC_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall",
                "-Wno-unused-function", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                "-I", INCLUDE, "-I", CSRC]

@@ -21,6 +21,8 @@ GBA_PRO_NONE, GBA_PRO_RELU = 0, 1
 GBA_SECOND_NONE, GBA_SECOND_ADD, GBA_SECOND_SUB = 0, 1, 2
 GBA_BIAS_NONE, GBA_BIAS_ROW, GBA_BIAS_FULL = 0, 1, 2
 GBA_OP_ADD, GBA_OP_SUB = 0, 1
+GBA_F16, GBA_BF16 = 0, 1
+GBA_MAX_REQUESTS = 4096
 
 ACTS = {"none": GBA_ACT_NONE, "relu": GBA_ACT_RELU, "sigmoid": GBA_ACT_SIGMOID,
         "tanh": GBA_ACT_TANH}
@@ -46,6 +48,32 @@ class Plan(ctypes.Structure):
     _fields_ = [("path", _int), ("bm", _int), ("bn", _int), ("splits", _int), ("threads", _int), ("workgroups", _i64)]
 
 
+class Q4WeightDesc(ctypes.Structure):
+    """Mirror of struct gba_q4_weight."""
+    _fields_ = [("dtype", _int), ("group", _int), ("K", _i64), ("N", _i64), ("codes", _vp), ("scales", _vp), ("zeros", _vp)]
+
+
+class BlockTablesDesc(ctypes.Structure):
+    """Mirror of struct gba_block_tables."""
+    _fields_ = [("requests", _i64), ("width", _i64), ("num_blocks", _i64), ("block_size", _i64),
+                ("table", _vp), ("held", _vp), ("free_blocks", _vp), ("free_count", _vp)]
+
+
+class PagedCacheDesc(ctypes.Structure):
+    """Mirror of struct gba_paged_cache."""
+    _fields_ = [("dtype", _int), ("num_blocks", _i64), ("block_size", _i64), ("heads", _i64), ("dim", _i64),
+                ("k", _vp), ("v", _vp), ("k_block", _i64), ("k_token", _i64), ("k_head", _i64),
+                ("v_block", _i64), ("v_token", _i64), ("v_head", _i64)]
+
+
+class AttentionDesc(ctypes.Structure):
+    """Mirror of struct gba_attention."""
+    _fields_ = [("cache", PagedCacheDesc), ("requests", _i64), ("width", _i64), ("tokens", _i64), ("max_new", _i64),
+                ("q_heads", _i64), ("scale", ctypes.c_float), ("q", _vp), ("q_token", _i64), ("q_head", _i64),
+                ("out", _vp), ("out_token", _i64), ("out_head", _i64), ("table", _vp), ("lens", _vp), ("offsets", _vp),
+                ("mask", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
 PATHS = ("empty", "tile", "deep", "few_rows", "unaligned", "general")  # enum gba_path
 
 # Every function include/gba.h declares, with its ctypes signature.
@@ -66,6 +94,12 @@ SIGNATURES = {
     "gba_fused_workspace_size": (_int, [ctypes.POINTER(FusedDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "gba_fused_tile": (_int, [ctypes.POINTER(FusedDesc), ctypes.POINTER(_int)]),
     "gba_fused_plan": (_int, [ctypes.POINTER(FusedDesc), ctypes.POINTER(Plan)]),
+    "gba_q4_pack": (_int, [_i64, _i64, _vp, _i64, _vp, _vp]),
+    "gba_q4_linear": (_int, [ctypes.POINTER(Q4WeightDesc), _i64, _vp, _i64, _vp, _int, _vp, _i64, _vp]),
+    "gba_tables_step": (_int, [ctypes.POINTER(BlockTablesDesc), _vp, _vp, _vp, _i64, _vp, _vp, _vp, _vp, _vp, _vp]),
+    "gba_cache_store": (_int, [ctypes.POINTER(PagedCacheDesc), _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp]),
+    "gba_tree_attention": (_int, [ctypes.POINTER(AttentionDesc), _vp]),
+    "gba_tree_attention_workspace_size": (_int, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "gba_status_string": (_cp, [_int]),
     "gba_version": (_cp, []),
 }
