@@ -1,10 +1,28 @@
 // gba_tree_attention.hip -- attention of each request's new tokens over a
 // paged cache.
 //
-// One wave a token and query head: 64 keys at a time, a lane each, with the
-// running maximum and sum of a softmax; then a lane for every 64th element of
-// the output.
+// The query rows of a request that share a key head (its new tokens times the
+// query heads a key head) are taken 16 RT at a time.  With K a tile of 32
+// keys and Q the rows, one matrix instruction per 32 of dim gives 16 keys by
+// 16 rows of S = K Q^T, so that a lane holds the scores of one row; with the
+// keys of the two 16-key halves in the order in which those registers hold
+// them, exp(S - m) is the operand of O = V^T P as it stands, with no exchange
+// between lanes.  V^T comes from transposing LDS reads.
+//
+// One pass: every row has a running maximum m and sum l.  m follows the scores
+// only when one passes it by more than 2^8 (in the base-2 exponent), so that
+// the accumulators are seldom scaled; weights then stay below 2^8, and their
+// relative rounding is the same at any size.  l is one more matrix
+// instruction, of ones and the rounded weights.
+//
+// Few rows read a whole cache: the bound is HBM.  A wave copies its tiles
+// straight into its own part of LDS, one tile ahead, and waits for nothing but
+// its own copies; the waves of a workgroup take the tiles of a run of keys in
+// turn and meet once, at its end.  Runs are cut to one length for all
+// requests, from the sum of their lengths, which every wave reads for itself;
+// the runs of one request are joined by a second kernel.
 #include "gba_decode.hpp"
+#include "gba_kernel.hpp"
 
 namespace gba {
 namespace {
@@ -15,68 +33,470 @@ struct AttentionArgs {
     const int32_t *table, *lens, *offsets;
     const uint64_t *mask;
     int64_t k_block, k_token, k_head, v_block, v_token, v_head, q_token, q_head, out_token, out_head;
-    int requests, width, tokens, max_new, q_heads, share, num_blocks, block_size, dim;
-    float scale;
+    int requests, width, tokens, max_new, q_heads, heads, share, num_blocks, block_size, dim;
+    float scale2;      // scale * log2(e)
+    int row_tiles;     // of a request and head
+    int slots;         // runs of keys there is room for: at least as many as there are
+    int target;        // runs to aim at (0: one for each request)
+    int32_t *first_run;  // [requests][2]: a request's first run and how many it has
+    float *part;       // [slots][heads][row_tiles]: 16 RT x dim sums, then 16 RT maxima, 16 RT sums of weights
 };
 
+constexpr int KEYS = 32;        // of a tile
+constexpr int SHORTEST = 256;   // keys of a run, but a request's last
+constexpr float SLACK = 8.f;
+
+// A request's new tokens and keys, none for one with too many.
+struct Request {
+    int first, fresh;
+    int64_t kept, end;
+};
+
+__device__ __forceinline__ Request request_of(const AttentionArgs &p, int r)
+{
+    Request q;
+    q.first = p.offsets[r];
+    q.fresh = min(p.offsets[r + 1], p.tokens) - q.first;
+    if (q.first < 0 || q.fresh < 0 || q.fresh > p.max_new) q.fresh = 0;
+    q.kept = max(p.lens[r], 0);
+    q.end = min(q.kept + q.fresh, (int64_t)p.width * p.block_size);
+    return q;
+}
+
+// A value that every lane holds, in scalar registers.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ int64_t uniform(int64_t v)
+{
+    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v), hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// Which request's run number x is, and which keys: [from, to) of request r;
+// r = -1 where there is no such run.  n, first: the request's runs.
+struct Run {
+    int r, n, first;
+    int64_t from, to;
+};
+
+__device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, int step)
+{
+    Run u;
+    if (p.target == 0) {
+        const Request q = request_of(p, x);
+        u.r = uniform(q.fresh) > 0 ? x : -1;
+        u.n = 1;
+        u.first = x;
+        u.from = 0;
+        u.to = uniform(q.end);
+        return u;
+    }
+    int64_t total = 0;
+    for (int r = lane; r < p.requests; r += 64) {
+        const Request q = request_of(p, r);
+        if (q.fresh > 0) total += q.end;
+    }
+    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
+    int64_t length = (uniform(total) + p.target - 1) / p.target;
+    length = (length + step - 1) / step * step;
+    if (length < SHORTEST) length = SHORTEST;
+    u.r = -1;
+    int before = 0;
+    for (int base = 0; base < p.requests; base += 64) {
+        const int r = base + lane;
+        int n = 0;
+        int64_t end = 0;
+        if (r < p.requests) {
+            const Request q = request_of(p, r);
+            end = q.end;
+            if (q.fresh > 0) n = end > length ? (int)((end + length - 1) / length) : 1;
+        }
+        int upto = n;
+        for (int d = 1; d < 64; d <<= 1) {
+            const int y = __shfl_up(upto, d);
+            if (lane >= d) upto += y;
+        }
+        const uint64_t past = __ballot(before + upto > x);
+        if (past != 0) {
+            const int l = __ffsll((unsigned long long)past) - 1;
+            u.r = base + l;
+            u.n = __builtin_amdgcn_readlane(n, l);
+            u.first = before + __builtin_amdgcn_readlane(upto, l) - u.n;
+            u.from = (x - u.first) * length;
+            const int64_t e = uniform(__shfl(end, l));
+            u.to = u.from + length < e ? u.from + length : e;
+            return u;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return u;
+}
+
+// Chunk permutations of a tile's rows in LDS: 16-byte chunk c of key r stands
+// at c ^ swap(r).  K is read 16 keys at one chunk, V eight keys at a pair of
+// chunks a half wave: all banks each time.
+template <int DP>
+__device__ __forceinline__ int swap_k(int key)
+{
+    return DP == 64 ? (key >> 1) & 7 : key & 15;
+}
+template <int DP>
+__device__ __forceinline__ int swap_v(int key)
+{
+    return DP == 64 ? ((key >> 1) & 3) << 1 : (key & 7) << 1;
+}
+
+// The largest of the four lanes that hold one row.
+__device__ __forceinline__ float across_max(float x)
+{
+    x = fmaxf(x, __shfl_xor(x, 32));
+    return fmaxf(x, __shfl_xor(x, 16));
+}
+
+// What one lane of a wave has written to LDS, another one reads after this: a
+// wave's accesses run in order, so only the compiler has to keep it.
+__device__ __forceinline__ void lanes_meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Waves of a workgroup: as many as have room for two tiles in LDS.
+constexpr int waves_of(int dp) { return dp == 256 ? 2 : 4; }
+
+// DP: dim, padded.  RT: blocks of 16 rows.  WHOLE: 16 consecutive keys, from a
+// multiple of 16 on, are in one block.
+template <class T, int DP, int RT, bool WHOLE>
+struct Attention {
+    typedef typename T::elem elem;
+    typedef typename T::vec8 vec8;
+    static constexpr int WAVES = waves_of(DP);
+    static constexpr int CPR = DP / 8;         // 16-byte chunks of a row
+    static constexpr int KPI = 64 / CPR;       // keys that one 64-lane copy covers
+    static constexpr int COPIES = KEYS / KPI;  // of a tile of K or V
+    static constexpr int ROW = 2 * DP, TILE = KEYS * ROW, STAGE = 2 * TILE;
+    static constexpr int SMEM = WAVES * 2 * STAGE;
+};
+
+template <class T, int DP, int RT, bool WHOLE>
+__global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(AttentionArgs p)
+{
+    typedef Attention<T, DP, RT, WHOLE> C;
+    typedef typename C::elem elem;
+    typedef typename C::vec8 vec8;
+    constexpr int WAVES = C::WAVES, CPR = C::CPR, KPI = C::KPI, COPIES = C::COPIES, ROW = C::ROW, TILE = C::TILE;
+    constexpr int STEPS = DP / 32, BLOCKS = DP / 16;
+    __shared__ __attribute__((aligned(16))) char smem[C::SMEM];
+    __shared__ float tops[WAVES][16 * RT], sums[WAVES][16 * RT];
+
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int c = lane & 15, g = lane >> 4;
+    // The row tiles of one run and head have ids 8 apart: the same XCD's L2.
+    const int xcd = blockIdx.x & 7, rest = blockIdx.x >> 3;
+    const int row_tile = rest % p.row_tiles, item = rest / p.row_tiles * 8 + xcd;
+    const int head = item % p.heads, x = item / p.heads;
+    if (x >= p.slots) return;
+    const Run run = run_of(p, x, lane, KEYS * WAVES);
+    if (run.r < 0) return;
+    Request rq = request_of(p, run.r);
+    rq.first = uniform(rq.first);
+    rq.fresh = uniform(rq.fresh);
+    rq.kept = uniform(rq.kept);
+    const int rows = rq.fresh * p.share, row0 = row_tile * (16 * RT);
+    if (p.target != 0 && run.first == x && head == 0 && row_tile == 0 && threadIdx.x == 0) {
+        p.first_run[2 * run.r] = x;
+        p.first_run[2 * run.r + 1] = run.n;
+    }
+    if (row0 >= rows) return;
+
+    // this lane's rows: as the second operand, row c of each block; dim 32 s + 8 g on
+    vec8 query[RT][STEPS];
+    uint64_t sees[RT];  // bits of the new tokens that the row sees
+    int index[RT];      // its token among the new ones
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int row = row0 + 16 * i + c;
+        const bool real = row < rows;
+        index[i] = real ? row / p.share : 0;
+        const int token = rq.first + index[i];
+        const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? row % p.share : 0)) * p.q_head;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int d = 32 * s + 8 * g;
+            const u4 none = {0, 0, 0, 0};
+            query[i][s] = real && d < p.dim ? *reinterpret_cast<const vec8 *>(q + d) : __builtin_bit_cast(vec8, none);
+        }
+        sees[i] = p.mask != nullptr ? p.mask[token] : 0;
+    }
+
+    f4 out[RT][BLOCKS] = {}, weights[RT] = {};
+    float top[RT], base2[RT];  // running maximum; what is subtracted (0 while there is none)
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        top[i] = -INFINITY;
+        base2[i] = 0.f;
+    }
+
+    char *mine = smem + wave * (2 * C::STAGE);
+    const int tiles = (int)((run.to - run.from + KEYS - 1) / KEYS);
+    const int count = tiles > wave ? (tiles - wave + WAVES - 1) / WAVES : 0;  // of this wave
+    const int32_t *entries = p.table + (int64_t)run.r * p.width;
+    auto key0 = [&](int n) { return run.from + (int64_t)KEYS * (wave + WAVES * n); };
+
+    // ---- copies of a tile: 1 KB each, lane l the chunk at byte 16 l
+    const int in_copy = lane / CPR, place = lane % CPR;
+    constexpr int PER_HALF = COPIES / 2;
+    const char *k_head = reinterpret_cast<const char *>(static_cast<const elem *>(p.k) + head * p.k_head);
+    const char *v_head = reinterpret_cast<const char *>(static_cast<const elem *>(p.v) + head * p.v_head);
+    int k_off[WHOLE ? PER_HALF : 1], v_off[WHOLE ? PER_HALF : 1];
+    if constexpr (WHOLE) {
+#pragma unroll
+        for (int i = 0; i < PER_HALF; ++i) {
+            const int key = KPI * i + in_copy, kc = place ^ swap_k<DP>(key), vc = place ^ swap_v<DP>(key);
+            k_off[i] = 8 * kc < p.dim ? (int)(key * p.k_token * 2) + 16 * kc : OOB_OFFSET;
+            v_off[i] = 8 * vc < p.dim ? (int)(key * p.v_token * 2) + 16 * vc : OOB_OFFSET;
+        }
+    }
+    // WHOLE: the blocks of the next 32 tiles' halves, a lane each.  Else: the
+    // block and token of key lane % 32 of the next tile, and its registers.
+    int entry = -1, within = 0, entries_from = 0;
+    u4 k_next[WHOLE ? 1 : COPIES], v_next[WHOLE ? 1 : COPIES];
+    unsigned next_there = 0, there = 0;  // keys of the tile that exist
+
+    auto look_up = [&](int n) {
+        const int64_t pos = WHOLE ? key0(n + lane / 2) + 16 * (lane & 1) : key0(n) + (lane & 31);
+        entry = -1;
+        if (pos < run.to) {
+            const int page = (int)pos / p.block_size;
+            within = (int)pos - page * p.block_size;
+            const int b = entries[page];
+            entry = b >= 0 && b < p.num_blocks ? b : -1;
+        }
+        entries_from = n;
+    };
+    auto copy = [&](int n, int stage) {
+        char *k_lds = mine + stage * C::STAGE, *v_lds = k_lds + TILE;
+        if constexpr (WHOLE) {
+            if (n - entries_from == 32) look_up(n);
+            next_there = 0;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int at = 2 * (n - entries_from) + h;
+                const int b = __builtin_amdgcn_readlane(entry, at), t = __builtin_amdgcn_readlane(within, at);
+                const int64_t left = run.to - (key0(n) + 16 * h);
+                const int keys = b < 0 ? 0 : left < 16 ? (int)left : 16;
+                next_there |= ((1u << keys) - 1) << (16 * h);
+                // beyond the last key the buffer has ended: zeros
+                const char *kb = k_head + 2 * ((b < 0 ? 0 : b) * p.k_block + t * p.k_token);
+                const char *vb = v_head + 2 * ((b < 0 ? 0 : b) * p.v_block + t * p.v_token);
+                const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<char *>(kb), (short)0, keys ? (int)((keys - 1) * p.k_token + p.dim) * 2 : 0, RSRC_WORD3);
+                const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
+                    const_cast<char *>(vb), (short)0, keys ? (int)((keys - 1) * p.v_token + p.dim) * 2 : 0, RSRC_WORD3);
+#pragma unroll
+                for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(kr, k_lds + 1024 * (PER_HALF * h + i), k_off[i], 0);
+#pragma unroll
+                for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(vr, v_lds + 1024 * (PER_HALF * h + i), v_off[i], 0);
+            }
+        } else {
+            next_there = (unsigned)__ballot(entry >= 0);
+            const int block = entry, token = within;
+            if (n + 1 < count) look_up(n + 1);
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                const int key = KPI * i + in_copy, kc = place ^ swap_k<DP>(key), vc = place ^ swap_v<DP>(key);
+                const int64_t b = __shfl(block, key), t = __shfl(token, key);
+                const u4 none = {0, 0, 0, 0};
+                k_next[i] = v_next[i] = none;
+                if (b >= 0 && 8 * kc < p.dim) k_next[i] = *reinterpret_cast<const u4 *>(k_head + 2 * (b * p.k_block + t * p.k_token) + 16 * kc);
+                if (b >= 0 && 8 * vc < p.dim) v_next[i] = *reinterpret_cast<const u4 *>(v_head + 2 * (b * p.v_block + t * p.v_token) + 16 * vc);
+            }
+        }
+    };
+
+    // ---- LDS addresses of the fragments
+    int k_at[STEPS], v_at;
+#pragma unroll
+    for (int s = 0; s < STEPS; ++s) k_at[s] = c * ROW + 16 * ((4 * s + g) ^ swap_k<DP>(c));
+    const int v_key = 4 * g + (c >> 2), v_swap = 16 * swap_v<DP>(v_key);
+    v_at = v_key * ROW + 16 * ((c & 3) >> 1) + 8 * (c & 1);
+
+    const bool masked = p.mask != nullptr;
+    if (count > 0) {
+        look_up(0);
+        wait_vm_lgkm0<0>();  // the rows too: from here on only copies are under way
+        copy(0, 0);
+    }
+    const u4 ones_bits = __builtin_bit_cast(u4, vec8{(elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f});
+    const vec8 ones = __builtin_bit_cast(vec8, ones_bits);
+    for (int n = 0; n < count; ++n) {
+        const int stage = WHOLE ? n & 1 : 0;
+        const char *k_lds = mine + stage * C::STAGE, *v_lds = k_lds + TILE;
+        there = next_there;
+        if constexpr (WHOLE) {
+            wait_vm_lgkm0<63>();  // the other stage's fragments have been read
+            if (n + 1 < count) {
+                copy(n + 1, stage ^ 1);
+                wait_vm_lgkm0<2 * COPIES < 64 ? 2 * COPIES : 63>();
+            } else {
+                wait_vm_lgkm0<0>();
+            }
+        } else {
+            lanes_meet();  // the last tile's fragments have been read
+#pragma unroll
+            for (int i = 0; i < COPIES; ++i) {
+                *reinterpret_cast<u4 *>(mine + 1024 * i + 16 * lane) = k_next[i];
+                *reinterpret_cast<u4 *>(mine + TILE + 1024 * i + 16 * lane) = v_next[i];
+            }
+            if (n + 1 < count) copy(n + 1, 0);
+        }
+        lanes_meet();
+
+        // scores: keys 16 h + 4 g + e of the tile, row c of each block
+        f4 score[RT][2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) score[i][h] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const vec8 k = *reinterpret_cast<const vec8 *>(k_lds + 16 * h * ROW + k_at[s]);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) score[i][h] = T::mfma(k, query[i][s], score[i][h]);
+            }
+        }
+        const int64_t first_key = key0(n);
+        const bool all = there == 0xFFFFFFFFu && first_key + KEYS <= rq.kept;
+        const int first_draft = (int)(first_key - rq.kept);
+        vec8 weight[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            float t[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) t[e] = score[i][e >> 2][e & 3] * p.scale2;
+            if (!all) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int key = 16 * (e >> 2) + 4 * g + (e & 3);
+                    const int draft = first_draft + key;  // of the new tokens, or below 0
+                    const bool in_tree = masked ? (draft < 64) & (int)((sees[i] >> (draft & 63)) & 1) : draft <= index[i];
+                    const bool seen = ((there >> key) & 1) & ((draft < 0) | in_tree);
+                    t[e] = seen ? t[e] : -INFINITY;
+                }
+            }
+            float most = t[0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) most = fmaxf(most, t[e]);
+            if (__ballot(most > top[i] + SLACK)) {
+                const float now = fmaxf(across_max(most), top[i]);
+                const float next = now == -INFINITY ? 0.f : now;
+                const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
+                top[i] = now;
+                base2[i] = next;
+                weights[i] *= keep;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) out[i][b] *= keep;
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) weight[i][e] = (elem)__builtin_amdgcn_exp2f(t[e] - base2[i]);
+            weights[i] = T::mfma(ones, weight[i], weights[i]);
+        }
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b) {
+            const char *at = v_lds + v_at + ((32 * b) ^ v_swap);
+            const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)at);
+            const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(at + 16 * ROW));
+            const vec8 v = __builtin_bit_cast(vec8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+#pragma unroll
+            for (int i = 0; i < RT; ++i) out[i][b] = T::mfma(v, weight[i], out[i][b]);
+        }
+    }
+
+    // ---- the waves' sums, joined through LDS: row c, chunks of four of dim,
+    // chunk j of a row at j ^ c
+    wait_vm_lgkm0<0>();
+    lanes_meet();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        if (g == 0) {
+            tops[wave][16 * i + c] = top[i];
+            sums[wave][16 * i + c] = weights[i][0];
+        }
+#pragma unroll
+        for (int b = 0; b < BLOCKS; ++b)
+            *reinterpret_cast<f4 *>(mine + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = out[i][b];
+    }
+    __syncthreads();
+    const bool whole_request = run.n == 1;
+    float *part = whole_request ? nullptr
+                                : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * (16 * RT) * (int64_t)(p.dim + 2);
+    constexpr int FOURS = DP / 4;
+    for (int j = threadIdx.x; j < 16 * RT * FOURS; j += 64 * WAVES) {
+        const int row = j / FOURS, four = j % FOURS, d = 4 * four;
+        if (row0 + row >= rows || d >= p.dim) continue;
+        float m = tops[0][row];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][row]);
+        f4 o = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) {
+            const float share = tops[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[w][row] - m);
+            l += share * sums[w][row];
+            o += share * *reinterpret_cast<const f4 *>(smem + w * (2 * C::STAGE) + row * (4 * DP) + 16 * (four ^ (row & 15)));
+        }
+        if (whole_request) {
+            typedef elem four_t __attribute__((ext_vector_type(4)));
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
+            four_t r;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r[e] = (elem)(o[e] * inv);
+            *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r;
+        } else {
+            *reinterpret_cast<f4 *>(part + row * p.dim + d) = o;
+            if (four == 0) {
+                part[16 * RT * p.dim + row] = m;
+                part[16 * RT * (p.dim + 1) + row] = l;
+            }
+        }
+    }
+}
+
+// The runs of a request, added in their order; one wave a token and query head.
 template <class T>
-__global__ void __launch_bounds__(64) attention_simple(AttentionArgs p)
+__global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_rows)
 {
     typedef typename T::elem elem;
-    __shared__ float query[256], weight[64];
-    __shared__ int64_t value_at[64];
-    const int lane = threadIdx.x, t = blockIdx.x, head = blockIdx.y, key_head = head / p.share;
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int t = (int)(id / p.q_heads), head = (int)(id % p.q_heads);
+    if (t >= p.tokens) return;
     const int r = owner_of(p.offsets, p.requests, t);
-    if (r >= p.requests || t < p.offsets[r]) return;
-    const int first = p.offsets[r], T_new = min(p.offsets[r + 1], p.tokens) - first;
-    if (T_new > p.max_new) return;
-    const int64_t kept = max(p.lens[r], 0), end = min(kept + T_new, (int64_t)p.width * p.block_size);
-    const uint64_t mask = p.mask == nullptr ? 0 : p.mask[t];
-    const elem *q = static_cast<const elem *>(p.q) + t * p.q_token + head * p.q_head;
-    for (int d = lane; d < p.dim; d += 64) query[d] = (float)q[d];
-    __syncthreads();
-    float top = -INFINITY, total = 0.f, o[4] = {};
-    for (int64_t base = 0; base < end; base += 64) {
-        const int64_t pos = base + lane, draft = pos - kept;
-        bool sees = pos < end && (draft < 0 || (p.mask == nullptr ? draft <= t - first : draft < 64 && ((mask >> draft) & 1)));
-        int block = -1;
-        if (sees) {
-            block = p.table[(int64_t)r * p.width + pos / p.block_size];
-            sees = block >= 0 && block < p.num_blocks;
-        }
-        float s = -INFINITY;
-        if (sees) {
-            const int64_t token = pos % p.block_size;
-            const elem *k = static_cast<const elem *>(p.k) + block * p.k_block + token * p.k_token + key_head * p.k_head;
-            s = 0.f;
-            for (int d = 0; d < p.dim; ++d) s += query[d] * (float)k[d];
-            s *= p.scale;
-            value_at[lane] = block * p.v_block + token * p.v_token + key_head * p.v_head;
-        }
-        float m = s;
-        for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-        m = fmaxf(m, top);
-        if (m == -INFINITY) continue;
-        const float keep = top == -INFINITY ? 0.f : __expf(top - m);
-        const float w = sees ? (float)(elem)__expf(s - m) : 0.f;
-        weight[lane] = sees ? w : -1.f;
-        float sum = w;
-        for (int d = 32; d; d >>= 1) sum += __shfl_xor(sum, d);
-        total = total * keep + sum;
-        top = m;
-        __syncthreads();
-        for (int i = 0; i < 4; ++i) o[i] *= keep;
-        for (int j = 0; j < 64; ++j) {
-            if (weight[j] < 0.f) continue;
-            const elem *v = static_cast<const elem *>(p.v) + value_at[j];
-            for (int i = 0; i < 4; ++i)
-                if (lane + 64 * i < p.dim) o[i] += weight[j] * (float)v[lane + 64 * i];
-        }
-        __syncthreads();
+    if (r >= p.requests) return;
+    const Request rq = request_of(p, r);
+    if (rq.fresh == 0 || t < rq.first) return;
+    const int n = p.first_run[2 * r + 1], x0 = p.first_run[2 * r];
+    if (n <= 1) return;
+    const int row = (t - rq.first) * p.share + head % p.share, tile = row / tile_rows, in_tile = row % tile_rows;
+    const int64_t tile_size = (int64_t)tile_rows * (p.dim + 2), stride = tile_size * p.heads * p.row_tiles;
+    const float *part = p.part + (((int64_t)x0 * p.heads + head / p.share) * p.row_tiles + tile) * tile_size;
+    const float *tops = part + tile_rows * p.dim + in_tile, *sums = tops + tile_rows;
+    float m = -INFINITY;
+    for (int i = lane; i < n; i += 64) m = fmaxf(m, tops[i * stride]);
+    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    float l = 0.f, o[4] = {};
+    for (int i = 0; i < n; ++i) {
+        const float top = tops[i * stride], share = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - m);
+        l += share * sums[i * stride];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (lane + 64 * j < p.dim) o[j] += share * part[i * stride + in_tile * p.dim + lane + 64 * j];
     }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
     elem *out = static_cast<elem *>(p.out) + t * p.out_token + head * p.out_head;
-    for (int i = 0; i < 4; ++i)
-        if (lane + 64 * i < p.dim) out[lane + 64 * i] = (elem)(total > 0.f ? o[i] / total : 0.f);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (lane + 64 * j < p.dim) out[lane + 64 * j] = (elem)(o[j] * inv);
 }
 
 gba_status validate(const gba_attention &d)
@@ -108,6 +528,79 @@ gba_status validate(const gba_attention &d)
     return GBA_OK;
 }
 
+// How a call runs: rows of a tile, tiles, runs of keys and their room.
+struct Shape {
+    bool whole;
+    int dp, rt, row_tiles, target, slots;
+    size_t header, bytes;  // of the workspace
+};
+
+constexpr int RUNS = 1024;          // workgroups to aim at
+constexpr int SPLIT_REQUESTS = 1024;  // above that each request is one run
+
+Shape shape_of(const gba_attention &d)
+{
+    const gba_paged_cache &c = d.cache;
+    Shape s;
+    // 16 keys in one block, and their offsets in a buffer of 32 bits
+    s.whole = c.block_size % 16 == 0 && c.k_token >= 0 && c.v_token >= 0 && c.k_token < (1 << 25) && c.v_token < (1 << 25);
+    s.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
+    const int64_t rows = d.max_new * (d.q_heads / c.heads);
+    // as many rows as the registers hold: those that are not copied straight
+    // to LDS pass through them
+    const int most = s.dp == 64 ? 4 : s.dp == 128 ? (s.whole ? 4 : 2) : (s.whole ? 2 : 1);
+    s.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+    if (s.rt > most) s.rt = most;
+    s.row_tiles = (int)div_up(rows, 16 * s.rt);
+    s.target = 0;
+    s.slots = (int)d.requests;
+    s.header = s.bytes = 0;
+    if (d.requests <= SPLIT_REQUESTS && d.width * c.block_size > SHORTEST) {
+        s.target = (int)div_up(RUNS, c.heads * (int64_t)s.row_tiles);
+        s.slots = (int)d.requests + s.target;
+        s.header = (size_t)div_up(d.requests * 8, 256) * 256;
+        s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt) * (c.dim + 2) * sizeof(float);
+    }
+    return s;
+}
+
+template <class T, int DP, int RT, bool WHOLE>
+gba_status run_attention(const AttentionArgs &a, hipStream_t s)
+{
+    const int64_t groups = div_up((int64_t)a.slots * a.heads, 8) * 8 * a.row_tiles;
+    constexpr int threads = 64 * waves_of(DP);
+    if (groups > (int64_t)UINT_MAX / threads) return GBA_EUNSUPPORTED;
+    const gba_status st = launch(attention_kernel<T, DP, RT, WHOLE>, dim3((unsigned)groups), dim3(threads), s, a);
+    if (st != GBA_OK || a.target == 0) return st;
+    return launch(join_kernel<T>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, 16 * RT);
+}
+
+template <class T, bool WHOLE>
+gba_status run_attention(const AttentionArgs &a, const Shape &sh, hipStream_t s)
+{
+    if (sh.dp == 64)
+        return sh.rt == 1 ? run_attention<T, 64, 1, WHOLE>(a, s) : sh.rt == 2 ? run_attention<T, 64, 2, WHOLE>(a, s) : run_attention<T, 64, 4, WHOLE>(a, s);
+    if (sh.dp == 128) {
+        if constexpr (WHOLE)
+            if (sh.rt == 4) return run_attention<T, 128, 4, true>(a, s);
+        return sh.rt == 1 ? run_attention<T, 128, 1, WHOLE>(a, s) : run_attention<T, 128, 2, WHOLE>(a, s);
+    }
+    if constexpr (WHOLE)
+        if (sh.rt == 2) return run_attention<T, 256, 2, true>(a, s);
+    return run_attention<T, 256, 1, WHOLE>(a, s);
+}
+
+template <class T>
+gba_status run_attention(const AttentionArgs &a, const Shape &sh, hipStream_t s)
+{
+    return sh.whole ? run_attention<T, true>(a, sh, s) : run_attention<T, false>(a, sh, s);
+}
+
+bool nothing_to_do(const gba_attention &d)
+{
+    return d.tokens == 0 || d.requests == 0 || d.q_heads == 0 || d.max_new == 0 || d.cache.dim == 0;
+}
+
 }  // namespace
 }  // namespace gba
 
@@ -116,8 +609,9 @@ using namespace gba;
 extern "C" gba_status gba_tree_attention_workspace_size(const gba_attention *desc, size_t *bytes)
 {
     if (desc == nullptr || bytes == nullptr) return GBA_EINVAL;
-    *bytes = 0;
-    return validate(*desc);
+    const gba_status st = validate(*desc);
+    if (st == GBA_OK) *bytes = nothing_to_do(*desc) ? 0 : shape_of(*desc).bytes;
+    return st;
 }
 
 extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t stream)
@@ -126,7 +620,12 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     const gba_attention &d = *desc;
     const gba_paged_cache &c = d.cache;
     const gba_status st = validate(d);
-    if (st != GBA_OK || d.tokens == 0 || d.requests == 0 || d.q_heads == 0 || d.max_new == 0 || c.dim == 0) return st;
+    if (st != GBA_OK || nothing_to_do(d)) return st;
+    Shape sh = shape_of(d);
+    if (sh.target != 0 && (d.workspace == nullptr || d.workspace_bytes < sh.bytes)) {
+        sh.target = 0;
+        sh.slots = (int)d.requests;
+    }
     AttentionArgs a;
     a.q = d.q;
     a.k = c.k;
@@ -147,16 +646,21 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     a.out_token = d.out_token;
     a.out_head = d.out_head;
     a.requests = (int)d.requests;
-    a.width = (int)d.width;
+    a.width = c.num_blocks > 0 ? (int)d.width : 0;  // an empty cache: no keys
     a.tokens = (int)d.tokens;
     a.max_new = (int)d.max_new;
     a.q_heads = (int)d.q_heads;
+    a.heads = (int)c.heads;
     a.share = (int)(d.q_heads / c.heads);
     a.num_blocks = (int)c.num_blocks;
     a.block_size = (int)c.block_size;
     a.dim = (int)c.dim;
-    a.scale = d.scale;
-    const dim3 grid((unsigned)d.tokens, (unsigned)d.q_heads), block(64);
+    a.scale2 = d.scale * 1.44269504088896340736f;
+    a.row_tiles = sh.row_tiles;
+    a.slots = sh.slots;
+    a.target = sh.target;
+    a.first_run = static_cast<int32_t *>(d.workspace);
+    a.part = sh.target != 0 ? reinterpret_cast<float *>(static_cast<char *>(d.workspace) + sh.header) : nullptr;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    return c.dtype == GBA_F16 ? launch(attention_simple<F16>, grid, block, s, a) : launch(attention_simple<BF16>, grid, block, s, a);
+    return c.dtype == GBA_F16 ? run_attention<F16>(a, sh, s) : run_attention<BF16>(a, sh, s);
 }
