@@ -51,6 +51,14 @@ __device__ __forceinline__ int owner_of(const P *before, int n, int64_t v)
     return lo;
 }
 
+// What one lane of a wave has written to LDS, another one reads after this: a
+// wave's accesses run in order, so only the compiler has to keep it.
+__device__ __forceinline__ void lanes_meet()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_wave_barrier();
+}
+
 inline bool aligned_to(const void *p, uintptr_t a) { return (reinterpret_cast<uintptr_t>(p) & (a - 1)) == 0; }
 inline bool is_dtype(int d) { return d == GBA_F16 || d == GBA_BF16; }
 inline bool is_act(int a) { return a >= GBA_ACT_NONE && a <= GBA_ACT_TANH; }

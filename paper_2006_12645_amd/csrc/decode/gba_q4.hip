@@ -4,15 +4,21 @@
 // into the top of the fraction of the 16-bit float 16.0, are the float 16 + q
 // with no conversion; so a group's sum is
 //     sum_k a_k (q_k - z) = sum_k a_k (16 + q_k) - (16 + z) sum_k a_k
-// and both sums are matrix instructions: the second one takes A times ones,
-// or, where every z is 8, A times -24 into the same accumulator.  The products
-// are exact and the sums fp32; the scale multiplies a group's fp32 sum.
+// and both sums are matrix instructions, the second one of A and ones, for all
+// columns of a wave at once.  The products are exact and the sums fp32; the
+// scale multiplies a group's fp32 sum.
 //
-// A workgroup owns 16 columns and 16 MT rows; its waves take the 128-deep
-// chunks of K in turn (a chunk of a column block is 1 KB, contiguous: 16 bytes
-// a lane, the lane's operands of four 32-deep matrix instructions) and add
-// their sums through LDS in wave order.
+// The bound is reading W once.  A workgroup owns 16 NT columns and 16 MT rows;
+// its waves take the 128-deep chunks of K in turn and never wait for each
+// other before the end, where their sums are added through LDS in wave order.
+// A chunk of a column block is 1 KB, contiguous: 16 bytes a lane, the lane's
+// operands of four 32-deep matrix instructions.  A wave holds the codes,
+// scales and rows of A of its next chunks in registers; A passes through the
+// wave's own corner of LDS on its way to the matrix instructions' order, so
+// that it is read in whole rows, of which the address unit takes four times
+// as much a clock as of 16-byte pieces.
 #include "gba_decode.hpp"
+#include "gba_kernel.hpp"
 
 namespace gba {
 namespace {
@@ -23,16 +29,19 @@ struct Q4Args {
     void *C;
     int64_t lda, ldc;
     int M, N, K;
-    int KB, GB;  // 128-deep chunks, groups
+    int NB, KB, GB;  // 16-column blocks, 128-deep chunks, groups
     int act;
 };
 
 constexpr int WAVES = 8;
 
+// The 16-bit floats 16 + q of eight codes.
 template <class T>
 __device__ __forceinline__ typename T::vec8 unpack(unsigned w)
 {
-    constexpr unsigned M = 0x000F000Fu << T::TOP;
+    // in a vector register, or a mask and a constant are two instructions
+    unsigned M = 0x000F000Fu << T::TOP;
+    asm("" : "+v"(M));
     u4 r;
     r[0] = ((w << T::TOP) & M) | T::SIXTEEN;
     if constexpr (T::TOP >= 4) r[1] = ((w << (T::TOP - 4)) & M) | T::SIXTEEN;
@@ -42,86 +51,37 @@ __device__ __forceinline__ typename T::vec8 unpack(unsigned w)
     return __builtin_bit_cast(typename T::vec8, r);
 }
 
-template <class T>
-__device__ __forceinline__ typename T::vec8 splat(float v)
-{
-    typename T::vec8 r;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) r[e] = (typename T::elem)v;
-    return r;
-}
-
 // Eight elements of a row from k on, zeros beyond K.
 template <class T>
-__device__ __forceinline__ typename T::vec8 load_row8(const typename T::elem *row, int k, int K)
+__device__ __forceinline__ u4 load_row8(const typename T::elem *row, int k, int K)
 {
-    typedef typename T::vec8 unaligned __attribute__((aligned(2)));
+    typedef u4 unaligned __attribute__((aligned(2)));
     if (k + 8 <= K) return *reinterpret_cast<const unaligned *>(row + k);
-    typename T::vec8 r = splat<T>(0.f);
+    typename T::vec8 r;
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-        if (k + e < K) r[e] = row[k + e];
-    return r;
+    for (int e = 0; e < 8; ++e) r[e] = k + e < K ? row[k + e] : (typename T::elem)0.f;
+    return __builtin_bit_cast(u4, r);
 }
 
-// STEPS: 32-deep steps of a group
-template <class T, int MT, int STEPS, bool ZEROS>
-__global__ void __launch_bounds__(64 * WAVES) q4_kernel(Q4Args p)
+// The waves' sums, added in wave order, bias, activation, and the one rounding.
+template <class T, int MT, int NT, int W>
+__device__ __forceinline__ void q4_store(const Q4Args &p, const f4 (&acc)[MT][NT], char *smem, int row0, int nb0)
 {
     typedef typename T::elem elem;
-    typedef typename T::vec8 vec8;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 15, kq = 8 * (lane >> 4);
-    const int nb = blockIdx.x, row0 = blockIdx.y * (16 * MT);
-    const u4 *codes = p.codes + (int64_t)nb * p.KB * 64 + lane;
-    const elem *scales = static_cast<const elem *>(p.scales) + (int64_t)nb * p.GB * 16 + c;
-    const elem *zeros = static_cast<const elem *>(p.zeros) + (int64_t)nb * p.GB * 16 + c;
-    const elem *rows[MT];
-    bool there[MT];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    f4 *part = reinterpret_cast<f4 *>(smem);
 #pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int row = row0 + 16 * t + c;
-        there[t] = row < p.M;
-        rows[t] = static_cast<const elem *>(p.A) + (there[t] ? row : 0) * p.lda;
-    }
-    const vec8 fixed = splat<T>(ZEROS ? 1.f : -24.f), none = splat<T>(0.f);
-    f4 acc[MT] = {};
-    for (int kb = wave; kb < p.KB; kb += WAVES) {
-        const u4 w = codes[(int64_t)kb * 64];
+    for (int t = 0; t < MT; ++t)
 #pragma unroll
-        for (int g = 0; g < 4 / STEPS; ++g) {
-            int group = kb * (4 / STEPS) + g;
-            if (group >= p.GB) group = p.GB - 1;  // beyond K: A's elements there are zeros
-            const float scale = (float)scales[group * 16];
-            f4 sum[MT] = {}, ones[MT] = {};
-#pragma unroll
-            for (int i = 0; i < STEPS; ++i) {
-                const int j = g * STEPS + i;
-                const vec8 b = unpack<T>(w[j]);
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-                    const vec8 a = there[t] ? load_row8<T>(rows[t], kb * 128 + 32 * j + kq, p.K) : none;
-                    sum[t] = T::mfma(a, b, sum[t]);
-                    if (ZEROS) ones[t] = T::mfma(a, fixed, ones[t]);
-                    else sum[t] = T::mfma(a, fixed, sum[t]);
-                }
-            }
-            const float shift = ZEROS ? 16.f + (float)zeros[group * 16] : 0.f;
-#pragma unroll
-            for (int t = 0; t < MT; ++t)
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    acc[t][e] += scale * (ZEROS ? sum[t][e] - shift * ones[t][e] : sum[t][e]);
-        }
-    }
-    __shared__ f4 part[WAVES][MT][64];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) part[wave][t][lane] = acc[t];
+        for (int n = 0; n < NT; ++n) part[((wave * MT + t) * NT + n) * 64 + lane] = acc[t][n];
     __syncthreads();
-    for (int e = threadIdx.x; e < 256 * MT; e += 64 * WAVES) {
-        const int row = row0 + e / 16, col = 16 * nb + e % 16;
+    const float *sums = reinterpret_cast<const float *>(smem);
+    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * W) {
+        const int t = i / (256 * NT), r = i / (16 * NT) % 16, n = i / 16 % NT, j = i % 16;
+        const int row = row0 + 16 * t + r, col = 16 * (nb0 + n) + j;
         float x[1] = {0.f};
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) x[0] += part[w][e / 256][(e / 64 % 4) * 16 + e % 16][e / 16 % 4];
+        for (int w = 0; w < W; ++w) x[0] += sums[(((w * MT + t) * NT + n) * 64 + (r / 4) * 16 + j) * 4 + r % 4];
         if (row < p.M && col < p.N) {
             if (p.bias != nullptr) x[0] += (float)static_cast<const elem *>(p.bias)[col];
             activate(p.act, x);
@@ -130,21 +90,306 @@ __global__ void __launch_bounds__(64 * WAVES) q4_kernel(Q4Args p)
     }
 }
 
-template <class T, int MT>
-gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
+// Up to 16 rows.  STEPS: 32-deep steps of a group.  AHEAD: chunks held in
+// registers.
+template <class T, int NT, int STEPS, bool ZEROS, int AHEAD>
+__global__ void __launch_bounds__(64 * WAVES) q4_kernel(Q4Args p)
 {
-    const dim3 grid((unsigned)div_up(a.N, 16), (unsigned)div_up(a.M, 16 * MT)), block(64 * WAVES);
-    const bool z = a.zeros != nullptr;
-    if (group == 32) return z ? launch(q4_kernel<T, MT, 1, true>, grid, block, s, a) : launch(q4_kernel<T, MT, 1, false>, grid, block, s, a);
-    if (group == 64) return z ? launch(q4_kernel<T, MT, 2, true>, grid, block, s, a) : launch(q4_kernel<T, MT, 2, false>, grid, block, s, a);
-    return z ? launch(q4_kernel<T, MT, 4, true>, grid, block, s, a) : launch(q4_kernel<T, MT, 4, false>, grid, block, s, a);
+    constexpr int MT = 1;
+    typedef typename T::elem elem;
+    typedef typename T::vec8 vec8;
+    constexpr int GROUPS = 4 / STEPS;              // of a chunk
+    constexpr int ROWS = 16 * MT, LOADS = ROWS / 4;  // a load: four rows of 256 bytes
+    constexpr int CORNER = ROWS * 256, PART = MT * NT * 1024;
+    __shared__ __attribute__((aligned(16))) char smem[WAVES * (CORNER > PART ? CORNER : PART)];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int nb0 = blockIdx.x * NT, row0 = blockIdx.y * ROWS;
+    char *corner = smem + wave * CORNER;
+
+    // column blocks beyond the last one repeat it; they are not stored
+    const u4 *codes[NT];
+    const elem *scales[NT], *zeros[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t nb = nb0 + n < p.NB ? nb0 + n : p.NB - 1;
+        codes[n] = p.codes + nb * p.KB * 64 + lane;
+        scales[n] = static_cast<const elem *>(p.scales) + nb * p.GB * 16 + c;
+        zeros[n] = static_cast<const elem *>(p.zeros) + nb * p.GB * 16 + c;
+    }
+    const int rows = p.M - row0 < ROWS ? p.M - row0 : ROWS;
+    const elem *A = static_cast<const elem *>(p.A) + row0 * p.lda;
+
+    u4 code[AHEAD][NT], a[AHEAD][LOADS];
+    elem scale[AHEAD][NT], zero[AHEAD][NT];  // of group lane / 16 of the chunk
+    auto load = [&](int d, int kb) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            code[d][n] = codes[n][(int64_t)kb * 64];
+            int group = kb * GROUPS + g % GROUPS;
+            if (group >= p.GB) group = p.GB - 1;  // beyond K: A's elements there are zeros
+            scale[d][n] = scales[n][group * 16];
+            if (ZEROS) zero[d][n] = zeros[n][group * 16];
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+            if (4 * i < rows) {
+                const int row = 4 * i + g;
+                a[d][i] = load_row8<T>(A + (row < rows ? row : rows - 1) * p.lda, kb * 128 + 8 * c, p.K);
+            }
+    };
+    vec8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (elem)1.f;
+    f4 acc[MT][NT] = {};
+    auto use = [&](int d) {
+        // row r's 16-byte piece j stands at j ^ (r % 16)
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) *reinterpret_cast<u4 *>(corner + (4 * i + g) * 256 + 16 * (c ^ ((4 * i + g) & 15))) = a[d][i];
+        lanes_meet();
+#pragma unroll
+        for (int s = 0; s < GROUPS; ++s) {
+            f4 sum[MT][NT] = {}, all[MT] = {};
+#pragma unroll
+            for (int i = 0; i < STEPS; ++i) {
+                const int j = s * STEPS + i;
+                vec8 b[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) b[n] = unpack<T>(code[d][n][j]);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const vec8 x = *reinterpret_cast<const vec8 *>(corner + (16 * t + c) * 256 + 16 * ((4 * j + g) ^ c));
+                    all[t] = T::mfma(x, ones, all[t]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sum[t][n] = T::mfma(x, b[n], sum[t][n]);
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float f = (float)scale[d][n], shift = ZEROS ? 16.f + (float)zero[d][n] : 24.f;
+                if (GROUPS > 1) {
+                    f = __shfl(f, 16 * s + c);
+                    if (ZEROS) shift = __shfl(shift, 16 * s + c);
+                }
+#pragma unroll
+                for (int t = 0; t < MT; ++t)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[t][n][e] += f * (sum[t][n][e] - shift * all[t][e]);
+            }
+        }
+        lanes_meet();
+    };
+
+#pragma unroll
+    for (int d = 0; d < AHEAD; ++d)
+        if (wave + WAVES * d < p.KB) load(d, wave + WAVES * d);
+    for (int kb = wave; kb < p.KB; kb += WAVES * AHEAD) {
+#pragma unroll
+        for (int d = 0; d < AHEAD; ++d) {
+            const int at = kb + WAVES * d;
+            if (at < p.KB) use(d);
+            if (at + WAVES * AHEAD < p.KB) load(d, at + WAVES * AHEAD);
+        }
+    }
+
+    __syncthreads();
+    q4_store<T, MT, NT, WAVES>(p, acc, smem, row0, nb0);
 }
 
+// 16 MT rows, MT 2 or 4, of which a wave could not hold the next chunks in
+// registers.  DIRECT (16-byte aligned rows of A and K a multiple of 8): A goes
+// straight to the wave's own part of LDS, AHEAD half chunks (16 MT rows of 64
+// k) before it is used; rows beyond M and k beyond K are read past the end of
+// a buffer, which gives zeros.  Else one half chunk ahead is in registers.
+// The codes, scales and zeros of the next two chunks stay in registers.
+template <int MT, int NT, bool DIRECT>
+struct Q4Lds {
+    static constexpr int AHEAD = MT == 4 || !DIRECT ? 1 : 3, SLOTS = DIRECT ? AHEAD + 1 : 1;
+    static constexpr int HALF = 16 * MT * 128, COPIES = 2 * MT, WAVE = SLOTS * HALF, PART = MT * NT * 1024;
+    static constexpr int SIZE = WAVES * (WAVE > PART ? WAVE : PART);
+};
+
+template <class T, int MT, int NT, int STEPS, bool ZEROS, bool DIRECT>
+__global__ void __launch_bounds__(64 * WAVES) q4_rows_kernel(Q4Args p)
+{
+    typedef Q4Lds<MT, NT, DIRECT> L;
+    typedef typename T::elem elem;
+    typedef typename T::vec8 vec8;
+    constexpr int GROUPS = 4 / STEPS, ROWS = 16 * MT;
+    __shared__ __attribute__((aligned(16))) char smem[L::SIZE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    const int nb0 = blockIdx.x * NT, row0 = blockIdx.y * ROWS;
+    char *mine = smem + wave * L::WAVE;
+    const int count = p.KB > wave ? (p.KB - wave + WAVES - 1) / WAVES : 0;
+
+    const u4 *codes[NT];
+    const elem *scales[NT], *zeros[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int64_t nb = nb0 + n < p.NB ? nb0 + n : p.NB - 1;
+        codes[n] = p.codes + nb * p.KB * 64 + lane;
+        scales[n] = static_cast<const elem *>(p.scales) + nb * p.GB * 16 + c;
+        zeros[n] = static_cast<const elem *>(p.zeros) + nb * p.GB * 16 + c;
+    }
+    u4 code[2][NT];
+    elem scale[2][NT], zero[2][NT];  // of group lane / 16 of the chunk
+    auto load = [&](int d, int i) {
+        const int kb = wave + WAVES * i;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            code[d][n] = codes[n][(int64_t)kb * 64];
+            int group = kb * GROUPS + g % GROUPS;
+            if (group >= p.GB) group = p.GB - 1;
+            scale[d][n] = scales[n][group * 16];
+            if (ZEROS) zero[d][n] = zeros[n][group * 16];
+        }
+    };
+
+    // row r's 16-byte piece j of a half chunk stands at j ^ (r % 8)
+    const int piece = (lane & 7) ^ (lane >> 3);
+    int off[DIRECT ? L::COPIES : 1];
+    if constexpr (DIRECT) {
+#pragma unroll
+        for (int i = 0; i < L::COPIES; ++i) {
+            const int row = 8 * i + (lane >> 3);
+            off[i] = row0 + row < p.M ? (int)(row * p.lda * 2) + 16 * piece : OOB_OFFSET;
+        }
+    }
+    const elem *A = static_cast<const elem *>(p.A) + row0 * p.lda;
+    const int rows = p.M - row0 < ROWS ? p.M - row0 : ROWS;
+    u4 next[DIRECT ? 1 : L::COPIES];
+    // half chunk u; DIRECT: those past the wave's last one are of length 0, so
+    // that the number of copies under way is always the same
+    auto copy = [&](int u) {
+        const int k0 = (wave + WAVES * (u >> 1)) * 128 + 64 * (u & 1);
+        const bool real = (u >> 1) < count;
+        if constexpr (DIRECT) {
+            const bool past = k0 + 8 * piece >= p.K;
+            const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<elem *>(A + (real ? k0 : 0)), (short)0,
+                                                                                real ? MAX_RECORDS : 0, RSRC_WORD3);
+#pragma unroll
+            for (int j = 0; j < L::COPIES; ++j)
+                buffer_load16_lds(rs, mine + u % L::SLOTS * L::HALF + 1024 * j, past ? OOB_OFFSET : off[j], 0);
+        } else if (real) {
+#pragma unroll
+            for (int j = 0; j < L::COPIES; ++j)
+                if (8 * j < rows) {
+                    const int row = 8 * j + (lane >> 3);
+                    next[j] = load_row8<T>(A + (row < rows ? row : rows - 1) * p.lda, k0 + 8 * piece, p.K);
+                }
+        }
+    };
+
+    vec8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (elem)1.f;
+    f4 acc[MT][NT] = {};
+    f4 sum[MT][NT], all[MT];
+    auto use = [&](int d, int i) {
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            const int u = 2 * i + half;
+            if constexpr (DIRECT) {
+                wait_vm_lgkm0<63>();  // the slot's last fragments have been read
+                copy(u + L::AHEAD);
+                wait_vm_lgkm0<L::COPIES * L::AHEAD>();
+            } else {
+                lanes_meet();
+#pragma unroll
+                for (int j = 0; j < L::COPIES; ++j) *reinterpret_cast<u4 *>(mine + 1024 * j + 16 * lane) = next[j];
+                copy(u + 1);
+            }
+            lanes_meet();
+            const char *a = mine + u % L::SLOTS * L::HALF;
+#pragma unroll
+            for (int j = 2 * half; j < 2 * half + 2; ++j) {
+                if (j % STEPS == 0) {
+#pragma unroll
+                    for (int t = 0; t < MT; ++t) {
+                        all[t] = f4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) sum[t][n] = f4{0.f, 0.f, 0.f, 0.f};
+                    }
+                }
+                vec8 b[NT];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) b[n] = unpack<T>(code[d][n][j]);
+#pragma unroll
+                for (int t = 0; t < MT; ++t) {
+                    const vec8 x = *reinterpret_cast<const vec8 *>(a + (16 * t + c) * 128 + 16 * ((4 * (j & 1) + g) ^ (c & 7)));
+                    all[t] = T::mfma(x, ones, all[t]);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sum[t][n] = T::mfma(x, b[n], sum[t][n]);
+                }
+                if (j % STEPS == STEPS - 1) {
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        float f = (float)scale[d][n], shift = ZEROS ? 16.f + (float)zero[d][n] : 24.f;
+                        if (GROUPS > 1) {
+                            f = __shfl(f, 16 * (j / STEPS) + c);
+                            if (ZEROS) shift = __shfl(shift, 16 * (j / STEPS) + c);
+                        }
+#pragma unroll
+                        for (int t = 0; t < MT; ++t)
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) acc[t][n][e] += f * (sum[t][n][e] - shift * all[t][e]);
+                    }
+                }
+            }
+        }
+    };
+    if (count > 0) {
+        load(0, 0);
+        if (count > 1) load(1, 1);
+#pragma unroll
+        for (int u = 0; u < L::AHEAD; ++u) copy(u);
+    }
+    for (int i = 0; i < count; i += 2) {
+        use(0, i);
+        if (i + 2 < count) load(0, i + 2);
+        if (i + 1 < count) {
+            use(1, i + 1);
+            if (i + 3 < count) load(1, i + 3);
+        }
+    }
+    wait_vm_lgkm0<0>();
+    __syncthreads();
+    q4_store<T, MT, NT, WAVES>(p, acc, smem, row0, nb0);
+}
+
+template <class T, int MT, int NT, bool DIRECT>
+gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
+{
+    const dim3 grid((unsigned)div_up(a.NB, NT), (unsigned)div_up(a.M, 16 * MT)), block(64 * WAVES);
+    const bool z = a.zeros != nullptr;
+    if constexpr (MT == 1) {
+        constexpr int AHEAD = NT == 4 ? 2 : 4;
+        if (group == 32) return z ? launch(q4_kernel<T, NT, 1, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 1, false, AHEAD>, grid, block, s, a);
+        if (group == 64) return z ? launch(q4_kernel<T, NT, 2, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 2, false, AHEAD>, grid, block, s, a);
+        return z ? launch(q4_kernel<T, NT, 4, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 4, false, AHEAD>, grid, block, s, a);
+    } else {
+        if (group == 32)
+            return z ? launch(q4_rows_kernel<T, MT, NT, 1, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 1, false, DIRECT>, grid, block, s, a);
+        if (group == 64)
+            return z ? launch(q4_rows_kernel<T, MT, NT, 2, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 2, false, DIRECT>, grid, block, s, a);
+        return z ? launch(q4_rows_kernel<T, MT, NT, 4, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 4, false, DIRECT>, grid, block, s, a);
+    }
+}
+
+// Which kernel: one 16-row block with its chunks in registers up to 16 rows,
+// else blocks of 32 or 64 rows.  Column blocks of a workgroup: as many as
+// leave 256 workgroups (a workgroup reads all of its rows of A, so fewer,
+// wider ones read less).
 template <class T>
 gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
 {
-    if (a.M <= 16) return run_q4<T, 1>(a, group, s);
-    return a.M <= 32 ? run_q4<T, 2>(a, group, s) : run_q4<T, 4>(a, group, s);
+    if (a.M <= 16) {
+        if (a.NB >= 1024) return run_q4<T, 1, 4, true>(a, group, s);
+        return a.NB >= 512 ? run_q4<T, 1, 2, true>(a, group, s) : run_q4<T, 1, 1, true>(a, group, s);
+    }
+    const bool direct = a.lda % 8 == 0 && a.K % 8 == 0 && a.lda < (1 << 23) && aligned_to(a.A, 16);
+    if (!direct) return a.M <= 32 ? run_q4<T, 2, 1, false>(a, group, s) : run_q4<T, 4, 1, false>(a, group, s);
+    if (a.NB >= 512) return a.M <= 32 ? run_q4<T, 2, 2, true>(a, group, s) : run_q4<T, 4, 2, true>(a, group, s);
+    return a.M <= 32 ? run_q4<T, 2, 1, true>(a, group, s) : run_q4<T, 4, 1, true>(a, group, s);
 }
 
 // One thread a word.
@@ -207,6 +452,7 @@ extern "C" gba_status gba_q4_linear(const gba_q4_weight *w, int64_t M, const voi
     a.M = (int)M;
     a.N = (int)N;
     a.K = (int)K;
+    a.NB = (int)div_up(N, 16);
     a.KB = (int)div_up(K, 128);
     a.GB = (int)div_up(K, w->group);
     a.act = act;

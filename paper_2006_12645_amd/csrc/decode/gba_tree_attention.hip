@@ -152,14 +152,6 @@ __device__ __forceinline__ float across_max(float x)
     return fmaxf(x, __shfl_xor(x, 16));
 }
 
-// What one lane of a wave has written to LDS, another one reads after this: a
-// wave's accesses run in order, so only the compiler has to keep it.
-__device__ __forceinline__ void lanes_meet()
-{
-    asm volatile("" ::: "memory");
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Waves of a workgroup: as many as have room for two tiles in LDS.
 constexpr int waves_of(int dp) { return dp == 256 ? 2 : 4; }
 
