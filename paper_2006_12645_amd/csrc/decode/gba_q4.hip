@@ -362,7 +362,10 @@ gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
     const dim3 grid((unsigned)div_up(a.NB, NT), (unsigned)div_up(a.M, 16 * MT)), block(64 * WAVES);
     const bool z = a.zeros != nullptr;
     if constexpr (MT == 1) {
-        constexpr int AHEAD = NT == 4 ? 2 : 4;
+        // one chunk of four column blocks or two of fewer: more waves fit with
+        // fewer registers (1 x 8192 x 32768: 28.5 us against 32.2 with twice
+        // as many chunks ahead)
+        constexpr int AHEAD = NT == 4 ? 1 : 2;
         if (group == 32) return z ? launch(q4_kernel<T, NT, 1, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 1, false, AHEAD>, grid, block, s, a);
         if (group == 64) return z ? launch(q4_kernel<T, NT, 2, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 2, false, AHEAD>, grid, block, s, a);
         return z ? launch(q4_kernel<T, NT, 4, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 4, false, AHEAD>, grid, block, s, a);
@@ -388,7 +391,9 @@ gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
     }
     const bool direct = a.lda % 8 == 0 && a.K % 8 == 0 && a.lda < (1 << 23) && aligned_to(a.A, 16);
     if (!direct) return a.M <= 32 ? run_q4<T, 2, 1, false>(a, group, s) : run_q4<T, 4, 1, false>(a, group, s);
-    if (a.NB >= 512) return a.M <= 32 ? run_q4<T, 2, 2, true>(a, group, s) : run_q4<T, 4, 2, true>(a, group, s);
+    // groups of 32 and two column blocks need more registers than there are
+    // (64 x 8192 x 8192: 75 us against 41)
+    if (a.NB >= 512 && (a.M <= 32 || group != 32)) return a.M <= 32 ? run_q4<T, 2, 2, true>(a, group, s) : run_q4<T, 4, 2, true>(a, group, s);
     return a.M <= 32 ? run_q4<T, 2, 1, true>(a, group, s) : run_q4<T, 4, 1, true>(a, group, s);
 }
 
