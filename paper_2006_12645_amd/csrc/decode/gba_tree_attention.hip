@@ -39,7 +39,7 @@ struct AttentionArgs {
     int slots;         // runs of keys there is room for: at least as many as there are
     int target;        // runs to aim at (0: one for each request)
     int32_t *first_run;  // [requests][2]: a request's first run and how many it has
-    float *part;       // [slots][heads][row_tiles]: 16 RT x dim sums, then 16 RT maxima, 16 RT sums of weights
+    float *part;       // [slots][heads][row_tiles]: rows x dim sums, then as many maxima and sums of weights
 };
 
 constexpr int KEYS = 32;        // of a tile
@@ -48,8 +48,7 @@ constexpr float SLACK = 8.f;
 
 // A request's new tokens and keys, none for one with too many.
 struct Request {
-    int first, fresh;
-    int64_t kept, end;
+    int first, fresh, kept, end;
 };
 
 __device__ __forceinline__ Request request_of(const AttentionArgs &p, int r)
@@ -59,25 +58,54 @@ __device__ __forceinline__ Request request_of(const AttentionArgs &p, int r)
     q.fresh = min(p.offsets[r + 1], p.tokens) - q.first;
     if (q.first < 0 || q.fresh < 0 || q.fresh > p.max_new) q.fresh = 0;
     q.kept = max(p.lens[r], 0);
-    q.end = min(q.kept + q.fresh, (int64_t)p.width * p.block_size);
+    q.end = (int)min((int64_t)q.kept + q.fresh, (int64_t)p.width * p.block_size);
     return q;
 }
 
-// A value that every lane holds, in scalar registers.
-__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ int64_t uniform(int64_t v)
+// Running sums over a wave, in the order of its lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x)
 {
-    const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)v), hi = __builtin_amdgcn_readfirstlane((unsigned)(v >> 32));
-    return (int64_t)((uint64_t)hi << 32 | lo);
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_sums(int x)
+{
+    x += moved<0x111, 0xF>(x);  // one lane up, within 16
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);  // lanes 15 and 47 to the 16 after them
+    x += moved<0x143, 0xC>(x);  // lane 31 to the 32 after it
+    return x;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float x)
+{
+    return __builtin_bit_cast(float, moved<CTRL, ROWS>(__builtin_bit_cast(int, x)));
+}
+__device__ __forceinline__ float wave_total(float x)
+{
+    x += moved<0x111, 0xF>(x);
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);
+    x += moved<0x143, 0xC>(x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// Which request's run number x is, and which keys: [from, to) of request r;
-// r = -1 where there is no such run.  n, first: the request's runs.
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Run number x: keys [from, to) of request r, one of the n runs that begin
+// with number `first`; r = -1 where there is no such run.
 struct Run {
-    int r, n, first;
-    int64_t from, to;
+    int r, n, first, from, to;
 };
 
+// Every run but a request's last is of one length, a multiple of `step`:
+// the mean of all keys over p.target runs, so there are no more than
+// p.target + p.requests.  The sum of the lengths is one in 24 bits; the
+// factor covers its rounding.
 __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, int step)
 {
     Run u;
@@ -90,31 +118,25 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
         u.to = uniform(q.end);
         return u;
     }
-    int64_t total = 0;
+    float keys = 0.f;
+    Request q = {0, 0, 0, 0};
     for (int r = lane; r < p.requests; r += 64) {
-        const Request q = request_of(p, r);
-        if (q.fresh > 0) total += q.end;
+        q = request_of(p, r);
+        if (q.fresh > 0) keys += (float)q.end;
     }
-    for (int d = 32; d; d >>= 1) total += __shfl_xor(total, d);
-    int64_t length = (uniform(total) + p.target - 1) / p.target;
-    length = (length + step - 1) / step * step;
+    const float mean = wave_total(keys) / (float)p.target * 1.00001f;
+    const int most = INT_MAX / step * step;
+    int length = mean < (float)(most - step) ? ((int)mean / step + 1) * step : most;
     if (length < SHORTEST) length = SHORTEST;
+    length = uniform(length);
     u.r = -1;
     int before = 0;
     for (int base = 0; base < p.requests; base += 64) {
         const int r = base + lane;
+        if (p.requests > 64 && r < p.requests) q = request_of(p, r);
         int n = 0;
-        int64_t end = 0;
-        if (r < p.requests) {
-            const Request q = request_of(p, r);
-            end = q.end;
-            if (q.fresh > 0) n = end > length ? (int)((end + length - 1) / length) : 1;
-        }
-        int upto = n;
-        for (int d = 1; d < 64; d <<= 1) {
-            const int y = __shfl_up(upto, d);
-            if (lane >= d) upto += y;
-        }
+        if (r < p.requests && q.fresh > 0) n = q.end > length ? (q.end - 1) / length + 1 : 1;
+        const int upto = wave_sums(n);
         const uint64_t past = __ballot(before + upto > x);
         if (past != 0) {
             const int l = __ffsll((unsigned long long)past) - 1;
@@ -122,8 +144,8 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
             u.n = __builtin_amdgcn_readlane(n, l);
             u.first = before + __builtin_amdgcn_readlane(upto, l) - u.n;
             u.from = (x - u.first) * length;
-            const int64_t e = uniform(__shfl(end, l));
-            u.to = u.from + length < e ? u.from + length : e;
+            const int end = __builtin_amdgcn_readlane(q.end, l);
+            u.to = end - u.from > length ? u.from + length : end;
             return u;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
@@ -152,89 +174,75 @@ __device__ __forceinline__ float across_max(float x)
     return fmaxf(x, __shfl_xor(x, 16));
 }
 
-// Waves of a workgroup: as many as have room for two tiles in LDS.
-constexpr int waves_of(int dp) { return dp == 256 ? 2 : 4; }
-
-// DP: dim, padded.  RT: blocks of 16 rows.  WHOLE: 16 consecutive keys, from a
-// multiple of 16 on, are in one block.
-template <class T, int DP, int RT, bool WHOLE>
-struct Attention {
-    typedef typename T::elem elem;
-    typedef typename T::vec8 vec8;
-    static constexpr int WAVES = waves_of(DP);
-    static constexpr int CPR = DP / 8;         // 16-byte chunks of a row
-    static constexpr int KPI = 64 / CPR;       // keys that one 64-lane copy covers
-    static constexpr int COPIES = KEYS / KPI;  // of a tile of K or V
-    static constexpr int ROW = 2 * DP, TILE = KEYS * ROW, STAGE = 2 * TILE;
-    static constexpr int SMEM = WAVES * 2 * STAGE;
+// A workgroup's waves: RG of them take 16 RT rows each of the same keys, and
+// KG such groups the tiles of a run in turn.  One group keeps STAGES tiles in
+// LDS.
+template <int DP, int RG>
+struct Shared {
+    static constexpr int KG = RG == 8 ? 1 : RG == 4 || DP == 256 ? 2 : 4, WAVES = RG * KG;
+    static constexpr int STAGES = RG == 8 ? 4 : RG == 4 ? 3 : 2;
+    static constexpr int CPR = DP / 8;                   // 16-byte chunks of a row
+    static constexpr int KPI = 64 / CPR;                 // keys that one 64-lane copy covers
+    static constexpr int COPIES = KEYS / KPI;            // of a tile of K or V
+    static constexpr int ROW = 2 * DP, TILE = KEYS * ROW, STAGE = 2 * TILE, GROUP = STAGES * STAGE;
 };
 
-template <class T, int DP, int RT, bool WHOLE>
-__global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(AttentionArgs p)
+// The join of the key groups needs 16 RT rows of fp32 for each wave.
+template <int DP, int RT, int RG>
+constexpr int lds_bytes()
 {
-    typedef Attention<T, DP, RT, WHOLE> C;
-    typedef typename C::elem elem;
-    typedef typename C::vec8 vec8;
-    constexpr int WAVES = C::WAVES, CPR = C::CPR, KPI = C::KPI, COPIES = C::COPIES, ROW = C::ROW, TILE = C::TILE;
-    constexpr int STEPS = DP / 32, BLOCKS = DP / 16;
-    __shared__ __attribute__((aligned(16))) char smem[C::SMEM];
+    typedef Shared<DP, RG> S;
+    return S::KG * S::GROUP > S::WAVES * 16 * RT * 4 * DP ? S::KG * S::GROUP : S::WAVES * 16 * RT * 4 * DP;
+}
+template <int DP, int RG>
+constexpr int threads_of()
+{
+    return 64 * Shared<DP, RG>::WAVES;
+}
+
+// DP: dim, padded.  RT: blocks of 16 rows of a wave.  WHOLE: 16 consecutive
+// keys, from a multiple of 16 on, are in one block, and go straight to LDS;
+// else (RG 1 only) they pass through registers, which hold the next tile.
+template <class T, int DP, int RT, int RG, bool WHOLE>
+__global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) attention_kernel(AttentionArgs p)
+{
+    typedef Shared<DP, RG> S;
+    typedef typename T::elem elem;
+    typedef typename T::vec8 vec8;
+    static_assert(WHOLE || RG == 1, "waves share only what goes straight to LDS");
+    constexpr int WAVES = S::WAVES, KG = S::KG, STAGES = WHOLE ? S::STAGES : 1;
+    constexpr int CPR = S::CPR, KPI = S::KPI, COPIES = S::COPIES, ROW = S::ROW, TILE = S::TILE;
+    constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = 16 * RT * RG;
+    __shared__ __attribute__((aligned(16))) char smem[lds_bytes<DP, RT, RG>()];
     __shared__ float tops[WAVES][16 * RT], sums[WAVES][16 * RT];
 
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), rg = wave % RG, kg = wave / RG;
     const int c = lane & 15, g = lane >> 4;
     // The row tiles of one run and head have ids 8 apart: the same XCD's L2.
     const int xcd = blockIdx.x & 7, rest = blockIdx.x >> 3;
     const int row_tile = rest % p.row_tiles, item = rest / p.row_tiles * 8 + xcd;
     const int head = item % p.heads, x = item / p.heads;
     if (x >= p.slots) return;
-    const Run run = run_of(p, x, lane, KEYS * WAVES);
+    const Run run = run_of(p, x, lane, KEYS * KG);
     if (run.r < 0) return;
     Request rq = request_of(p, run.r);
     rq.first = uniform(rq.first);
     rq.fresh = uniform(rq.fresh);
     rq.kept = uniform(rq.kept);
-    const int rows = rq.fresh * p.share, row0 = row_tile * (16 * RT);
+    const int rows = rq.fresh * p.share, row0 = row_tile * ROWS;
     if (p.target != 0 && run.first == x && head == 0 && row_tile == 0 && threadIdx.x == 0) {
         p.first_run[2 * run.r] = x;
         p.first_run[2 * run.r + 1] = run.n;
     }
     if (row0 >= rows) return;
 
-    // this lane's rows: as the second operand, row c of each block; dim 32 s + 8 g on
-    vec8 query[RT][STEPS];
-    uint64_t sees[RT];  // bits of the new tokens that the row sees
-    int index[RT];      // its token among the new ones
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int row = row0 + 16 * i + c;
-        const bool real = row < rows;
-        index[i] = real ? row / p.share : 0;
-        const int token = rq.first + index[i];
-        const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? row % p.share : 0)) * p.q_head;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int d = 32 * s + 8 * g;
-            const u4 none = {0, 0, 0, 0};
-            query[i][s] = real && d < p.dim ? *reinterpret_cast<const vec8 *>(q + d) : __builtin_bit_cast(vec8, none);
-        }
-        sees[i] = p.mask != nullptr ? p.mask[token] : 0;
-    }
-
-    f4 out[RT][BLOCKS] = {}, weights[RT] = {};
-    float top[RT], base2[RT];  // running maximum; what is subtracted (0 while there is none)
-#pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        top[i] = -INFINITY;
-        base2[i] = 0.f;
-    }
-
-    char *mine = smem + wave * (2 * C::STAGE);
-    const int tiles = (int)((run.to - run.from + KEYS - 1) / KEYS);
-    const int count = tiles > wave ? (tiles - wave + WAVES - 1) / WAVES : 0;  // of this wave
-    const int32_t *entries = p.table + (int64_t)run.r * p.width;
-    auto key0 = [&](int n) { return run.from + (int64_t)KEYS * (wave + WAVES * n); };
-
     // ---- copies of a tile: 1 KB each, lane l the chunk at byte 16 l
+    char *mine = smem + kg * S::GROUP;
+    const int tiles = (run.to - run.from + KEYS - 1) / KEYS;
+    const int count = tiles > kg ? (tiles - kg + KG - 1) / KG : 0;  // of this group
+    const int rounds = RG == 1 ? count : (tiles + KG - 1) / KG;     // of every group, where waves wait for each other
+    const int32_t *entries = p.table + (int64_t)run.r * p.width;
+    auto key0 = [&](int n) { return run.from + KEYS * (kg + KG * n); };
     const int in_copy = lane / CPR, place = lane % CPR;
     constexpr int PER_HALF = COPIES / 2;
     const char *k_head = reinterpret_cast<const char *>(static_cast<const elem *>(p.k) + head * p.k_head);
@@ -252,45 +260,54 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
     // block and token of key lane % 32 of the next tile, and its registers.
     int entry = -1, within = 0, entries_from = 0;
     u4 k_next[WHOLE ? 1 : COPIES], v_next[WHOLE ? 1 : COPIES];
-    unsigned next_there = 0, there = 0;  // keys of the tile that exist
-
     auto look_up = [&](int n) {
-        const int64_t pos = WHOLE ? key0(n + lane / 2) + 16 * (lane & 1) : key0(n) + (lane & 31);
+        const int pos = WHOLE ? key0(n + lane / 2) + 16 * (lane & 1) : key0(n) + (lane & 31);
         entry = -1;
         if (pos < run.to) {
-            const int page = (int)pos / p.block_size;
-            within = (int)pos - page * p.block_size;
+            const int page = pos / p.block_size;
+            within = pos - page * p.block_size;
             const int b = entries[page];
             entry = b >= 0 && b < p.num_blocks ? b : -1;
         }
         entries_from = n;
     };
-    auto copy = [&](int n, int stage) {
-        char *k_lds = mine + stage * C::STAGE, *v_lds = k_lds + TILE;
+    // How many keys of a half of tile n exist (WHOLE): those up to the run's
+    // end, if its block does.
+    auto keys_of = [&](int n, int h) {
+        const int b = __builtin_amdgcn_readlane(entry, 2 * (n - entries_from) + h), left = run.to - (key0(n) + 16 * h);
+        return b < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+    };
+    // Copies tile n, and says which of its keys exist.  A share of a group's
+    // copies for each of its waves; none are left out past the last tile, so
+    // that the number under way is always the same.
+    constexpr int MY_COPIES = 2 * COPIES / RG;
+    auto copy = [&](int n) -> unsigned {
         if constexpr (WHOLE) {
+            unsigned there = 0;
+            char *k_lds = mine + n % STAGES * S::STAGE, *v_lds = k_lds + TILE;
             if (n - entries_from == 32) look_up(n);
-            next_there = 0;
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int at = 2 * (n - entries_from) + h;
-                const int b = __builtin_amdgcn_readlane(entry, at), t = __builtin_amdgcn_readlane(within, at);
-                const int64_t left = run.to - (key0(n) + 16 * h);
-                const int keys = b < 0 ? 0 : left < 16 ? (int)left : 16;
-                next_there |= ((1u << keys) - 1) << (16 * h);
+                const int at = 2 * (n - entries_from) + h, keys = n < count ? keys_of(n, h) : 0;
+                there |= ((1u << keys) - 1) << (16 * h);
+                const int b = keys ? __builtin_amdgcn_readlane(entry, at) : 0, t = keys ? __builtin_amdgcn_readlane(within, at) : 0;
                 // beyond the last key the buffer has ended: zeros
-                const char *kb = k_head + 2 * ((b < 0 ? 0 : b) * p.k_block + t * p.k_token);
-                const char *vb = v_head + 2 * ((b < 0 ? 0 : b) * p.v_block + t * p.v_token);
-                const __amdgpu_buffer_rsrc_t kr = __builtin_amdgcn_make_buffer_rsrc(
-                    const_cast<char *>(kb), (short)0, keys ? (int)((keys - 1) * p.k_token + p.dim) * 2 : 0, RSRC_WORD3);
-                const __amdgpu_buffer_rsrc_t vr = __builtin_amdgcn_make_buffer_rsrc(
-                    const_cast<char *>(vb), (short)0, keys ? (int)((keys - 1) * p.v_token + p.dim) * 2 : 0, RSRC_WORD3);
+                const __amdgpu_buffer_rsrc_t kr =
+                    __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(k_head + 2 * (b * p.k_block + t * p.k_token)), (short)0,
+                                                      keys ? (int)((keys - 1) * p.k_token + p.dim) * 2 : 0, RSRC_WORD3);
+                const __amdgpu_buffer_rsrc_t vr =
+                    __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(v_head + 2 * (b * p.v_block + t * p.v_token)), (short)0,
+                                                      keys ? (int)((keys - 1) * p.v_token + p.dim) * 2 : 0, RSRC_WORD3);
 #pragma unroll
-                for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(kr, k_lds + 1024 * (PER_HALF * h + i), k_off[i], 0);
-#pragma unroll
-                for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(vr, v_lds + 1024 * (PER_HALF * h + i), v_off[i], 0);
+                for (int i = 0; i < PER_HALF; ++i) {
+                    const int j = PER_HALF * h + i;
+                    if (RG == 1 || (2 * j) % RG == rg) buffer_load16_lds(kr, k_lds + 1024 * j, k_off[i], 0);
+                    if (RG == 1 || (2 * j + 1) % RG == rg) buffer_load16_lds(vr, v_lds + 1024 * j, v_off[i], 0);
+                }
             }
+            return there;
         } else {
-            next_there = (unsigned)__ballot(entry >= 0);
+            const unsigned there = (unsigned)__ballot(entry >= 0);
             const int block = entry, token = within;
             if (n + 1 < count) look_up(n + 1);
 #pragma unroll
@@ -302,36 +319,75 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
                 if (b >= 0 && 8 * kc < p.dim) k_next[i] = *reinterpret_cast<const u4 *>(k_head + 2 * (b * p.k_block + t * p.k_token) + 16 * kc);
                 if (b >= 0 && 8 * vc < p.dim) v_next[i] = *reinterpret_cast<const u4 *>(v_head + 2 * (b * p.v_block + t * p.v_token) + 16 * vc);
             }
+            return there;
         }
     };
+    if (rounds > 0) look_up(0);
+
+    // ---- this wave's rows: as the second operand, row c of each block; dim
+    // 32 s + 8 g on
+    vec8 query[RT][STEPS];
+    uint64_t sees[RT];  // bits of the new tokens that the row sees
+    int index[RT];      // its token among the new ones
+    const int wave_row0 = row0 + rg * 16 * RT;
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int row = wave_row0 + 16 * i + c;
+        const bool real = row < rows;
+        index[i] = real ? row / p.share : 0;
+        const int token = rq.first + index[i];
+        const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? row % p.share : 0)) * p.q_head;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int d = 32 * s + 8 * g;
+            const u4 none = {0, 0, 0, 0};
+            query[i][s] = real && d < p.dim ? *reinterpret_cast<const vec8 *>(q + d) : __builtin_bit_cast(vec8, none);
+        }
+        sees[i] = p.mask != nullptr ? p.mask[token] : 0;
+    }
+    const bool masked = p.mask != nullptr;
+
+    f4 out[RT][BLOCKS] = {}, weights[RT] = {};
+    float top[RT], base2[RT];  // running maximum; what is subtracted (0 while there is none)
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        top[i] = -INFINITY;
+        base2[i] = 0.f;
+    }
 
     // ---- LDS addresses of the fragments
-    int k_at[STEPS], v_at;
+    int k_at[STEPS];
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) k_at[s] = c * ROW + 16 * ((4 * s + g) ^ swap_k<DP>(c));
     const int v_key = 4 * g + (c >> 2), v_swap = 16 * swap_v<DP>(v_key);
-    v_at = v_key * ROW + 16 * ((c & 3) >> 1) + 8 * (c & 1);
+    const int v_at = v_key * ROW + 16 * ((c & 3) >> 1) + 8 * (c & 1);
+    vec8 ones;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ones[e] = (elem)1.f;
 
-    const bool masked = p.mask != nullptr;
-    if (count > 0) {
-        look_up(0);
-        wait_vm_lgkm0<0>();  // the rows too: from here on only copies are under way
-        copy(0, 0);
+    unsigned ahead[WHOLE ? STAGES - 1 : 1];  // which keys of the tiles under way exist
+    if constexpr (WHOLE) {
+        wait_vm_lgkm0<0>();  // the rows and blocks: from here on only copies are under way
+        if (rounds > 0) {
+#pragma unroll
+            for (int n = 0; n < STAGES - 1; ++n) ahead[n] = copy(n);
+        }
+    } else if (rounds > 0) {
+        ahead[0] = copy(0);
     }
-    const u4 ones_bits = __builtin_bit_cast(u4, vec8{(elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f});
-    const vec8 ones = __builtin_bit_cast(vec8, ones_bits);
-    for (int n = 0; n < count; ++n) {
-        const int stage = WHOLE ? n & 1 : 0;
-        const char *k_lds = mine + stage * C::STAGE, *v_lds = k_lds + TILE;
-        there = next_there;
-        if constexpr (WHOLE) {
-            wait_vm_lgkm0<63>();  // the other stage's fragments have been read
-            if (n + 1 < count) {
-                copy(n + 1, stage ^ 1);
-                wait_vm_lgkm0<2 * COPIES < 64 ? 2 * COPIES : 63>();
-            } else {
-                wait_vm_lgkm0<0>();
-            }
+    for (int n = 0; n < rounds; ++n) {
+        const char *k_lds = mine + n % STAGES * S::STAGE, *v_lds = k_lds + TILE;
+        const unsigned there = ahead[0];
+#pragma unroll
+        for (int i = 0; i + 2 < STAGES; ++i) ahead[i] = ahead[i + 1];
+        if constexpr (WHOLE && RG == 1) {
+            wait_vm_lgkm0<63>();  // the slot's last fragments have been read
+            ahead[STAGES - 2] = copy(n + STAGES - 1);
+            wait_vm_lgkm0<(STAGES - 1) * MY_COPIES>();
+        } else if constexpr (WHOLE) {
+            wait_vm_lgkm0<(STAGES - 2) * MY_COPIES>();
+            __builtin_amdgcn_s_barrier();  // every wave's share is there, and the last slot has been read
+            ahead[STAGES - 2] = copy(n + STAGES - 1);
         } else {
             lanes_meet();  // the last tile's fragments have been read
 #pragma unroll
@@ -339,9 +395,10 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
                 *reinterpret_cast<u4 *>(mine + 1024 * i + 16 * lane) = k_next[i];
                 *reinterpret_cast<u4 *>(mine + TILE + 1024 * i + 16 * lane) = v_next[i];
             }
-            if (n + 1 < count) copy(n + 1, 0);
+            if (n + 1 < count) ahead[0] = copy(n + 1);
         }
         lanes_meet();
+        if (there == 0) continue;
 
         // scores: keys 16 h + 4 g + e of the tile, row c of each block
         f4 score[RT][2];
@@ -356,9 +413,8 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
                 for (int i = 0; i < RT; ++i) score[i][h] = T::mfma(k, query[i][s], score[i][h]);
             }
         }
-        const int64_t first_key = key0(n);
-        const bool all = there == 0xFFFFFFFFu && first_key + KEYS <= rq.kept;
-        const int first_draft = (int)(first_key - rq.kept);
+        const int first_draft = key0(n) - rq.kept;  // of the new tokens, or below 0
+        const bool all = there == 0xFFFFFFFFu && first_draft + KEYS <= 0;
         vec8 weight[RT];
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
@@ -368,8 +424,7 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
             if (!all) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const int key = 16 * (e >> 2) + 4 * g + (e & 3);
-                    const int draft = first_draft + key;  // of the new tokens, or below 0
+                    const int key = 16 * (e >> 2) + 4 * g + (e & 3), draft = first_draft + key;
                     const bool in_tree = masked ? (draft < 64) & (int)((sees[i] >> (draft & 63)) & 1) : draft <= index[i];
                     const bool seen = ((there >> key) & 1) & ((draft < 0) | in_tree);
                     t[e] = seen ? t[e] : -INFINITY;
@@ -403,10 +458,13 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
         }
     }
 
-    // ---- the waves' sums, joined through LDS: row c, chunks of four of dim,
-    // chunk j of a row at j ^ c
+    // ---- the key groups' sums, joined through LDS: row c, chunks of four of
+    // dim, chunk j of a row at j ^ c
     wait_vm_lgkm0<0>();
+    if (RG > 1) __syncthreads();  // the tiles have been read
     lanes_meet();
+    char *sums_of_wave = smem + wave * (16 * RT * 4 * DP);
+    if (RG == 1) sums_of_wave = mine;
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         if (g == 0) {
@@ -415,80 +473,110 @@ __global__ void __launch_bounds__(64 * waves_of(DP), 1) attention_kernel(Attenti
         }
 #pragma unroll
         for (int b = 0; b < BLOCKS; ++b)
-            *reinterpret_cast<f4 *>(mine + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = out[i][b];
+            *reinterpret_cast<f4 *>(sums_of_wave + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = out[i][b];
     }
     __syncthreads();
     const bool whole_request = run.n == 1;
-    float *part = whole_request ? nullptr
-                                : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * (16 * RT) * (int64_t)(p.dim + 2);
+    float *part = whole_request ? nullptr : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * ROWS * (int64_t)(p.dim + 2);
     constexpr int FOURS = DP / 4;
-    for (int j = threadIdx.x; j < 16 * RT * FOURS; j += 64 * WAVES) {
-        const int row = j / FOURS, four = j % FOURS, d = 4 * four;
+    for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * WAVES) {
+        const int row = j / FOURS, four = j % FOURS, d = 4 * four, w0 = row / (16 * RT), r = row % (16 * RT);
         if (row0 + row >= rows || d >= p.dim) continue;
-        float m = tops[0][row];
+        float m = tops[w0][r];
 #pragma unroll
-        for (int w = 1; w < WAVES; ++w) m = fmaxf(m, tops[w][row]);
+        for (int w = 1; w < KG; ++w) m = fmaxf(m, tops[w0 + w * RG][r]);
         f4 o = {0.f, 0.f, 0.f, 0.f};
         float l = 0.f;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) {
-            const float share = tops[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[w][row] - m);
-            l += share * sums[w][row];
-            o += share * *reinterpret_cast<const f4 *>(smem + w * (2 * C::STAGE) + row * (4 * DP) + 16 * (four ^ (row & 15)));
+        for (int w = 0; w < KG; ++w) {
+            const int from = w0 + w * RG;
+            const float share = tops[from][r] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[from][r] - m);
+            l += share * sums[from][r];
+            o += share * *reinterpret_cast<const f4 *>(smem + (RG == 1 ? from * S::GROUP : from * (16 * RT * 4 * DP)) + r * (4 * DP) + 16 * (four ^ (r & 15)));
         }
         if (whole_request) {
             typedef elem four_t __attribute__((ext_vector_type(4)));
             const float inv = l > 0.f ? 1.f / l : 0.f;
             const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
-            four_t r;
+            four_t r4;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) r[e] = (elem)(o[e] * inv);
-            *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r;
+            for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+            *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r4;
         } else {
             *reinterpret_cast<f4 *>(part + row * p.dim + d) = o;
             if (four == 0) {
-                part[16 * RT * p.dim + row] = m;
-                part[16 * RT * (p.dim + 1) + row] = l;
+                part[ROWS * p.dim + row] = m;
+                part[ROWS * (p.dim + 1) + row] = l;
             }
         }
     }
 }
 
-// The runs of a request, added in their order; one wave a token and query head.
-template <class T>
+// The runs of a request, added in their order; one wave a token and query
+// head, lane l four elements of every (256 / DP)-th run: its share of the
+// weight comes from the lane that holds that run's maximum and sum.
+template <class T, int DP>
 __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_rows)
 {
     typedef typename T::elem elem;
+    constexpr int FOURS = DP / 4, AT_ONCE = 64 / FOURS;
     const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int t = (int)(id / p.q_heads), head = (int)(id % p.q_heads);
+    const int64_t id = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+    const int t = (int)(id / p.q_heads), head = (int)(id - (int64_t)t * p.q_heads);
     if (t >= p.tokens) return;
-    const int r = owner_of(p.offsets, p.requests, t);
+    int r = 0;  // the number of requests that end at or before t
+    for (int base = 0; base < p.requests; base += 64)
+        r += __popcll(__ballot(base + lane < p.requests && p.offsets[base + lane + 1] <= t));
     if (r >= p.requests) return;
+    const int x0 = p.first_run[2 * r], n = p.first_run[2 * r + 1];
     const Request rq = request_of(p, r);
-    if (rq.fresh == 0 || t < rq.first) return;
-    const int n = p.first_run[2 * r + 1], x0 = p.first_run[2 * r];
-    if (n <= 1) return;
+    if (rq.fresh == 0 || t < rq.first || n <= 1) return;
     const int row = (t - rq.first) * p.share + head % p.share, tile = row / tile_rows, in_tile = row % tile_rows;
     const int64_t tile_size = (int64_t)tile_rows * (p.dim + 2), stride = tile_size * p.heads * p.row_tiles;
     const float *part = p.part + (((int64_t)x0 * p.heads + head / p.share) * p.row_tiles + tile) * tile_size;
     const float *tops = part + tile_rows * p.dim + in_tile, *sums = tops + tile_rows;
-    float m = -INFINITY;
-    for (int i = lane; i < n; i += 64) m = fmaxf(m, tops[i * stride]);
-    for (int d = 32; d; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
-    float l = 0.f, o[4] = {};
-    for (int i = 0; i < n; ++i) {
-        const float top = tops[i * stride], share = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - m);
-        l += share * sums[i * stride];
+    const int d = 4 * (lane % FOURS), which = lane / FOURS;
+    const float *mine = part + (int64_t)in_tile * p.dim + (d < p.dim ? d : 0);
+    float m = -INFINITY, l = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int base = 0; base < n; base += 64) {
+        const int here = n - base < 64 ? n - base : 64;
+        const float top = lane < here ? tops[(base + lane) * stride] : -INFINITY;
+        const float sum = lane < here ? sums[(base + lane) * stride] : 0.f;
+        float next = top;
+        for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
+        next = fmaxf(next, m);
+        if (next == -INFINITY) continue;
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+        const float share = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next);
+        m = next;
+        l = l * keep + share * sum;
+        o *= keep;
+        for (int i = 0; i < here; i += 4 * AT_ONCE) {
+            f4 v[4];
+            float f[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (lane + 64 * j < p.dim) o[j] += share * part[i * stride + in_tile * p.dim + lane + 64 * j];
+            for (int u = 0; u < 4; ++u) {
+                const int from = i + u * AT_ONCE + which;
+                const float w = __shfl(share, from & 63);
+                f[u] = from < here ? w : 0.f;
+                v[u] = *reinterpret_cast<const f4 *>(mine + (base + (from < here ? from : 0)) * stride);
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o += f[u] * v[u];
+        }
     }
-    const float inv = l > 0.f ? 1.f / l : 0.f;
-    elem *out = static_cast<elem *>(p.out) + t * p.out_token + head * p.out_head;
+    for (int s = 32; s; s >>= 1) l += __shfl_xor(l, s);
+    for (int s = 32; s >= FOURS; s >>= 1)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-        if (lane + 64 * j < p.dim) out[lane + 64 * j] = (elem)(o[j] * inv);
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
+    if (which != 0 || d >= p.dim) return;
+    typedef elem four_t __attribute__((ext_vector_type(4)));
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    four_t r4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+    *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + t * p.out_token + head * p.out_head + d) = r4;
 }
 
 gba_status validate(const gba_attention &d)
@@ -520,15 +608,15 @@ gba_status validate(const gba_attention &d)
     return GBA_OK;
 }
 
-// How a call runs: rows of a tile, tiles, runs of keys and their room.
+// How a call runs: the kernel, tiles of rows, runs of keys and their room.
 struct Shape {
     bool whole;
-    int dp, rt, row_tiles, target, slots;
+    int dp, rt, rg, row_tiles, target, slots;
     size_t header, bytes;  // of the workspace
 };
 
-constexpr int RUNS = 1024;          // workgroups to aim at
-constexpr int SPLIT_REQUESTS = 1024;  // above that each request is one run
+constexpr int RUNS = 1024, RUNS_SHARED = 512;  // workgroups to aim at
+constexpr int SPLIT_REQUESTS = 1024;           // above that each request is one run
 
 Shape shape_of(const gba_attention &d)
 {
@@ -538,54 +626,56 @@ Shape shape_of(const gba_attention &d)
     s.whole = c.block_size % 16 == 0 && c.k_token >= 0 && c.v_token >= 0 && c.k_token < (1 << 25) && c.v_token < (1 << 25);
     s.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
     const int64_t rows = d.max_new * (d.q_heads / c.heads);
-    // as many rows as the registers hold: those that are not copied straight
-    // to LDS pass through them
-    const int most = s.dp == 64 ? 4 : s.dp == 128 ? (s.whole ? 4 : 2) : (s.whole ? 2 : 1);
-    s.rt = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
-    if (s.rt > most) s.rt = most;
-    s.row_tiles = (int)div_up(rows, 16 * s.rt);
+    // 16 or 32 rows a wave; more rows on more waves that share the tiles
+    s.rt = rows <= 16 || (s.dp == 256 && !s.whole) ? 1 : 2;
+    s.rg = rows <= 32 || s.dp == 256 || !s.whole ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
+    s.row_tiles = (int)div_up(rows, 16 * s.rt * s.rg);
     s.target = 0;
     s.slots = (int)d.requests;
     s.header = s.bytes = 0;
     if (d.requests <= SPLIT_REQUESTS && d.width * c.block_size > SHORTEST) {
-        s.target = (int)div_up(RUNS, c.heads * (int64_t)s.row_tiles);
+        s.target = (int)div_up(s.rg > 2 ? RUNS_SHARED : RUNS, c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
         s.header = (size_t)div_up(d.requests * 8, 256) * 256;
-        s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt) * (c.dim + 2) * sizeof(float);
+        s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt * s.rg) * (c.dim + 2) * sizeof(float);
     }
     return s;
 }
 
-template <class T, int DP, int RT, bool WHOLE>
+template <class T, int DP, int RT, int RG, bool WHOLE>
 gba_status run_attention(const AttentionArgs &a, hipStream_t s)
 {
     const int64_t groups = div_up((int64_t)a.slots * a.heads, 8) * 8 * a.row_tiles;
-    constexpr int threads = 64 * waves_of(DP);
-    if (groups > (int64_t)UINT_MAX / threads) return GBA_EUNSUPPORTED;
-    const gba_status st = launch(attention_kernel<T, DP, RT, WHOLE>, dim3((unsigned)groups), dim3(threads), s, a);
+    constexpr int threads = threads_of<DP, RG>();
+    if (groups > (int64_t)UINT_MAX / threads || div_up((int64_t)a.tokens * a.q_heads, 4) > (int64_t)UINT_MAX / 256) return GBA_EUNSUPPORTED;
+    const gba_status st = launch(attention_kernel<T, DP, RT, RG, WHOLE>, dim3((unsigned)groups), dim3(threads), s, a);
     if (st != GBA_OK || a.target == 0) return st;
-    return launch(join_kernel<T>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, 16 * RT);
+    return launch(join_kernel<T, DP>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, 16 * RT * RG);
 }
 
-template <class T, bool WHOLE>
+template <class T, int DP>
 gba_status run_attention(const AttentionArgs &a, const Shape &sh, hipStream_t s)
 {
-    if (sh.dp == 64)
-        return sh.rt == 1 ? run_attention<T, 64, 1, WHOLE>(a, s) : sh.rt == 2 ? run_attention<T, 64, 2, WHOLE>(a, s) : run_attention<T, 64, 4, WHOLE>(a, s);
-    if (sh.dp == 128) {
-        if constexpr (WHOLE)
-            if (sh.rt == 4) return run_attention<T, 128, 4, true>(a, s);
-        return sh.rt == 1 ? run_attention<T, 128, 1, WHOLE>(a, s) : run_attention<T, 128, 2, WHOLE>(a, s);
+    if constexpr (DP == 256) {
+        if (!sh.whole) return run_attention<T, 256, 1, 1, false>(a, s);
+        return sh.rt == 1 ? run_attention<T, 256, 1, 1, true>(a, s) : run_attention<T, 256, 2, 1, true>(a, s);
+    } else {
+        if (!sh.whole) return sh.rt == 1 ? run_attention<T, DP, 1, 1, false>(a, s) : run_attention<T, DP, 2, 1, false>(a, s);
+        if (sh.rt == 1) return run_attention<T, DP, 1, 1, true>(a, s);
+        switch (sh.rg) {
+        case 1: return run_attention<T, DP, 2, 1, true>(a, s);
+        case 2: return run_attention<T, DP, 2, 2, true>(a, s);
+        case 4: return run_attention<T, DP, 2, 4, true>(a, s);
+        default: return run_attention<T, DP, 2, 8, true>(a, s);
+        }
     }
-    if constexpr (WHOLE)
-        if (sh.rt == 2) return run_attention<T, 256, 2, true>(a, s);
-    return run_attention<T, 256, 1, WHOLE>(a, s);
 }
 
 template <class T>
 gba_status run_attention(const AttentionArgs &a, const Shape &sh, hipStream_t s)
 {
-    return sh.whole ? run_attention<T, true>(a, sh, s) : run_attention<T, false>(a, sh, s);
+    if (sh.dp == 64) return run_attention<T, 64>(a, sh, s);
+    return sh.dp == 128 ? run_attention<T, 128>(a, sh, s) : run_attention<T, 256>(a, sh, s);
 }
 
 bool nothing_to_do(const gba_attention &d)
