@@ -21,6 +21,7 @@
 // turn and meet once, at its end.  Runs are cut to one length for all
 // requests, from the sum of their lengths, which every wave reads for itself;
 // the runs of one request are joined by a second kernel.
+#include <stdlib.h>
 #include "gba_decode.hpp"
 #include "gba_kernel.hpp"
 
@@ -34,7 +35,8 @@ struct AttentionArgs {
     const uint64_t *mask;
     int64_t k_block, k_token, k_head, v_block, v_token, v_head, q_token, q_head, out_token, out_head;
     int requests, width, tokens, max_new, q_heads, heads, share, num_blocks, block_size, dim;
-    float scale2;      // scale * log2(e)
+    float scale2;      // |scale| * log2(e); its sign, or 0, goes to the queries
+    float sign;
     int row_tiles;     // of a request and head
     int slots;         // runs of keys there is room for: at least as many as there are
     int target;        // runs to aim at (0: one for each request)
@@ -174,25 +176,70 @@ __device__ __forceinline__ float across_max(float x)
     return fmaxf(x, __shfl_xor(x, 16));
 }
 
+// Which of 32 keys from new token `first` on (below 0: from the cached ones)
+// a row sees, if they exist: the bits of its mask, or with no mask those up to
+// its own token; all cached ones.
+__device__ __forceinline__ unsigned seen_of(bool masked, uint64_t mask, int index, int first)
+{
+    if (first <= -32) return 0xFFFFFFFFu;
+    if (!masked) {
+        const int n = index - first + 1;
+        return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1;
+    }
+    if (first < 0) return (unsigned)(mask << -first) | ((1u << -first) - 1);
+    return first < 64 ? (unsigned)(mask >> first) : 0u;
+}
+
+// Reads of 16 bytes in one block of assembly that waits for them: before a
+// load from LDS of its own the compiler waits for every copy to LDS that is
+// under way, the next tile's too.
+__device__ __forceinline__ void read_four(const unsigned (&at)[4], u4 (&v)[4])
+{
+    asm volatile(
+        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+        : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]));
+}
+
+// Four blocks of 16 of dim, transposed: rows 4 j .. 4 j + 3 of the lane's group
+// at `at` and 16 rows further on.
+template <int FURTHER>
+__device__ __forceinline__ void read_transposed(const unsigned (&at)[4], u4 (&v)[4])
+{
+    typedef unsigned u2 __attribute__((ext_vector_type(2)));
+    u2 r[8];
+    asm volatile(
+        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "s_waitcnt lgkmcnt(0)"
+        : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(FURTHER));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = u4{r[2 * i][0], r[2 * i][1], r[2 * i + 1][0], r[2 * i + 1][1]};
+}
+
 // A workgroup's waves: RG of them take 16 RT rows each of the same keys, and
-// KG such groups the tiles of a run in turn.  One group keeps STAGES tiles in
-// LDS.
+// KG such groups the tiles of a run in turn.  A group keeps two stages of SUB
+// tiles in LDS; its waves meet once a stage, and between that drift apart, so
+// that some are at the matrix unit while others read LDS or take exponentials.
 template <int DP, int RG>
 struct Shared {
     static constexpr int KG = RG == 8 ? 1 : RG == 4 || DP == 256 ? 2 : 4, WAVES = RG * KG;
-    static constexpr int STAGES = RG == 8 ? 4 : RG == 4 ? 3 : 2;
+    static constexpr int SUB = RG == 8 ? 4 : RG == 4 ? 2 : 1;
     static constexpr int CPR = DP / 8;                   // 16-byte chunks of a row
     static constexpr int KPI = 64 / CPR;                 // keys that one 64-lane copy covers
     static constexpr int COPIES = KEYS / KPI;            // of a tile of K or V
-    static constexpr int ROW = 2 * DP, TILE = KEYS * ROW, STAGE = 2 * TILE, GROUP = STAGES * STAGE;
+    static constexpr int ROW = 2 * DP, TILE = KEYS * ROW, PAIR = 2 * TILE, GROUP = 2 * SUB * PAIR;
 };
 
-// The join of the key groups needs 16 RT rows of fp32 for each wave.
+// The join of several key groups needs 16 RT rows of fp32 for each wave.
 template <int DP, int RT, int RG>
 constexpr int lds_bytes()
 {
     typedef Shared<DP, RG> S;
-    return S::KG * S::GROUP > S::WAVES * 16 * RT * 4 * DP ? S::KG * S::GROUP : S::WAVES * 16 * RT * 4 * DP;
+    return S::KG == 1 || S::KG * S::GROUP > S::WAVES * 16 * RT * 4 * DP ? S::KG * S::GROUP : S::WAVES * 16 * RT * 4 * DP;
 }
 template <int DP, int RG>
 constexpr int threads_of()
@@ -210,7 +257,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
     static_assert(WHOLE || RG == 1, "waves share only what goes straight to LDS");
-    constexpr int WAVES = S::WAVES, KG = S::KG, STAGES = WHOLE ? S::STAGES : 1;
+    constexpr int WAVES = S::WAVES, KG = S::KG, SUB = S::SUB, SLOTS = WHOLE ? 2 * SUB : 1;
     constexpr int CPR = S::CPR, KPI = S::KPI, COPIES = S::COPIES, ROW = S::ROW, TILE = S::TILE;
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = 16 * RT * RG;
     __shared__ __attribute__((aligned(16))) char smem[lds_bytes<DP, RT, RG>()];
@@ -240,25 +287,45 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     char *mine = smem + kg * S::GROUP;
     const int tiles = (run.to - run.from + KEYS - 1) / KEYS;
     const int count = tiles > kg ? (tiles - kg + KG - 1) / KG : 0;  // of this group
-    const int rounds = RG == 1 ? count : (tiles + KG - 1) / KG;     // of every group, where waves wait for each other
+    const int rounds = RG == 1 ? count : (tiles + KG * SUB - 1) / (KG * SUB);  // stages of every group, where waves meet
     const int32_t *entries = p.table + (int64_t)run.r * p.width;
     auto key0 = [&](int n) { return run.from + KEYS * (kg + KG * n); };
     const int in_copy = lane / CPR, place = lane % CPR;
     constexpr int PER_HALF = COPIES / 2;
     const char *k_head = reinterpret_cast<const char *>(static_cast<const elem *>(p.k) + head * p.k_head);
     const char *v_head = reinterpret_cast<const char *>(static_cast<const elem *>(p.v) + head * p.v_head);
-    int k_off[WHOLE ? PER_HALF : 1], v_off[WHOLE ? PER_HALF : 1];
+    // Byte offset of this lane's chunk of copy i of a half, or beyond the
+    // buffer; of K or of V.
+    auto chunk_of = [&](int i, bool v) {
+        const int key = KPI * i + in_copy, chunk = place ^ (v ? swap_v<DP>(key) : swap_k<DP>(key));
+        return 8 * chunk < p.dim ? (int)(key * (v ? p.v_token : p.k_token) * 2) + 16 * chunk : OOB_OFFSET;
+    };
+    // A tile's copies: those of K, then of V.  With waves that share tiles, half
+    // of them copy K and half V, MINE each: from copy MINE * (rg % (RG / 2)) on.
+    constexpr int MINE = 2 * COPIES / RG;
+    const bool copies_v = RG > 1 && rg >= RG / 2;
+    const int first_copy = RG > 1 ? MINE * (rg % (RG / 2 > 0 ? RG / 2 : 1)) : 0;
+    int k_off[WHOLE ? PER_HALF : 1], v_off[WHOLE && RG == 1 ? PER_HALF : 1];  // RG > 1: k_off is of what it copies
     if constexpr (WHOLE) {
 #pragma unroll
         for (int i = 0; i < PER_HALF; ++i) {
-            const int key = KPI * i + in_copy, kc = place ^ swap_k<DP>(key), vc = place ^ swap_v<DP>(key);
-            k_off[i] = 8 * kc < p.dim ? (int)(key * p.k_token * 2) + 16 * kc : OOB_OFFSET;
-            v_off[i] = 8 * vc < p.dim ? (int)(key * p.v_token * 2) + 16 * vc : OOB_OFFSET;
+            if (RG == 1) {
+                k_off[i] = chunk_of(i, false);
+                v_off[i] = chunk_of(i, true);
+            } else {
+                k_off[i] = chunk_of((first_copy + i) % PER_HALF, copies_v);
+            }
         }
     }
-    // WHOLE: the blocks of the next 32 tiles' halves, a lane each.  Else: the
-    // block and token of key lane % 32 of the next tile, and its registers.
-    int entry = -1, within = 0, entries_from = 0;
+    // WHOLE: a lane for each half of the next 32 tiles: where its first key is,
+    // the length of a buffer that ends with its last one (there are zeros
+    // beyond), and bits of the keys that exist: those up to the run's end, if
+    // their block does.  Else: the block and token of key lane % 32 of the next
+    // tile, and its registers.
+    int64_t k_from = 0, v_from = 0;
+    int k_bytes = 0, v_bytes = 0, entries_from = 0;
+    unsigned bits = 0;
+    int entry = -1, within = 0;
     u4 k_next[WHOLE ? 1 : COPIES], v_next[WHOLE ? 1 : COPIES];
     auto look_up = [&](int n) {
         const int pos = WHOLE ? key0(n + lane / 2) + 16 * (lane & 1) : key0(n) + (lane & 31);
@@ -269,43 +336,53 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             const int b = entries[page];
             entry = b >= 0 && b < p.num_blocks ? b : -1;
         }
-        entries_from = n;
+        if constexpr (WHOLE) {
+            const int left = run.to - pos, keys = entry < 0 ? 0 : left < 16 ? left : 16;
+            bits = (1u << keys) - 1;
+            k_from = keys ? 2 * (entry * p.k_block + within * p.k_token) : 0;
+            v_from = keys ? 2 * (entry * p.v_block + within * p.v_token) : 0;
+            k_bytes = keys ? (int)((keys - 1) * p.k_token + p.dim) * 2 : 0;
+            v_bytes = keys ? (int)((keys - 1) * p.v_token + p.dim) * 2 : 0;
+            entries_from = n;
+        }
     };
-    // How many keys of a half of tile n exist (WHOLE): those up to the run's
-    // end, if its block does.
-    auto keys_of = [&](int n, int h) {
-        const int b = __builtin_amdgcn_readlane(entry, 2 * (n - entries_from) + h), left = run.to - (key0(n) + 16 * h);
-        return b < 0 || left < 0 ? 0 : left < 16 ? left : 16;
+    auto buffer_of = [&](const char *head_of, int64_t from, int bytes, int at, bool real) {
+        const unsigned lo = __builtin_amdgcn_readlane((unsigned)from, at), hi = __builtin_amdgcn_readlane((unsigned)(from >> 32), at);
+        return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(head_of + (int64_t)((uint64_t)hi << 32 | lo)), (short)0,
+                                                 real ? __builtin_amdgcn_readlane(bytes, at) : 0, RSRC_WORD3);
     };
-    // Copies tile n, and says which of its keys exist.  A share of a group's
-    // copies for each of its waves; none are left out past the last tile, so
-    // that the number under way is always the same.
-    constexpr int MY_COPIES = 2 * COPIES / RG;
+    // Copies tile n, and says which of its keys exist.  None are left out past
+    // the last tile, so that the number under way is always the same.
     auto copy = [&](int n) -> unsigned {
         if constexpr (WHOLE) {
-            unsigned there = 0;
-            char *k_lds = mine + n % STAGES * S::STAGE, *v_lds = k_lds + TILE;
+            char *k_lds = mine + n % SLOTS * S::PAIR, *v_lds = k_lds + TILE;
             if (n - entries_from == 32) look_up(n);
+            const int at = 2 * (n - entries_from);
+            const bool real = n < count;
+            if constexpr (RG == 1) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int at = 2 * (n - entries_from) + h, keys = n < count ? keys_of(n, h) : 0;
-                there |= ((1u << keys) - 1) << (16 * h);
-                const int b = keys ? __builtin_amdgcn_readlane(entry, at) : 0, t = keys ? __builtin_amdgcn_readlane(within, at) : 0;
-                // beyond the last key the buffer has ended: zeros
-                const __amdgpu_buffer_rsrc_t kr =
-                    __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(k_head + 2 * (b * p.k_block + t * p.k_token)), (short)0,
-                                                      keys ? (int)((keys - 1) * p.k_token + p.dim) * 2 : 0, RSRC_WORD3);
-                const __amdgpu_buffer_rsrc_t vr =
-                    __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(v_head + 2 * (b * p.v_block + t * p.v_token)), (short)0,
-                                                      keys ? (int)((keys - 1) * p.v_token + p.dim) * 2 : 0, RSRC_WORD3);
+                for (int h = 0; h < 2; ++h) {
+                    const __amdgpu_buffer_rsrc_t kr = buffer_of(k_head, k_from, k_bytes, at + h, real);
 #pragma unroll
-                for (int i = 0; i < PER_HALF; ++i) {
-                    const int j = PER_HALF * h + i;
-                    if (RG == 1 || (2 * j) % RG == rg) buffer_load16_lds(kr, k_lds + 1024 * j, k_off[i], 0);
-                    if (RG == 1 || (2 * j + 1) % RG == rg) buffer_load16_lds(vr, v_lds + 1024 * j, v_off[i], 0);
+                    for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(kr, k_lds + 1024 * (PER_HALF * h + i), k_off[i], 0);
+                    const __amdgpu_buffer_rsrc_t vr = buffer_of(v_head, v_from, v_bytes, at + h, real);
+#pragma unroll
+                    for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(vr, v_lds + 1024 * (PER_HALF * h + i), v_off[i], 0);
+                }
+            } else {
+                char *to = (copies_v ? v_lds : k_lds) + 1024 * first_copy;
+                const char *head_of = copies_v ? v_head : k_head;
+                const int64_t from = copies_v ? v_from : k_from;
+                const int bytes = copies_v ? v_bytes : k_bytes;
+                constexpr int HALVES = MINE > PER_HALF ? 2 : 1, EACH = MINE / HALVES;
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) {
+                    const __amdgpu_buffer_rsrc_t rs = buffer_of(head_of, from, bytes, at + h + first_copy / PER_HALF, real);
+#pragma unroll
+                    for (int i = 0; i < EACH; ++i) buffer_load16_lds(rs, to + 1024 * (EACH * h + i), k_off[i], 0);
                 }
             }
-            return there;
+            return real ? __builtin_amdgcn_readlane(bits, at) | __builtin_amdgcn_readlane(bits, at + 1) << 16 : 0;
         } else {
             const unsigned there = (unsigned)__ballot(entry >= 0);
             const int block = entry, token = within;
@@ -342,6 +419,9 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             const int d = 32 * s + 8 * g;
             const u4 none = {0, 0, 0, 0};
             query[i][s] = real && d < p.dim ? *reinterpret_cast<const vec8 *>(q + d) : __builtin_bit_cast(vec8, none);
+            if (p.sign != 1.f)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) query[i][s][e] = (elem)((float)query[i][s][e] * p.sign);
         }
         sees[i] = p.mask != nullptr ? p.mask[token] : 0;
     }
@@ -365,29 +445,25 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
 #pragma unroll
     for (int e = 0; e < 8; ++e) ones[e] = (elem)1.f;
 
-    unsigned ahead[WHOLE ? STAGES - 1 : 1];  // which keys of the tiles under way exist
-    if constexpr (WHOLE) {
-        wait_vm_lgkm0<0>();  // the rows and blocks: from here on only copies are under way
-        if (rounds > 0) {
+    unsigned ahead[SUB] = {};  // which keys of the tiles under way exist
+    if constexpr (WHOLE) wait_vm_lgkm0<0>();  // the rows and blocks: from here on only copies are under way
+    if (rounds > 0) {
 #pragma unroll
-            for (int n = 0; n < STAGES - 1; ++n) ahead[n] = copy(n);
-        }
-    } else if (rounds > 0) {
-        ahead[0] = copy(0);
+        for (int j = 0; j < SUB; ++j) ahead[j] = copy(j);
     }
-    for (int n = 0; n < rounds; ++n) {
-        const char *k_lds = mine + n % STAGES * S::STAGE, *v_lds = k_lds + TILE;
-        const unsigned there = ahead[0];
+    for (int round = 0; round < rounds; ++round) {
+        unsigned now[SUB];
 #pragma unroll
-        for (int i = 0; i + 2 < STAGES; ++i) ahead[i] = ahead[i + 1];
+        for (int j = 0; j < SUB; ++j) now[j] = ahead[j];
         if constexpr (WHOLE && RG == 1) {
             wait_vm_lgkm0<63>();  // the slot's last fragments have been read
-            ahead[STAGES - 2] = copy(n + STAGES - 1);
-            wait_vm_lgkm0<(STAGES - 1) * MY_COPIES>();
+            ahead[0] = copy(round + 1);
+            wait_vm_lgkm0<MINE>();
         } else if constexpr (WHOLE) {
-            wait_vm_lgkm0<(STAGES - 2) * MY_COPIES>();
-            __builtin_amdgcn_s_barrier();  // every wave's share is there, and the last slot has been read
-            ahead[STAGES - 2] = copy(n + STAGES - 1);
+            wait_vm_lgkm0<0>();
+            __builtin_amdgcn_s_barrier();  // every wave's share is there, and the other stage has been read
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) ahead[j] = copy((round + 1) * SUB + j);
         } else {
             lanes_meet();  // the last tile's fragments have been read
 #pragma unroll
@@ -395,23 +471,39 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
                 *reinterpret_cast<u4 *>(mine + 1024 * i + 16 * lane) = k_next[i];
                 *reinterpret_cast<u4 *>(mine + TILE + 1024 * i + 16 * lane) = v_next[i];
             }
-            if (n + 1 < count) ahead[0] = copy(n + 1);
+            if (round + 1 < count) ahead[0] = copy(round + 1);
         }
         lanes_meet();
+#pragma unroll 1
+        for (int sub = 0; sub < SUB; ++sub) {
+        // half of the waves begin with the second half of a stage
+        const int j = SUB > 1 ? (sub + (rg >= RG / 2 ? SUB / 2 : 0)) % SUB : 0, n = round * SUB + j;
+        unsigned there = now[0];
+#pragma unroll
+        for (int i = 1; i < SUB; ++i) there = j == i ? now[i] : there;
         if (there == 0) continue;
+        const char *k_lds = mine + n % SLOTS * S::PAIR, *v_lds = k_lds + TILE;
 
         // scores: keys 16 h + 4 g + e of the tile, row c of each block
         f4 score[RT][2];
+        const unsigned k_base = (unsigned)(uintptr_t)(lds_void *)k_lds;
+        // (step, half) pairs in fours: steps first
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < RT; ++i) score[i][h] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int s = 0; s < STEPS; ++s) {
-                const vec8 k = *reinterpret_cast<const vec8 *>(k_lds + 16 * h * ROW + k_at[s]);
+        for (int q = 0; q < 2 * STEPS; q += 4) {
+            unsigned at[4];
+            u4 k[4];
 #pragma unroll
-                for (int i = 0; i < RT; ++i) score[i][h] = T::mfma(k, query[i][s], score[i][h]);
-            }
+            for (int e = 0; e < 4; ++e) at[e] = k_base + k_at[(q + e) % STEPS] + (q + e) / STEPS * 16 * ROW;
+            read_four(at, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+                    score[i][(q + e) / STEPS] = T::mfma(__builtin_bit_cast(vec8, k[e]), query[i][(q + e) % STEPS], score[i][(q + e) / STEPS]);
         }
         const int first_draft = key0(n) - rq.kept;  // of the new tokens, or below 0
         const bool all = there == 0xFFFFFFFFu && first_draft + KEYS <= 0;
@@ -420,19 +512,16 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         for (int i = 0; i < RT; ++i) {
             float t[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] = score[i][e >> 2][e & 3] * p.scale2;
+            for (int e = 0; e < 8; ++e) t[e] = score[i][e >> 2][e & 3];
             if (!all) {
+                const unsigned seen = (there & seen_of(masked, sees[i], index[i], first_draft)) >> (4 * g);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int key = 16 * (e >> 2) + 4 * g + (e & 3), draft = first_draft + key;
-                    const bool in_tree = masked ? (draft < 64) & (int)((sees[i] >> (draft & 63)) & 1) : draft <= index[i];
-                    const bool seen = ((there >> key) & 1) & ((draft < 0) | in_tree);
-                    t[e] = seen ? t[e] : -INFINITY;
-                }
+                for (int e = 0; e < 8; ++e) t[e] = (seen >> (16 * (e >> 2) + (e & 3))) & 1 ? t[e] : -INFINITY;
             }
             float most = t[0];
 #pragma unroll
             for (int e = 1; e < 8; ++e) most = fmaxf(most, t[e]);
+            most *= p.scale2;
             if (__ballot(most > top[i] + SLACK)) {
                 const float now = fmaxf(across_max(most), top[i]);
                 const float next = now == -INFINITY ? 0.f : now;
@@ -444,18 +533,56 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
                 for (int b = 0; b < BLOCKS; ++b) out[i][b] *= keep;
             }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) weight[i][e] = (elem)__builtin_amdgcn_exp2f(t[e] - base2[i]);
+            for (int e = 0; e < 8; ++e) weight[i][e] = (elem)__builtin_amdgcn_exp2f(__builtin_fmaf(t[e], p.scale2, -base2[i]));
             weights[i] = T::mfma(ones, weight[i], weights[i]);
         }
 #pragma unroll
-        for (int b = 0; b < BLOCKS; ++b) {
-            const char *at = v_lds + v_at + ((32 * b) ^ v_swap);
-            const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)at);
-            const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4v *)(at + 16 * ROW));
-            const vec8 v = __builtin_bit_cast(vec8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
+        for (int b = 0; b < BLOCKS; b += 4) {
+            unsigned at[4];
+            u4 v[4];
+            const unsigned from = (unsigned)(uintptr_t)(lds_void *)(v_lds + v_at);
 #pragma unroll
-            for (int i = 0; i < RT; ++i) out[i][b] = T::mfma(v, weight[i], out[i][b]);
+            for (int j = 0; j < 4; ++j) at[j] = from + ((32 * (b + j)) ^ v_swap);
+            read_transposed<16 * ROW>(at, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < RT; ++i) out[i][b + j] = T::mfma(__builtin_bit_cast(vec8, v[j]), weight[i], out[i][b + j]);
         }
+        }
+    }
+
+    const bool whole_request = run.n == 1;
+    typedef elem four_t __attribute__((ext_vector_type(4)));
+    float *part = whole_request ? nullptr : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * ROWS * (int64_t)(p.dim + 2);
+    if constexpr (KG == 1) {  // one key group: the sums are these
+        wait_vm_lgkm0<0>();
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            const int row = wave_row0 + 16 * i + c;
+            if (row >= rows) continue;
+            const float l = weights[i][0], inv = l > 0.f ? 1.f / l : 0.f;
+            elem *to = static_cast<elem *>(p.out) + (int64_t)(rq.first + index[i]) * p.out_token +
+                       (int64_t)(head * p.share + row - index[i] * p.share) * p.out_head + 4 * g;
+            float *to_part = part + (row - row0) * p.dim + 4 * g;
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) {
+                if (16 * b + 4 * g >= p.dim) continue;
+                if (whole_request) {
+                    four_t r4;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) r4[e] = (elem)(out[i][b][e] * inv);
+                    *reinterpret_cast<four_t *>(to + 16 * b) = r4;
+                } else {
+                    *reinterpret_cast<f4 *>(to_part + 16 * b) = out[i][b];
+                }
+            }
+            if (!whole_request && g == 0) {
+                part[ROWS * p.dim + row - row0] = top[i];
+                part[ROWS * (p.dim + 1) + row - row0] = l;
+            }
+        }
+        return;
     }
 
     // ---- the key groups' sums, joined through LDS: row c, chunks of four of
@@ -476,8 +603,6 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             *reinterpret_cast<f4 *>(sums_of_wave + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = out[i][b];
     }
     __syncthreads();
-    const bool whole_request = run.n == 1;
-    float *part = whole_request ? nullptr : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * ROWS * (int64_t)(p.dim + 2);
     constexpr int FOURS = DP / 4;
     for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * WAVES) {
         const int row = j / FOURS, four = j % FOURS, d = 4 * four, w0 = row / (16 * RT), r = row % (16 * RT);
@@ -495,7 +620,6 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             o += share * *reinterpret_cast<const f4 *>(smem + (RG == 1 ? from * S::GROUP : from * (16 * RT * 4 * DP)) + r * (4 * DP) + 16 * (four ^ (r & 15)));
         }
         if (whole_request) {
-            typedef elem four_t __attribute__((ext_vector_type(4)));
             const float inv = l > 0.f ? 1.f / l : 0.f;
             const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
             four_t r4;
@@ -634,6 +758,7 @@ Shape shape_of(const gba_attention &d)
     s.slots = (int)d.requests;
     s.header = s.bytes = 0;
     if (d.requests <= SPLIT_REQUESTS && d.width * c.block_size > SHORTEST) {
+        const int RUNS = getenv("RUNS") ? atoi(getenv("RUNS")) : 1024, RUNS_SHARED = RUNS;
         s.target = (int)div_up(s.rg > 2 ? RUNS_SHARED : RUNS, c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
         s.header = (size_t)div_up(d.requests * 8, 256) * 256;
@@ -737,7 +862,9 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     a.num_blocks = (int)c.num_blocks;
     a.block_size = (int)c.block_size;
     a.dim = (int)c.dim;
-    a.scale2 = d.scale * 1.44269504088896340736f;
+    const float scale2 = d.scale * 1.44269504088896340736f;
+    a.sign = scale2 > 0.f ? 1.f : scale2 < 0.f ? -1.f : 0.f;
+    a.scale2 = scale2 > 0.f ? scale2 : scale2 < 0.f ? -scale2 : 1.f;
     a.row_tiles = sh.row_tiles;
     a.slots = sh.slots;
     a.target = sh.target;
