@@ -190,40 +190,46 @@ __device__ __forceinline__ unsigned seen_of(bool masked, uint64_t mask, int inde
     return first < 64 ? (unsigned)(mask >> first) : 0u;
 }
 
-// Reads of 16 bytes in one block of assembly that waits for them: before a
-// load from LDS of its own the compiler waits for every copy to LDS that is
-// under way, the next tile's too.
-__device__ __forceinline__ void read_four(const unsigned (&at)[4], u4 (&v)[4])
+// Reads of 16 bytes, OFF bytes past each address, in one block of assembly that
+// waits for them: before a load from LDS of its own the compiler waits for
+// every copy to LDS that is under way, the next tile's too.
+template <int O0, int O1, int O2, int O3>
+__device__ __forceinline__ void read_four(unsigned a0, unsigned a1, unsigned a2, unsigned a3, u4 (&v)[4])
 {
     asm volatile(
-        "ds_read_b128 %0, %4\n\tds_read_b128 %1, %5\n\tds_read_b128 %2, %6\n\tds_read_b128 %3, %7\n\ts_waitcnt lgkmcnt(0)"
+        "ds_read_b128 %0, %4 offset:%8\n\tds_read_b128 %1, %5 offset:%9\n\t"
+        "ds_read_b128 %2, %6 offset:%10\n\tds_read_b128 %3, %7 offset:%11\n\ts_waitcnt lgkmcnt(0)"
         : "=&v"(v[0]), "=&v"(v[1]), "=&v"(v[2]), "=&v"(v[3])
-        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]));
+        : "v"(a0), "v"(a1), "v"(a2), "v"(a3), "n"(O0), "n"(O1), "n"(O2), "n"(O3));
 }
 
-// Four blocks of 16 of dim, transposed: rows 4 j .. 4 j + 3 of the lane's group
-// at `at` and 16 rows further on.
-template <int FURTHER>
-__device__ __forceinline__ void read_transposed(const unsigned (&at)[4], u4 (&v)[4])
+// Four blocks of 16 of dim, transposed: keys 4 j .. 4 j + 3 of the lane's group
+// OFF bytes past each address, and those FURTHER bytes on.
+template <int OFF, int FURTHER>
+__device__ __forceinline__ void read_transposed(const unsigned *at, u4 (&v)[4])
 {
     typedef unsigned u2 __attribute__((ext_vector_type(2)));
     u2 r[8];
     asm volatile(
-        "ds_read_b64_tr_b16 %0, %8\n\tds_read_b64_tr_b16 %1, %8 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %2, %9\n\tds_read_b64_tr_b16 %3, %9 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %4, %10\n\tds_read_b64_tr_b16 %5, %10 offset:%12\n\t"
-        "ds_read_b64_tr_b16 %6, %11\n\tds_read_b64_tr_b16 %7, %11 offset:%12\n\t"
+        "ds_read_b64_tr_b16 %0, %8 offset:%12\n\tds_read_b64_tr_b16 %1, %8 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %2, %9 offset:%12\n\tds_read_b64_tr_b16 %3, %9 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %4, %10 offset:%12\n\tds_read_b64_tr_b16 %5, %10 offset:%13\n\t"
+        "ds_read_b64_tr_b16 %6, %11 offset:%12\n\tds_read_b64_tr_b16 %7, %11 offset:%13\n\t"
         "s_waitcnt lgkmcnt(0)"
         : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
-        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(FURTHER));
+        : "v"(at[0]), "v"(at[1]), "v"(at[2]), "v"(at[3]), "n"(OFF), "n"(OFF + FURTHER));
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = u4{r[2 * i][0], r[2 * i][1], r[2 * i + 1][0], r[2 * i + 1][1]};
 }
 
+template <int N>
+struct Const {
+    static constexpr int value = N;
+};
+
 // A workgroup's waves: RG of them take 16 RT rows each of the same keys, and
 // KG such groups the tiles of a run in turn.  A group keeps two stages of SUB
-// tiles in LDS; its waves meet once a stage, and between that drift apart, so
-// that some are at the matrix unit while others read LDS or take exponentials.
+// tiles in LDS; its waves meet once a stage.
 template <int DP, int RG>
 struct Shared {
     static constexpr int KG = RG == 8 ? 1 : RG == 4 || DP == 256 ? 2 : 4, WAVES = RG * KG;
@@ -287,7 +293,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     char *mine = smem + kg * S::GROUP;
     const int tiles = (run.to - run.from + KEYS - 1) / KEYS;
     const int count = tiles > kg ? (tiles - kg + KG - 1) / KG : 0;  // of this group
-    const int rounds = RG == 1 ? count : (tiles + KG * SUB - 1) / (KG * SUB);  // stages of every group, where waves meet
+    const int rounds = (tiles + KG * SUB - 1) / (KG * SUB);           // stages of every group, where waves meet
     const int32_t *entries = p.table + (int64_t)run.r * p.width;
     auto key0 = [&](int n) { return run.from + KEYS * (kg + KG * n); };
     const int in_copy = lane / CPR, place = lane % CPR;
@@ -351,53 +357,55 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(head_of + (int64_t)((uint64_t)hi << 32 | lo)), (short)0,
                                                  real ? __builtin_amdgcn_readlane(bytes, at) : 0, RSRC_WORD3);
     };
-    // Copies tile n, and says which of its keys exist.  None are left out past
-    // the last tile, so that the number under way is always the same.
-    auto copy = [&](int n) -> unsigned {
-        if constexpr (WHOLE) {
-            char *k_lds = mine + n % SLOTS * S::PAIR, *v_lds = k_lds + TILE;
-            if (n - entries_from == 32) look_up(n);
-            const int at = 2 * (n - entries_from);
-            const bool real = n < count;
-            if constexpr (RG == 1) {
+    // Copies K (part 0) or V (part 1) of tile n, or with waves that share tiles
+    // the wave's share of both.  None are left out past the last tile, so that
+    // the number under way is always the same.
+    auto copy = [&](int n, int part) {
+        char *k_lds = mine + n % SLOTS * S::PAIR, *v_lds = k_lds + TILE;
+        const int at = 2 * (n - entries_from);
+        const bool real = n < count;
+        if constexpr (RG == 1) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const __amdgpu_buffer_rsrc_t kr = buffer_of(k_head, k_from, k_bytes, at + h, real);
+            for (int h = 0; h < 2; ++h) {
+                const __amdgpu_buffer_rsrc_t rs = part ? buffer_of(v_head, v_from, v_bytes, at + h, real) : buffer_of(k_head, k_from, k_bytes, at + h, real);
 #pragma unroll
-                    for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(kr, k_lds + 1024 * (PER_HALF * h + i), k_off[i], 0);
-                    const __amdgpu_buffer_rsrc_t vr = buffer_of(v_head, v_from, v_bytes, at + h, real);
-#pragma unroll
-                    for (int i = 0; i < PER_HALF; ++i) buffer_load16_lds(vr, v_lds + 1024 * (PER_HALF * h + i), v_off[i], 0);
-                }
-            } else {
-                char *to = (copies_v ? v_lds : k_lds) + 1024 * first_copy;
-                const char *head_of = copies_v ? v_head : k_head;
-                const int64_t from = copies_v ? v_from : k_from;
-                const int bytes = copies_v ? v_bytes : k_bytes;
-                constexpr int HALVES = MINE > PER_HALF ? 2 : 1, EACH = MINE / HALVES;
-#pragma unroll
-                for (int h = 0; h < HALVES; ++h) {
-                    const __amdgpu_buffer_rsrc_t rs = buffer_of(head_of, from, bytes, at + h + first_copy / PER_HALF, real);
-#pragma unroll
-                    for (int i = 0; i < EACH; ++i) buffer_load16_lds(rs, to + 1024 * (EACH * h + i), k_off[i], 0);
-                }
+                for (int i = 0; i < PER_HALF; ++i)
+                    buffer_load16_lds(rs, (part ? v_lds : k_lds) + 1024 * (PER_HALF * h + i), part ? v_off[i] : k_off[i], 0);
             }
-            return real ? __builtin_amdgcn_readlane(bits, at) | __builtin_amdgcn_readlane(bits, at + 1) << 16 : 0;
         } else {
-            const unsigned there = (unsigned)__ballot(entry >= 0);
-            const int block = entry, token = within;
-            if (n + 1 < count) look_up(n + 1);
+            char *to = (copies_v ? v_lds : k_lds) + 1024 * first_copy;
+            const char *head_of = copies_v ? v_head : k_head;
+            const int64_t from = copies_v ? v_from : k_from;
+            const int bytes = copies_v ? v_bytes : k_bytes;
+            constexpr int HALVES = MINE > PER_HALF ? 2 : 1, EACH = MINE / HALVES;
 #pragma unroll
-            for (int i = 0; i < COPIES; ++i) {
-                const int key = KPI * i + in_copy, kc = place ^ swap_k<DP>(key), vc = place ^ swap_v<DP>(key);
-                const int64_t b = __shfl(block, key), t = __shfl(token, key);
-                const u4 none = {0, 0, 0, 0};
-                k_next[i] = v_next[i] = none;
-                if (b >= 0 && 8 * kc < p.dim) k_next[i] = *reinterpret_cast<const u4 *>(k_head + 2 * (b * p.k_block + t * p.k_token) + 16 * kc);
-                if (b >= 0 && 8 * vc < p.dim) v_next[i] = *reinterpret_cast<const u4 *>(v_head + 2 * (b * p.v_block + t * p.v_token) + 16 * vc);
+            for (int h = 0; h < HALVES; ++h) {
+                const __amdgpu_buffer_rsrc_t rs = buffer_of(head_of, from, bytes, at + h + first_copy / PER_HALF, real);
+#pragma unroll
+                for (int i = 0; i < EACH; ++i) buffer_load16_lds(rs, to + 1024 * (EACH * h + i), k_off[i], 0);
             }
-            return there;
         }
+    };
+    // Which keys of tile n exist (WHOLE).
+    auto keys_of = [&](int n) -> unsigned {
+        const int at = 2 * (n - entries_from);
+        return n < count ? __builtin_amdgcn_readlane(bits, at) | __builtin_amdgcn_readlane(bits, at + 1) << 16 : 0u;
+    };
+    // Else: tile n's keys and values into registers, and which of them exist.
+    auto fetch = [&](int n) -> unsigned {
+        const unsigned there = (unsigned)__ballot(entry >= 0);
+        const int block = entry, token = within;
+        if (n + 1 < count) look_up(n + 1);
+#pragma unroll
+        for (int i = 0; i < COPIES; ++i) {
+            const int key = KPI * i + in_copy, kc = place ^ swap_k<DP>(key), vc = place ^ swap_v<DP>(key);
+            const int64_t b = __shfl(block, key), t = __shfl(token, key);
+            const u4 none = {0, 0, 0, 0};
+            k_next[i] = v_next[i] = none;
+            if (b >= 0 && 8 * kc < p.dim) k_next[i] = *reinterpret_cast<const u4 *>(k_head + 2 * (b * p.k_block + t * p.k_token) + 16 * kc);
+            if (b >= 0 && 8 * vc < p.dim) v_next[i] = *reinterpret_cast<const u4 *>(v_head + 2 * (b * p.v_block + t * p.v_token) + 16 * vc);
+        }
+        return there;
     };
     if (rounds > 0) look_up(0);
 
@@ -428,127 +436,192 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     const bool masked = p.mask != nullptr;
 
     f4 out[RT][BLOCKS] = {}, weights[RT] = {};
-    float top[RT], base2[RT];  // running maximum; what is subtracted (0 while there is none)
+    // running maximum; what a score may be before it moves; what is subtracted
+    // (0 while there is no maximum)
+    float top[RT], limit[RT], base2[RT];
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
-        top[i] = -INFINITY;
+        top[i] = limit[i] = -INFINITY;
         base2[i] = 0.f;
     }
 
     // ---- LDS addresses of the fragments
-    int k_at[STEPS];
+    const unsigned lds0 = (unsigned)(uintptr_t)(lds_void *)mine;
+    unsigned k_at[STEPS], v_at[BLOCKS];
 #pragma unroll
-    for (int s = 0; s < STEPS; ++s) k_at[s] = c * ROW + 16 * ((4 * s + g) ^ swap_k<DP>(c));
+    for (int s = 0; s < STEPS; ++s) k_at[s] = lds0 + c * ROW + 16 * ((4 * s + g) ^ swap_k<DP>(c));
     const int v_key = 4 * g + (c >> 2), v_swap = 16 * swap_v<DP>(v_key);
-    const int v_at = v_key * ROW + 16 * ((c & 3) >> 1) + 8 * (c & 1);
-    vec8 ones;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) ones[e] = (elem)1.f;
+    for (int b = 0; b < BLOCKS; ++b) v_at[b] = lds0 + TILE + v_key * ROW + 16 * ((c & 3) >> 1) + 8 * (c & 1) + ((32 * b) ^ v_swap);
+    u4 ones_bits = __builtin_bit_cast(u4, vec8{(elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f, (elem)1.f});
+    asm("" : "+v"(ones_bits));  // four registers of them, or they are made anew each time
+    const vec8 ones = __builtin_bit_cast(vec8, ones_bits);
 
-    unsigned ahead[SUB] = {};  // which keys of the tiles under way exist
-    if constexpr (WHOLE) wait_vm_lgkm0<0>();  // the rows and blocks: from here on only copies are under way
-    if (rounds > 0) {
+    f4 score[RT][2];
+    vec8 weight[RT];
+    // Scores of the tile OFF bytes past the addresses plus `slot`: keys 16 h +
+    // 4 g + e, row c of each block.
+    auto multiply_k = [&](auto off, unsigned slot) {
+        constexpr int OFF = decltype(off)::value;
 #pragma unroll
-        for (int j = 0; j < SUB; ++j) ahead[j] = copy(j);
-    }
-    for (int round = 0; round < rounds; ++round) {
-        unsigned now[SUB];
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int j = 0; j < SUB; ++j) now[j] = ahead[j];
-        if constexpr (WHOLE && RG == 1) {
-            wait_vm_lgkm0<63>();  // the slot's last fragments have been read
-            ahead[0] = copy(round + 1);
-            wait_vm_lgkm0<MINE>();
-        } else if constexpr (WHOLE) {
+            for (int i = 0; i < RT; ++i) score[i][h] = f4{0.f, 0.f, 0.f, 0.f};
+        auto four = [&](auto first) {
+            constexpr int Q = decltype(first)::value, HALF = 16 * ROW;
+            constexpr int S0 = Q % STEPS, S1 = (Q + 1) % STEPS, S2 = (Q + 2) % STEPS, S3 = (Q + 3) % STEPS;
+            u4 k[4];
+            read_four<OFF + Q / STEPS * HALF, OFF + (Q + 1) / STEPS * HALF, OFF + (Q + 2) / STEPS * HALF, OFF + (Q + 3) / STEPS * HALF>(
+                k_at[S0] + slot, k_at[S1] + slot, k_at[S2] + slot, k_at[S3] + slot, k);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+                    score[i][(Q + e) / STEPS] = T::mfma(__builtin_bit_cast(vec8, k[e]), query[i][(Q + e) % STEPS], score[i][(Q + e) / STEPS]);
+        };
+        four(Const<0>{});
+        if constexpr (2 * STEPS > 4) four(Const<4>{});
+        if constexpr (2 * STEPS > 8) {
+            four(Const<8>{});
+            four(Const<12>{});
+        }
+    };
+    // The weights of tile n, of which the keys in `there` exist.
+    auto soften = [&](int n, unsigned there) {
+        const int first_draft = key0(n) - rq.kept;  // of the new tokens, or below 0
+        if (there != 0xFFFFFFFFu || first_draft + KEYS > 0) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const unsigned seen = (there & seen_of(masked, sees[i], index[i], first_draft)) >> (4 * g);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) score[i][e >> 2][e & 3] = (seen >> (16 * (e >> 2) + (e & 3))) & 1 ? score[i][e >> 2][e & 3] : -INFINITY;
+            }
+        }
+        float most[RT];
+        bool past = false;
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            most[i] = score[i][0][0];
+#pragma unroll
+            for (int e = 1; e < 8; ++e) most[i] = fmaxf(most[i], score[i][e >> 2][e & 3]);
+            most[i] *= p.scale2;
+            past |= most[i] > limit[i];
+        }
+        if (__ballot(past)) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const float now = fmaxf(across_max(most[i]), top[i]);
+                const float next = now == -INFINITY ? 0.f : now;
+                const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
+                top[i] = now;
+                limit[i] = now + SLACK;
+                base2[i] = next;
+                weights[i] *= keep;
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) out[i][b] *= keep;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                weight[i][e] = (elem)__builtin_amdgcn_exp2f(__builtin_fmaf(score[i][e >> 2][e & 3], p.scale2, -base2[i]));
+            weights[i] = T::mfma(ones, weight[i], weights[i]);
+        }
+    };
+    auto multiply_v = [&](auto off, unsigned slot) {
+#pragma unroll
+        for (int b = 0; b < BLOCKS; b += 4) {
+            u4 v[4];
+            const unsigned at[4] = {v_at[b] + slot, v_at[b + 1] + slot, v_at[b + 2] + slot, v_at[b + 3] + slot};
+            read_transposed<decltype(off)::value, 16 * ROW>(at, v);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int i = 0; i < RT; ++i) out[i][b + j] = T::mfma(__builtin_bit_cast(vec8, v[j]), weight[i], out[i][b + j]);
+        }
+    };
+
+    if constexpr (WHOLE && RG == 1) {
+        // K and V are two tiles ahead each: K's slot is free as soon as the
+        // scores are there, V's when the tile is done.
+        wait_vm_lgkm0<0>();  // the rows and blocks: from here on only copies are under way
+        unsigned now = 0, next = 0;
+        if (count > 0) {
+            now = keys_of(0);
+            next = keys_of(1);
+            copy(0, 0);
+            copy(0, 1);
+            copy(1, 0);
+            copy(1, 1);
+        }
+        for (int n = 0; n < count; ++n) {
+            const unsigned slot = (n & 1) * S::PAIR;
+            wait_vm_lgkm0<3 * COPIES>();
+            lanes_meet();
+            multiply_k(Const<0>{}, slot);
+            if (n + 2 - entries_from == 32) look_up(n + 2);
+            const unsigned after = keys_of(n + 2);
+            copy(n + 2, 0);
+            soften(n, now);
+            wait_vm_lgkm0<3 * COPIES>();
+            lanes_meet();
+            multiply_v(Const<0>{}, slot);
+            copy(n + 2, 1);
+            now = next;
+            next = after;
+        }
+    } else if constexpr (WHOLE) {
+        wait_vm_lgkm0<0>();
+        unsigned ahead[SUB];
+        auto stage = [&](int first) {
+            if (first - entries_from == 32) look_up(first);
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) {
+                ahead[j] = keys_of(first + j);
+                copy(first + j, 0);
+            }
+        };
+        if (rounds > 0) stage(0);
+        for (int round = 0; round < rounds; ++round) {
+            unsigned now[SUB];
+#pragma unroll
+            for (int j = 0; j < SUB; ++j) now[j] = ahead[j];
             wait_vm_lgkm0<0>();
             __builtin_amdgcn_s_barrier();  // every wave's share is there, and the other stage has been read
-#pragma unroll
-            for (int j = 0; j < SUB; ++j) ahead[j] = copy((round + 1) * SUB + j);
-        } else {
+            stage((round + 1) * SUB);
+            lanes_meet();
+            const unsigned slot = (round & 1) * (SUB * S::PAIR);
+            auto tile = [&](auto j) {
+                constexpr int J = decltype(j)::value;
+                if (now[J] != 0) {
+                    multiply_k(Const<J * S::PAIR>{}, slot);
+                    soften(round * SUB + J, now[J]);
+                    multiply_v(Const<J * S::PAIR>{}, slot);
+                }
+            };
+            tile(Const<0>{});
+            if constexpr (SUB > 1) tile(Const<1>{});
+            if constexpr (SUB > 2) {
+                tile(Const<2>{});
+                tile(Const<3>{});
+            }
+        }
+    } else {
+        unsigned next = count > 0 ? fetch(0) : 0;
+        for (int n = 0; n < count; ++n) {
+            const unsigned now = next;
             lanes_meet();  // the last tile's fragments have been read
 #pragma unroll
             for (int i = 0; i < COPIES; ++i) {
                 *reinterpret_cast<u4 *>(mine + 1024 * i + 16 * lane) = k_next[i];
                 *reinterpret_cast<u4 *>(mine + TILE + 1024 * i + 16 * lane) = v_next[i];
             }
-            if (round + 1 < count) ahead[0] = copy(round + 1);
-        }
-        lanes_meet();
-#pragma unroll 1
-        for (int sub = 0; sub < SUB; ++sub) {
-        // half of the waves begin with the second half of a stage
-        const int j = SUB > 1 ? (sub + (rg >= RG / 2 ? SUB / 2 : 0)) % SUB : 0, n = round * SUB + j;
-        unsigned there = now[0];
-#pragma unroll
-        for (int i = 1; i < SUB; ++i) there = j == i ? now[i] : there;
-        if (there == 0) continue;
-        const char *k_lds = mine + n % SLOTS * S::PAIR, *v_lds = k_lds + TILE;
-
-        // scores: keys 16 h + 4 g + e of the tile, row c of each block
-        f4 score[RT][2];
-        const unsigned k_base = (unsigned)(uintptr_t)(lds_void *)k_lds;
-        // (step, half) pairs in fours: steps first
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int i = 0; i < RT; ++i) score[i][h] = f4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int q = 0; q < 2 * STEPS; q += 4) {
-            unsigned at[4];
-            u4 k[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) at[e] = k_base + k_at[(q + e) % STEPS] + (q + e) / STEPS * 16 * ROW;
-            read_four(at, k);
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-                    score[i][(q + e) / STEPS] = T::mfma(__builtin_bit_cast(vec8, k[e]), query[i][(q + e) % STEPS], score[i][(q + e) / STEPS]);
-        }
-        const int first_draft = key0(n) - rq.kept;  // of the new tokens, or below 0
-        const bool all = there == 0xFFFFFFFFu && first_draft + KEYS <= 0;
-        vec8 weight[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            float t[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) t[e] = score[i][e >> 2][e & 3];
-            if (!all) {
-                const unsigned seen = (there & seen_of(masked, sees[i], index[i], first_draft)) >> (4 * g);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) t[e] = (seen >> (16 * (e >> 2) + (e & 3))) & 1 ? t[e] : -INFINITY;
-            }
-            float most = t[0];
-#pragma unroll
-            for (int e = 1; e < 8; ++e) most = fmaxf(most, t[e]);
-            most *= p.scale2;
-            if (__ballot(most > top[i] + SLACK)) {
-                const float now = fmaxf(across_max(most), top[i]);
-                const float next = now == -INFINITY ? 0.f : now;
-                const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
-                top[i] = now;
-                base2[i] = next;
-                weights[i] *= keep;
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) out[i][b] *= keep;
-            }
-#pragma unroll
-            for (int e = 0; e < 8; ++e) weight[i][e] = (elem)__builtin_amdgcn_exp2f(__builtin_fmaf(t[e], p.scale2, -base2[i]));
-            weights[i] = T::mfma(ones, weight[i], weights[i]);
-        }
-#pragma unroll
-        for (int b = 0; b < BLOCKS; b += 4) {
-            unsigned at[4];
-            u4 v[4];
-            const unsigned from = (unsigned)(uintptr_t)(lds_void *)(v_lds + v_at);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) at[j] = from + ((32 * (b + j)) ^ v_swap);
-            read_transposed<16 * ROW>(at, v);
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < RT; ++i) out[i][b + j] = T::mfma(__builtin_bit_cast(vec8, v[j]), weight[i], out[i][b + j]);
-        }
+            if (n + 1 < count) next = fetch(n + 1);
+            lanes_meet();
+            multiply_k(Const<0>{}, 0);
+            soften(n, now);
+            multiply_v(Const<0>{}, 0);
         }
     }
 
