@@ -21,7 +21,6 @@
 // turn and meet once, at its end.  Runs are cut to one length for all
 // requests, from the sum of their lengths, which every wave reads for itself;
 // the runs of one request are joined by a second kernel.
-#include <stdlib.h>
 #include "gba_decode.hpp"
 #include "gba_kernel.hpp"
 
@@ -812,7 +811,21 @@ struct Shape {
     size_t header, bytes;  // of the workspace
 };
 
-constexpr int RUNS = 1024, RUNS_SHARED = 512;  // workgroups to aim at
+// Runs to aim at.  A compute unit has room for one workgroup (two of dim 64),
+// and each request and head adds half a run on average, its last one.  Few
+// requests: one run a compute unit (one of 32000 keys: 34 us, 52 with four).
+// Many of different lengths: more and shorter ones, to even out (64 of up to
+// 8192: 92 us with 256, 82 with 512, 87 with 1024; 128 of up to 4000: 139, 128,
+// 123).  Tiles of more than 64 rows are bound by their products, not by HBM,
+// and a run costs them more: all of them at once (16 trees of 64: 55 us with
+// 192, 65 with 224, 80 with 512).
+int64_t runs_to_aim_at(const gba_attention &d, int rg, int row_tiles)
+{
+    const int64_t pairs = d.requests * d.cache.heads * row_tiles;
+    if (rg > 2) return pairs < 256 ? 256 - pairs / 2 : 128;
+    return pairs <= 128 ? 256 : pairs < 1024 ? 512 : 1024;
+}
+
 constexpr int SPLIT_REQUESTS = 1024;           // above that each request is one run
 
 Shape shape_of(const gba_attention &d)
@@ -831,8 +844,7 @@ Shape shape_of(const gba_attention &d)
     s.slots = (int)d.requests;
     s.header = s.bytes = 0;
     if (d.requests <= SPLIT_REQUESTS && d.width * c.block_size > SHORTEST) {
-        const int RUNS = getenv("RUNS") ? atoi(getenv("RUNS")) : 1024, RUNS_SHARED = RUNS;
-        s.target = (int)div_up(s.rg > 2 ? RUNS_SHARED : RUNS, c.heads * (int64_t)s.row_tiles);
+        s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
         s.header = (size_t)div_up(d.requests * 8, 256) * 256;
         s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt * s.rg) * (c.dim + 2) * sizeof(float);
