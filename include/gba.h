@@ -446,8 +446,10 @@ gba_status gba_q4_linear(const gba_q4_weight *w, int64_t M, const void *A, int64
  * table[requests * width], held[requests] (blocks a request holds: the first
  * held[r] entries of its row), free_blocks[num_blocks], free_count[1] (the
  * stack is free_blocks[0 .. free_count), its top last).  Entries of a row past
- * held are -1.
+ * held are -1.  scratch: GBA_TABLES_SCRATCH(requests) words, 16-byte aligned,
+ * for a step's own use.
  */
+#define GBA_TABLES_SCRATCH(requests) (4 * ((requests) + 1))
 typedef struct gba_block_tables {
     int64_t requests, width, num_blocks;
     int64_t block_size;
@@ -455,6 +457,7 @@ typedef struct gba_block_tables {
     int32_t *held;
     int32_t *free_blocks;
     int32_t *free_count;
+    int32_t *scratch;
 } gba_block_tables;
 
 /*
@@ -491,8 +494,8 @@ typedef struct gba_block_tables {
  * Sums are of 64 bits; a step is the same whatever order its threads run in.
  *
  * Errors: GBA_EINVAL for tables == NULL, negative sizes, block_size < 1, a
- * NULL table, held, free_blocks, free_count, lens, count, offsets or status
- * with requests > 0, parents without mask; GBA_EUNSUPPORTED for more than
+ * NULL table, held, free_blocks, free_count, scratch, lens, count, offsets or
+ * status with requests > 0, parents without mask; GBA_EUNSUPPORTED for more than
  * GBA_MAX_REQUESTS requests, num_blocks * block_size, tokens or requests *
  * width above 2^31-1 or a pointer not aligned to its elements;
  * GBA_EHIP if a launch fails.

@@ -2,24 +2,38 @@
 // lengths, on the GPU.
 //
 // Three running sums over the requests say everything: of the blocks given
-// back, of the blocks wanted and of the new tokens.  Block i given back and
-// block j handed out then find their request by a search in those sums, so
-// all of them move in parallel, and what happens does not depend on the order
-// of the threads.  The first kernel is one workgroup (the stack is pushed
-// before it is popped); the second one writes what belongs to each token.
+// back, of the blocks wanted and of the new tokens.  They give each request its
+// places on the stack of free blocks, so that all requests move their blocks
+// at once, one wave each, and what happens does not depend on the order of the
+// threads.  The stack is pushed before it is popped: two kernels, of which each
+// workgroup of the first one takes the running sums for itself (they are a few
+// kilobytes) and pushes for its 16 requests; the second one pops, clears what
+// was given back, and writes what belongs to each token, whose new block it
+// reads from the stack itself.  Between them nothing that either one reads is
+// written.  A small step is one workgroup that does both.
+//
+// Bound by launches and by the latency of four dependent reads, not by bytes.
 #include "gba_decode.hpp"
 
 namespace gba {
 namespace {
 
-constexpr int TABLE_THREADS = 1024;
+constexpr int TABLE_THREADS = 1024, TABLE_WAVES = TABLE_THREADS / 64;
 constexpr int PER_THREAD = GBA_MAX_REQUESTS / TABLE_THREADS;
+constexpr int SMALL_REQUESTS = 64, SMALL_TOKENS = 1024;
+
+// What the second kernel knows of a request: blocks needed and held, the
+// running sum of the blocks wanted before it, and its status; of the step,
+// in the place after the last request's: blocks on the stack after the pushes,
+// blocks handed out, tokens.
+typedef int Plan __attribute__((ext_vector_type(4)));
 
 struct TableArgs {
     int32_t *table, *held, *free_blocks, *free_count;
     const int32_t *lens, *count, *parents;
     int32_t *offsets, *slots, *positions, *status;
     uint64_t *mask;
+    Plan *plan;
     int requests, width, num_blocks, block_size, tokens;
 };
 
@@ -37,161 +51,224 @@ __device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *scratch, int64
     __syncthreads();
     int64_t before = 0;
     total = 0;
-    for (int w = 0; w < TABLE_THREADS / 64; ++w) {
-        if (w < wave) before += scratch[w];
-        total += scratch[w];
+#pragma unroll
+    for (int w = 0; w < TABLE_WAVES; ++w) {
+        const int64_t y = scratch[w];
+        before += w < wave ? y : 0;
+        total += y;
     }
     return before + x - v;
 }
 
-__global__ void __launch_bounds__(TABLE_THREADS) tables_kernel(TableArgs p)
+// The step's plan, for a whole workgroup: into `plan`, requests + 1 of them;
+// `pushed` is the running sum of the blocks given back before each request.
+// With `writes`, offsets and status too.  Returns the blocks on the stack
+// before the step.
+__device__ __forceinline__ int make_plan(const TableArgs &p, Plan *plan, int *pushed, bool writes)
 {
-    __shared__ int32_t need_of[GBA_MAX_REQUESTS], held_of[GBA_MAX_REQUESTS];
-    __shared__ int32_t back[GBA_MAX_REQUESTS + 1], want[GBA_MAX_REQUESTS + 1];  // running sums
-    __shared__ int64_t scratch[TABLE_THREADS / 64];
-    const int R = p.requests, W = p.width, first = threadIdx.x * PER_THREAD;
+    __shared__ int64_t scratch[TABLE_WAVES];
+    __shared__ int handed_out;
+    const int R = p.requests, W = p.width;
+    // few requests: one a thread, so that their loads are all under way at once
+    const int each = R > TABLE_THREADS ? PER_THREAD : 1, first = threadIdx.x * each;
     int fc = *p.free_count;
     fc = fc < 0 ? 0 : fc > p.num_blocks ? p.num_blocks : fc;
+    if (threadIdx.x == 0) handed_out = 0;
 
-    int state[PER_THREAD], wants[PER_THREAD], backs[PER_THREAD];
+    int state[PER_THREAD], need[PER_THREAD], held[PER_THREAD];
     int64_t fresh[PER_THREAD], sum_fresh = 0, total;
+#pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         const int r = first + i;
-        const int n = r < R ? p.count[r] : 0;
+        const bool real = i < each && r < R;
+        const int n = real ? p.count[r] : 0, kept = real ? p.lens[r] : 0, h = real ? p.held[r] : 0;
         fresh[i] = n > 0 ? n : 0;
+        const uint32_t end = (uint32_t)(kept > 0 ? kept : 0) + (uint32_t)fresh[i];
+        const uint32_t want = end > 0 ? (end - 1) / (uint32_t)p.block_size + 1 : 0;
+        state[i] = want > (uint32_t)W ? 2 : 0;
+        need[i] = want > (uint32_t)W ? W : (int)want;
+        held[i] = h < 0 ? 0 : h > W ? W : h;
         sum_fresh += fresh[i];
     }
     int64_t at = block_scan(sum_fresh, scratch, total);
-    int64_t sum_back = 0, sum_want = 0;
+    // blocks given back in the upper half of a sum, those wanted in the lower:
+    // each is at most requests * width, so of 31 bits
+    int64_t sum = 0;
+#pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         const int r = first + i;
-        state[i] = wants[i] = backs[i] = 0;
-        if (r < R) {
-            const int n = p.lens[r];
-            const int64_t need = (((int64_t)(n > 0 ? n : 0) + fresh[i]) + p.block_size - 1) / p.block_size;
-            int held = p.held[r];
-            held = held < 0 ? 0 : held > W ? W : held;
-            p.offsets[r] = (int32_t)(at < p.tokens ? at : p.tokens);
-            at += fresh[i];
-            if (need > W) state[i] = 2;
-            else if (at > p.tokens || (p.parents != nullptr && fresh[i] > 64)) state[i] = 3;
-            if (need < held) backs[i] = held - (int)need;
-            else if (state[i] == 0) wants[i] = (int)need - held;
-            need_of[r] = (int)(need < W ? need : W);
-            held_of[r] = held;
-        }
-        sum_back += backs[i];
-        sum_want += wants[i];
+        const bool real = i < each && r < R;
+        if (writes && real) p.offsets[r] = (int32_t)(at < p.tokens ? at : p.tokens);
+        at += fresh[i];
+        if (state[i] == 0 && (at > p.tokens || (p.parents != nullptr && fresh[i] > 64))) state[i] = 3;
+        if (real && need[i] < held[i]) sum += (int64_t)(held[i] - need[i]) << 32;
+        else if (real && state[i] == 0) sum += need[i] - held[i];
     }
-    if (threadIdx.x == 0) p.offsets[R] = (int32_t)(total < p.tokens ? total : p.tokens);
-    int64_t total_back, total_want;
-    int64_t b = block_scan(sum_back, scratch, total_back), w = block_scan(sum_want, scratch, total_want);
-    for (int i = 0; i < PER_THREAD; ++i) {
-        back[first + i] = (int32_t)b;
-        want[first + i] = (int32_t)w;
-        b += backs[i];
-        w += wants[i];
-    }
-    if (threadIdx.x == TABLE_THREADS - 1) {
-        back[GBA_MAX_REQUESTS] = (int32_t)b;
-        want[GBA_MAX_REQUESTS] = (int32_t)w;
-    }
-    __syncthreads();
-
-    // blocks given back, onto the stack
-    for (int64_t i = threadIdx.x; i < total_back; i += TABLE_THREADS) {
-        const int r = owner_of(back, R, i);
-        int32_t *entry = p.table + (int64_t)r * W + need_of[r] + (i - back[r]);
-        if (fc + i < p.num_blocks) p.free_blocks[fc + i] = *entry;
-        *entry = -1;
-    }
-    __syncthreads();
-
-    // blocks handed out, from its top: to the requests whose running sum fits
-    const int64_t avail = fc + total_back;
-    const int first_short = owner_of(want, R, avail);  // the first one whose sum passes avail
-    const int64_t given = want[first_short];
-    for (int64_t i = threadIdx.x; i < given; i += TABLE_THREADS) {
-        const int r = owner_of(want, R, i);
-        const int64_t from = avail - 1 - i;
-        p.table[(int64_t)r * W + held_of[r] + (i - want[r])] = from < p.num_blocks ? p.free_blocks[from] : -1;
-    }
+    int64_t all, before = block_scan(sum, scratch, all);
+    const int avail = fc + (int)(all >> 32);
+#pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         const int r = first + i;
-        if (r >= R) break;
-        if (wants[i] > 0 && r >= first_short) {
-            state[i] = 1;
-            wants[i] = 0;
-        }
-        p.held[r] = held_of[r] - backs[i] + wants[i];
-        if (p.status != nullptr) p.status[r] = state[i];
+        if (i >= each || r >= R) break;
+        const int back = held[i] > need[i] ? held[i] - need[i] : 0, want = back == 0 && state[i] == 0 ? need[i] - held[i] : 0;
+        const int wanted = (int)(before & 0xFFFFFFFF);
+        if (want > 0 && wanted > avail - want) state[i] = 1;  // the running sum with its own passes what there is
+        else if (want > 0) atomicMax(&handed_out, wanted + want);
+        pushed[r] = (int)(before >> 32);
+        plan[r] = Plan{need[i], held[i], wanted, state[i]};
+        if (writes) p.status[r] = state[i];
+        before += ((int64_t)back << 32) + want;
     }
-    if (threadIdx.x == 0) *p.free_count = (int32_t)(avail - given);
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        const int tokens = (int)(total < p.tokens ? total : p.tokens);
+        plan[R] = Plan{avail, handed_out, tokens, 0};
+        if (writes) p.offsets[R] = tokens;
+    }
+    __syncthreads();
+    return fc;
 }
 
-__device__ __forceinline__ int slot_of(const TableArgs &p, int r, int64_t pos)
+// One wave: the blocks that request r gives back, onto the stack.
+__device__ __forceinline__ void push(const TableArgs &p, int r, const Plan &q, int64_t to, int lane)
 {
-    const int64_t column = pos / p.block_size;
-    if (column >= p.width) return -1;
-    // an entry is missing where the request got no blocks
-    const int entry = column < p.held[r] ? p.table[(int64_t)r * p.width + column] : -1;
-    return entry < 0 ? -1 : (int)((int64_t)entry * p.block_size + (pos - column * p.block_size));
+    const int32_t *from = p.table + (int64_t)r * p.width + q[0];
+    for (int i = lane; i < q[1] - q[0]; i += 64)
+        if (to + i < p.num_blocks) p.free_blocks[to + i] = from[i];
 }
 
-// Chains: one thread a token.
-__global__ void __launch_bounds__(256) chain_kernel(TableArgs p)
+// Entry `column` of a request's row after the step.
+__device__ __forceinline__ int entry_of(const TableArgs &p, int r, const Plan &q, int avail, int column)
 {
-    const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (t >= p.tokens) return;
-    const int r = owner_of(p.offsets, p.requests, t);
-    int64_t pos = -1;
-    int slot = -1;
-    if (r < p.requests) {
-        const int n = p.lens[r];
-        pos = (int64_t)(n > 0 ? n : 0) + (t - p.offsets[r]);
-        if (p.status[r] == 0) slot = slot_of(p, r, pos);
-    }
+    if (column < q[1]) return p.table[(int64_t)r * p.width + column];
+    const int from = avail - 1 - (q[2] + column - q[1]);
+    return from >= 0 && from < p.num_blocks ? p.free_blocks[from] : -1;
+}
+
+// One wave: request r's row and holdings.
+__device__ __forceinline__ void pop(const TableArgs &p, int r, const Plan &q, int avail, int lane)
+{
+    int32_t *row = p.table + (int64_t)r * p.width;
+    const int end = q[3] == 0 && q[0] > q[1] ? q[0] : q[1];
+    for (int i = q[1] + lane; i < end; i += 64) row[i] = entry_of(p, r, q, avail, i);
+    for (int i = q[0] + lane; i < q[1]; i += 64) row[i] = -1;
+    if (lane == 0) p.held[r] = q[0] < q[1] ? q[0] : end;
+}
+
+__device__ __forceinline__ void write_token(const TableArgs &p, int t, int slot, int64_t position)
+{
     if (p.slots != nullptr) p.slots[t] = slot;
-    if (p.positions != nullptr) p.positions[t] = (int32_t)pos;
+    if (p.positions != nullptr) p.positions[t] = (int32_t)position;
 }
 
-// Trees: one wave a request, one lane a token.  A token's mask is its own bit
-// and those of its ancestors, found by doubling: six rounds in which every
-// token takes the mask of the token it points to and then points to where
-// that one points.
-__global__ void __launch_bounds__(256) tree_kernel(TableArgs p)
+__device__ __forceinline__ int slot_of(const TableArgs &p, int r, const Plan &q, int avail, int64_t pos)
 {
-    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (r < p.requests) {
-        const int first = p.offsets[r], T = p.offsets[r + 1] - first;
-        const int n = p.lens[r], status = p.status[r];
-        if (T <= 64) {
-            const int parent = lane < T ? p.parents[first + lane] : -1;
-            int up = parent >= 0 && parent < lane ? parent : lane;
-            uint64_t mask = 1ull << lane;
-            for (int i = 0; i < 6; ++i) {
-                mask |= __shfl(mask, up);
-                up = __shfl(up, up);
-            }
-            if (lane < T) {
-                const int64_t kept = n > 0 ? n : 0;
-                if (p.slots != nullptr) p.slots[first + lane] = status == 0 ? slot_of(p, r, kept + lane) : -1;
-                if (p.positions != nullptr) p.positions[first + lane] = (int32_t)(kept + __popcll(mask) - 1);
-                p.mask[first + lane] = mask;
-            }
-        } else {
-            for (int i = lane; i < T; i += 64) {
-                if (p.slots != nullptr) p.slots[first + i] = -1;
-                if (p.positions != nullptr) p.positions[first + i] = -1;
-                p.mask[first + i] = 0;
-            }
+    if (q[3] != 0) return -1;
+    const int column = (int)((uint32_t)pos / (uint32_t)p.block_size), entry = entry_of(p, r, q, avail, column);
+    return entry < 0 ? -1 : (int)((int64_t)entry * p.block_size + (pos - (int64_t)column * p.block_size));
+}
+
+// One wave: the tokens of request r, a tree, one a lane.  A token's mask is its
+// own bit and those of its ancestors, found by doubling: six rounds in which
+// every token takes the mask of the token it points to and then points to where
+// that one points.
+__device__ __forceinline__ void tree(const TableArgs &p, int r, const Plan &q, int avail, int first, int T, int lane)
+{
+    if (T > 64) {
+        for (int i = lane; i < T; i += 64) {
+            write_token(p, first + i, -1, -1);
+            p.mask[first + i] = 0;
+        }
+        return;
+    }
+    const int n = p.lens[r], parent = lane < T ? p.parents[first + lane] : -1;
+    const int64_t kept = n > 0 ? n : 0;
+    const int slot = lane < T ? slot_of(p, r, q, avail, kept + lane) : -1;
+    int up = parent >= 0 && parent < lane ? parent : lane;
+    uint64_t mask = 1ull << lane;
+    for (int i = 0; i < 6; ++i) {
+        mask |= __shfl(mask, up);
+        up = __shfl(up, up);
+    }
+    if (lane < T) {
+        write_token(p, first + lane, slot, kept + __popcll(mask) - 1);
+        p.mask[first + lane] = mask;
+    }
+}
+
+// Entries past the last request's tokens.
+__device__ __forceinline__ void pad(const TableArgs &p, int64_t t, int64_t step)
+{
+    for (; t < p.tokens; t += step) {
+        write_token(p, (int)t, -1, -1);
+        if (p.parents != nullptr) p.mask[t] = 0;
+    }
+}
+
+__global__ void __launch_bounds__(TABLE_THREADS) small_kernel(TableArgs p)
+{
+    __shared__ Plan plan[SMALL_REQUESTS + 1];
+    __shared__ int pushed[SMALL_REQUESTS], begin[SMALL_REQUESTS + 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int fc = make_plan(p, plan, pushed, true);
+    const int avail = plan[p.requests][0], tokens = plan[p.requests][2];
+    if (threadIdx.x <= p.requests) begin[threadIdx.x] = p.offsets[threadIdx.x];
+    for (int r = wave; r < p.requests; r += TABLE_WAVES) push(p, r, plan[r], (int64_t)fc + pushed[r], lane);
+    __syncthreads();
+    // each entry's last reader before its writer: a token reads only what is
+    // its request's and stays, or the stack
+    if (p.parents != nullptr) {
+        for (int r = wave; r < p.requests; r += TABLE_WAVES) tree(p, r, plan[r], avail, begin[r], begin[r + 1] - begin[r], lane);
+    } else {
+        for (int t = threadIdx.x; t < tokens; t += TABLE_THREADS) {
+            const int r = owner_of(begin, p.requests, t), n = p.lens[r];
+            const int64_t pos = (int64_t)(n > 0 ? n : 0) + (t - begin[r]);
+            write_token(p, t, slot_of(p, r, plan[r], avail, pos), pos);
         }
     }
-    for (int64_t t = p.offsets[p.requests] + (int64_t)blockIdx.x * 256 + threadIdx.x; t < p.tokens; t += (int64_t)gridDim.x * 256) {
-        if (p.slots != nullptr) p.slots[t] = -1;
-        if (p.positions != nullptr) p.positions[t] = -1;
-        p.mask[t] = 0;
+    for (int r = wave; r < p.requests; r += TABLE_WAVES) pop(p, r, plan[r], avail, lane);
+    pad(p, tokens + threadIdx.x, TABLE_THREADS);
+    if (threadIdx.x == 0) *p.free_count = avail - plan[p.requests][1];
+}
+
+// 16 requests a workgroup.
+__global__ void __launch_bounds__(TABLE_THREADS) push_kernel(TableArgs p)
+{
+    __shared__ Plan plan[GBA_MAX_REQUESTS + 1];
+    __shared__ int pushed[GBA_MAX_REQUESTS];
+    const int lane = threadIdx.x & 63, r = blockIdx.x * TABLE_WAVES + (threadIdx.x >> 6);
+    const int fc = make_plan(p, plan, pushed, blockIdx.x == 0);
+    if (r < p.requests) {
+        push(p, r, plan[r], (int64_t)fc + pushed[r], lane);
+        if (lane == 0) p.plan[r] = plan[r];
     }
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.plan[p.requests] = plan[p.requests];
+}
+
+// The first workgroups: four requests each.  The others, for chains: 256
+// tokens each.
+__global__ void __launch_bounds__(256) pop_kernel(TableArgs p, int request_groups)
+{
+    __shared__ int begin[GBA_MAX_REQUESTS + 1];
+    const int lane = threadIdx.x & 63, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const Plan step = p.plan[p.requests];
+    if ((int)blockIdx.x < request_groups) {
+        if (r < p.requests) {
+            const Plan q = p.plan[r];
+            if (p.parents != nullptr) tree(p, r, q, step[0], p.offsets[r], p.offsets[r + 1] - p.offsets[r], lane);
+            pop(p, r, q, step[0], lane);
+        }
+        pad(p, step[2] + (int64_t)blockIdx.x * 256 + threadIdx.x, (int64_t)request_groups * 256);
+        if (blockIdx.x == 0 && threadIdx.x == 0) *p.free_count = step[0] - step[1];
+        return;
+    }
+    const int64_t t = (int64_t)((int)blockIdx.x - request_groups) * 256 + threadIdx.x;
+    for (int i = threadIdx.x; i <= p.requests; i += 256) begin[i] = p.offsets[i];
+    __syncthreads();
+    if (t >= step[2]) return;
+    const int of = owner_of(begin, p.requests, t), n = p.lens[of];
+    const int64_t pos = (int64_t)(n > 0 ? n : 0) + (t - begin[of]);
+    write_token(p, (int)t, slot_of(p, of, p.plan[of], step[0], pos), pos);
 }
 
 }  // namespace
@@ -211,12 +288,12 @@ extern "C" gba_status gba_tables_step(const gba_block_tables *b, const int32_t *
     if (parents != nullptr && mask == nullptr) return GBA_EINVAL;
     if (b->requests == 0) return GBA_OK;
     if ((b->width > 0 && b->table == nullptr) || b->held == nullptr || (b->num_blocks > 0 && b->free_blocks == nullptr) ||
-        b->free_count == nullptr || lens == nullptr || count == nullptr || offsets == nullptr || status == nullptr)
+        b->free_count == nullptr || b->scratch == nullptr || lens == nullptr || count == nullptr || offsets == nullptr || status == nullptr)
         return GBA_EINVAL;
     const void *ints[] = {b->table, b->held, b->free_blocks, b->free_count, lens, count, parents, offsets, slots, positions, status};
     for (const void *x : ints)
         if (!aligned_to(x, 4)) return GBA_EUNSUPPORTED;
-    if (!aligned_to(mask, 8)) return GBA_EUNSUPPORTED;
+    if (!aligned_to(mask, 8) || !aligned_to(b->scratch, 16)) return GBA_EUNSUPPORTED;
     TableArgs a;
     a.table = b->table;
     a.held = b->held;
@@ -230,14 +307,16 @@ extern "C" gba_status gba_tables_step(const gba_block_tables *b, const int32_t *
     a.positions = positions;
     a.status = status;
     a.mask = mask;
+    a.plan = reinterpret_cast<Plan *>(b->scratch);
     a.requests = (int)b->requests;
     a.width = (int)b->width;
     a.num_blocks = (int)b->num_blocks;
     a.block_size = (int)b->block_size;
     a.tokens = (int)tokens;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    const gba_status st = launch(tables_kernel, dim3(1), dim3(TABLE_THREADS), s, a);
-    if (st != GBA_OK || tokens == 0) return st;
-    if (parents != nullptr) return launch(tree_kernel, dim3((unsigned)div_up(b->requests, 4)), dim3(256), s, a);
-    return launch(chain_kernel, dim3((unsigned)div_up(tokens, 256)), dim3(256), s, a);
+    if (b->requests <= SMALL_REQUESTS && tokens <= SMALL_TOKENS) return launch(small_kernel, dim3(1), dim3(TABLE_THREADS), s, a);
+    const gba_status st = launch(push_kernel, dim3((unsigned)div_up(b->requests, TABLE_WAVES)), dim3(TABLE_THREADS), s, a);
+    if (st != GBA_OK) return st;
+    const int groups = (int)div_up(b->requests, 4);
+    return launch(pop_kernel, dim3((unsigned)(groups + (parents != nullptr ? 0 : div_up(tokens, 256)))), dim3(256), s, a, groups);
 }

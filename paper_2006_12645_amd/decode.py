@@ -25,12 +25,22 @@ def _gpu(name, t, dtype):
         raise TypeError(f"{name} must be a CUDA tensor of {dtype}")
 
 
-def _ints(name, t, shape):
+def _ints(name, t, shape, dtype=torch.int32):
     """A contiguous int32 CUDA tensor of this shape."""
-    if t.dtype is not torch.int32 or not t.is_cuda:
+    if t.dtype is not dtype or not t.is_cuda:
         raise TypeError(f"{name} must be an int32 CUDA tensor")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _stream_of(stream, index):
+    """The HIP stream to launch on: `stream`, else torch's current one of device `index`."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(index)
+    return gba._stream_handle(stream, torch.device("cuda", index))
 
 
 def _empty(shape, dtype, device, stream):
@@ -72,6 +82,7 @@ class Q4Weight:
         self._desc = gba.Q4WeightDesc(DTYPES[scales.dtype], group, K, N, codes.data_ptr(), scales.data_ptr(),
                                       None if zeros is None else zeros.data_ptr())
         self._ref = ctypes.byref(self._desc)
+        self._index, self._call = scales.device.index, gba.lib().gba_q4_linear
 
 
 def q4_pack(codes, stream=None):
@@ -99,29 +110,38 @@ def q4_linear(x, w, bias=None, act="none", out=None, stream=None):
     x, bias (N,) and out (M, N; allocated when None) are of the weight's
     dtype, x and out row-major with any row stride.
     """
+    # A call of a few rows is bound by this function and the launch: plain
+    # comparisons, and the weight's handle holds what does not change.
     M, K = x.shape
-    dtype = w.dtype
+    dtype, N = w.dtype, w.N
     if K != w.K:
         raise ValueError(f"x has {K} columns, the weight {w.K} rows")
-    for name, t in (("x", x), ("bias", bias), ("out", out)):
-        if t is not None and (t.dtype is not dtype or not t.is_cuda):
-            raise TypeError(f"{name} must be a CUDA tensor of the weight's dtype, {dtype}")
-    lda = gba._row_major_ld(x, "x")
-    if K > 1 and x.stride(1) != 1:
+    if x.dtype is not dtype or not x.is_cuda:
+        raise TypeError(f"x must be a CUDA tensor of the weight's dtype, {dtype}")
+    lda, unit = x.stride()
+    if M <= 1:
+        lda = K if K > 0 else 1
+    if unit != 1 and K > 1 or lda < K:
         raise ValueError("x must be a row-major (M, K) matrix")
-    N = w.N
-    if bias is not None and (bias.dim() != 1 or bias.shape[0] != N or (N > 1 and bias.stride(0) != 1)):
-        raise ValueError("bias must be a contiguous (N,) vector")
+    b = None
+    if bias is not None:
+        if bias.dtype is not dtype or not bias.is_cuda:
+            raise TypeError(f"bias must be a CUDA tensor of the weight's dtype, {dtype}")
+        if bias.dim() != 1 or bias.shape[0] != N or (N > 1 and bias.stride(0) != 1):
+            raise ValueError("bias must be a contiguous (N,) vector")
+        b = bias.data_ptr()
     if out is None:
-        out = _empty((M, N), dtype, x.device, stream)
-        ldc = max(N, 1)
+        out = x.new_empty((M, N)) if stream is None else _empty((M, N), dtype, x.device, stream)
+        ldc = N if N > 0 else 1
     else:
+        if out.dtype is not dtype or not out.is_cuda:
+            raise TypeError(f"out must be a CUDA tensor of the weight's dtype, {dtype}")
         if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
             raise ValueError("out must be a row-major (M, N) matrix")
         ldc = gba._row_major_ld(out, "out")
-    gba._check(gba.lib().gba_q4_linear(w._ref, M, x.data_ptr(), lda, None if bias is None else bias.data_ptr(),
-                                       gba.ACTS[act], out.data_ptr(), ldc, gba._stream_handle(stream, x.device)),
-               "gba_q4_linear")
+    status = w._call(w._ref, M, x.data_ptr(), lda, b, gba.ACTS[act], out.data_ptr(), ldc, _stream_of(stream, w._index))
+    if status:
+        raise gba.GbaError(status, "gba_q4_linear")
     return out
 
 
@@ -154,10 +174,16 @@ class BlockTables:
         self.table, self.held, self.free_blocks, self.free_count = table, held, free_blocks, free_count
         self.block_size, self.tokens, self.tree = block_size, tokens, tree
         self.requests, self.device = requests, table.device
+        self._plan = torch.empty(4 * (requests + 1), dtype=torch.int32, device=table.device)  # the step's own scratch
         self._sizes = [requests + 1, tokens, tokens, requests]
         self._desc = gba.BlockTablesDesc(requests, width, free_blocks.shape[0], block_size, table.data_ptr(), held.data_ptr(),
-                                         free_blocks.data_ptr(), free_count.data_ptr())
+                                         free_blocks.data_ptr(), free_count.data_ptr(), self._plan.data_ptr())
         self._ref = ctypes.byref(self._desc)
+        self._index, self._call, self._shape = table.device.index, gba.lib().gba_tables_step, (requests,)
+        # where the maps stand in one allocation: each at a multiple of 16 bytes
+        self._at = [0]
+        for n in self._sizes:
+            self._at.append(self._at[-1] + -(-n // 4) * 4)
 
     @classmethod
     def empty(cls, requests, width, num_blocks, block_size, *, tokens, tree=False, device="cuda"):
@@ -169,9 +195,9 @@ class BlockTables:
 
     def maps(self, stream=None):
         """Uninitialised StepMaps for step(out=...)."""
-        flat = _empty(sum(self._sizes), torch.int32, self.device, stream)
+        flat = _empty(self._at[4], torch.int32, self.device, stream)
         mask = _empty((self.tokens, 1), torch.int64, self.device, stream) if self.tree else None
-        return StepMaps(*flat.split(self._sizes), mask)
+        return StepMaps(*(flat.narrow(0, at, n) for at, n in zip(self._at, self._sizes)), mask)
 
     def step(self, lens, new, parents=None, out=None, stream=None):
         """Room for each request's new[r] tokens after the lens[r] that it
@@ -182,9 +208,9 @@ class BlockTables:
         (tokens,), each new token's parent among its request's new ones, -1
         for a root.  out: StepMaps to write (a captured graph's).
         """
-        R, T = self.requests, self.tokens
-        _ints("lens", lens, (R,))
-        _ints("new", new, (R,))
+        T = self.tokens
+        _ints("lens", lens, self._shape)
+        _ints("new", new, self._shape)
         if (parents is not None) != self.tree:
             raise ValueError("parents come with tree=True" if parents is not None else "a tree's steps need parents")
         if parents is not None:
@@ -198,10 +224,11 @@ class BlockTables:
                 m = out.mask
                 if m is None or m.dtype is not torch.int64 or not m.is_cuda or m.shape != (T, 1) or not m.is_contiguous():
                     raise ValueError("out.mask must be a contiguous int64 (tokens, 1) CUDA tensor")
-        gba._check(gba.lib().gba_tables_step(
-            self._ref, lens.data_ptr(), new.data_ptr(), None if parents is None else parents.data_ptr(), T,
-            out.offsets.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(), out.status.data_ptr(),
-            out.mask.data_ptr() if self.tree else None, gba._stream_handle(stream, self.device)), "gba_tables_step")
+        status = self._call(self._ref, lens.data_ptr(), new.data_ptr(), None if parents is None else parents.data_ptr(), T,
+                            out.offsets.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(), out.status.data_ptr(),
+                            out.mask.data_ptr() if self.tree else None, _stream_of(stream, self._index))
+        if status:
+            raise gba.GbaError(status, "gba_tables_step")
         return out
 
 
@@ -221,21 +248,27 @@ class PagedCache:
         self.num_blocks, self.block_size, self.heads, self.dim = k.shape
         self._desc = gba.PagedCacheDesc(DTYPES[k.dtype], *k.shape, k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
         self._ref = ctypes.byref(self._desc)
+        L = gba.lib()
+        self._index, self._store, self._attend = k.device.index, L.gba_cache_store, L.gba_tree_attention
 
     def store(self, k, v, slots, stream=None):
         """Write the rows k[t], v[t] (tokens, heads, dim) at slots[t] (int32;
         tokens whose slot is outside the cache are left out)."""
-        dtype, want = self.dtype, (slots.shape[0], self.heads, self.dim)
-        for name, t in (("k", k), ("v", v)):
-            if t.dtype is not dtype or not t.is_cuda:
-                raise TypeError(f"{name} must be a CUDA tensor of the cache's dtype, {dtype}")
-            if t.shape != want or (want[2] > 1 and t.stride(2) != 1):
-                raise ValueError(f"{name} must be {want} with dim contiguous, got {tuple(t.shape)}")
-        _ints("slots", slots, want[:1])
-        kt, kh, _ = k.stride()
-        vt, vh, _ = v.stride()
-        gba._check(gba.lib().gba_cache_store(self._ref, want[0], k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, slots.data_ptr(),
-                                             gba._stream_handle(stream, self.device)), "gba_cache_store")
+        dtype, tokens = self.dtype, slots.shape[0]
+        want = (tokens, self.heads, self.dim)
+        if k.dtype is not dtype or v.dtype is not dtype or not k.is_cuda or not v.is_cuda:
+            raise TypeError(f"k and v must be CUDA tensors of the cache's dtype, {dtype}")
+        if k.shape != want or v.shape != want:
+            raise ValueError(f"k and v must be {want}, got {tuple(k.shape)} and {tuple(v.shape)}")
+        kt, kh, k1 = k.stride()
+        vt, vh, v1 = v.stride()
+        if (k1 != 1 or v1 != 1) and self.dim > 1:
+            raise ValueError("dim must be contiguous in k and v")
+        _ints("slots", slots, (tokens,))
+        status = self._store(self._ref, tokens, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, slots.data_ptr(),
+                             _stream_of(stream, self._index))
+        if status:
+            raise gba.GbaError(status, "gba_cache_store")
 
 
 # Scratch of calls with workspace="auto", one per (device, stream): calls in a

@@ -56,7 +56,7 @@ class Q4WeightDesc(ctypes.Structure):
 class BlockTablesDesc(ctypes.Structure):
     """Mirror of struct gba_block_tables."""
     _fields_ = [("requests", _i64), ("width", _i64), ("num_blocks", _i64), ("block_size", _i64),
-                ("table", _vp), ("held", _vp), ("free_blocks", _vp), ("free_count", _vp)]
+                ("table", _vp), ("held", _vp), ("free_blocks", _vp), ("free_count", _vp), ("scratch", _vp)]
 
 
 class PagedCacheDesc(ctypes.Structure):

@@ -67,7 +67,7 @@ def test_linear_and_pack_refuse_null():
 
 
 def tables(desc=(), **kw):
-    d = gba.BlockTablesDesc(4, 8, 32, 16, FAKE, FAKE, FAKE, FAKE)
+    d = gba.BlockTablesDesc(4, 8, 32, 16, FAKE, FAKE, FAKE, FAKE, FAKE)
     for k, v in dict(desc).items():
         setattr(d, k, v)
     a = dict(lens=FAKE, count=FAKE, parents=None, tokens=16, offsets=FAKE, slots=FAKE, positions=FAKE, status=FAKE, mask=None)
@@ -78,7 +78,8 @@ def tables(desc=(), **kw):
 @pytest.mark.parametrize("kw,status", [
     (dict(desc=dict(requests=-1)), EINVAL), (dict(desc=dict(width=-1)), EINVAL), (dict(desc=dict(num_blocks=-1)), EINVAL),
     (dict(desc=dict(block_size=0)), EINVAL), (dict(tokens=-1), EINVAL), (dict(desc=dict(table=None)), EINVAL),
-    (dict(desc=dict(held=None)), EINVAL), (dict(desc=dict(free_blocks=None)), EINVAL), (dict(desc=dict(free_count=None)), EINVAL),
+    (dict(desc=dict(held=None)), EINVAL), (dict(desc=dict(free_blocks=None)), EINVAL), (dict(desc=dict(free_count=None)), EINVAL), (dict(desc=dict(scratch=None)), EINVAL),
+    (dict(desc=dict(scratch=FAKE + 4)), EUNSUPPORTED),
     (dict(lens=None), EINVAL), (dict(count=None), EINVAL), (dict(offsets=None), EINVAL), (dict(status=None), EINVAL),
     (dict(parents=FAKE), EINVAL), (dict(desc=dict(requests=gba.GBA_MAX_REQUESTS + 1)), EUNSUPPORTED),
     (dict(desc=dict(width=BIG)), EUNSUPPORTED), (dict(desc=dict(requests=4096, width=2 ** 20)), EUNSUPPORTED),
