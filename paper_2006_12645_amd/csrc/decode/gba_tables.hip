@@ -37,46 +37,59 @@ struct TableArgs {
     int requests, width, num_blocks, block_size, tokens;
 };
 
-// Exclusive running sum over the workgroup's threads; total for every thread.
-__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t *scratch, int64_t &total)
+struct Pair {
+    int a, b;
+};
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ void add_moved(Pair &x)
 {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v;
-    for (int d = 1; d < 64; d <<= 1) {
-        const int64_t y = __shfl_up(x, d);
-        if (lane >= d) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) scratch[wave] = x;
-    __syncthreads();
-    int64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < TABLE_WAVES; ++w) {
-        const int64_t y = scratch[w];
-        before += w < wave ? y : 0;
-        total += y;
-    }
-    return before + x - v;
+    x.a += __builtin_amdgcn_update_dpp(0, x.a, CTRL, ROWS, 0xF, false);
+    x.b += __builtin_amdgcn_update_dpp(0, x.b, CTRL, ROWS, 0xF, false);
 }
 
-// The step's plan, for a whole workgroup: into `plan`, requests + 1 of them;
-// `pushed` is the running sum of the blocks given back before each request.
-// With `writes`, offsets and status too.  Returns the blocks on the stack
-// before the step.
-__device__ __forceinline__ int make_plan(const TableArgs &p, Plan *plan, int *pushed, bool writes)
+// Exclusive running sums over the workgroup's threads; totals for every thread.
+__device__ __forceinline__ Pair block_scan(Pair v, Pair *scratch, Pair &total)
 {
-    __shared__ int64_t scratch[TABLE_WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    Pair x = v;
+    add_moved<0x111, 0xF>(x);  // one lane up, within 16
+    add_moved<0x112, 0xF>(x);
+    add_moved<0x114, 0xF>(x);
+    add_moved<0x118, 0xF>(x);
+    add_moved<0x142, 0xA>(x);  // lanes 15 and 47 to the 16 after them
+    add_moved<0x143, 0xC>(x);  // lane 31 to the 32 after it
+    if (lane == 63) scratch[wave] = x;
+    __syncthreads();
+    Pair before = {x.a - v.a, x.b - v.b};
+    total = {0, 0};
+    for (int w = 0; w < waves; ++w) {
+        const Pair y = scratch[w];
+        before.a += w < wave ? y.a : 0;
+        before.b += w < wave ? y.b : 0;
+        total.a += y.a;
+        total.b += y.b;
+    }
+    return before;
+}
+
+// The step's plan.  The whole workgroup takes part; it writes what it finds of
+// requests [base, base + count): into `plan` (and what the step as a whole is
+// into plan[count]), `to`, the place on the stack of the first block that each
+// gives back, offsets and status.
+__device__ __forceinline__ void make_plan(const TableArgs &p, int base, int count, Plan *plan, int64_t *to)
+{
+    __shared__ Pair scratch[2][TABLE_WAVES];
     __shared__ int handed_out;
     const int R = p.requests, W = p.width;
     // few requests: one a thread, so that their loads are all under way at once
-    const int each = R > TABLE_THREADS ? PER_THREAD : 1, first = threadIdx.x * each;
+    const int each = R > (int)blockDim.x ? PER_THREAD : 1, first = threadIdx.x * each;
     int fc = *p.free_count;
     fc = fc < 0 ? 0 : fc > p.num_blocks ? p.num_blocks : fc;
     if (threadIdx.x == 0) handed_out = 0;
 
-    int state[PER_THREAD], need[PER_THREAD], held[PER_THREAD];
-    int64_t fresh[PER_THREAD], sum_fresh = 0, total;
+    int state[PER_THREAD], need[PER_THREAD], held[PER_THREAD], fresh[PER_THREAD];
+    Pair sum = {0, 0}, all;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         const int r = first + i;
@@ -88,45 +101,50 @@ __device__ __forceinline__ int make_plan(const TableArgs &p, Plan *plan, int *pu
         state[i] = want > (uint32_t)W ? 2 : 0;
         need[i] = want > (uint32_t)W ? W : (int)want;
         held[i] = h < 0 ? 0 : h > W ? W : h;
-        sum_fresh += fresh[i];
+        // tokens in two halves, whose sums fit 32 bits
+        sum.a += fresh[i] >> 16;
+        sum.b += fresh[i] & 0xFFFF;
     }
-    int64_t at = block_scan(sum_fresh, scratch, total);
-    // blocks given back in the upper half of a sum, those wanted in the lower:
-    // each is at most requests * width, so of 31 bits
-    int64_t sum = 0;
+    const Pair start = block_scan(sum, scratch[0], all);
+    int64_t at = ((int64_t)start.a << 16) + start.b;
+    const int64_t total = ((int64_t)all.a << 16) + all.b;
+    const int tokens = (int)(total < p.tokens ? total : p.tokens);
+    // blocks given back and blocks wanted: each sum is at most requests * width
+    sum = {0, 0};
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         const int r = first + i;
         const bool real = i < each && r < R;
-        if (writes && real) p.offsets[r] = (int32_t)(at < p.tokens ? at : p.tokens);
+        if (real && r >= base && r < base + count) p.offsets[r] = (int32_t)(at < p.tokens ? at : p.tokens);
         at += fresh[i];
         if (state[i] == 0 && (at > p.tokens || (p.parents != nullptr && fresh[i] > 64))) state[i] = 3;
-        if (real && need[i] < held[i]) sum += (int64_t)(held[i] - need[i]) << 32;
-        else if (real && state[i] == 0) sum += need[i] - held[i];
+        if (real && need[i] < held[i]) sum.a += held[i] - need[i];
+        else if (real && state[i] == 0) sum.b += need[i] - held[i];
     }
-    int64_t all, before = block_scan(sum, scratch, all);
-    const int avail = fc + (int)(all >> 32);
+    Pair before = block_scan(sum, scratch[1], all);
+    const int64_t avail = (int64_t)fc + all.a;
 #pragma unroll
     for (int i = 0; i < PER_THREAD; ++i) {
         const int r = first + i;
         if (i >= each || r >= R) break;
         const int back = held[i] > need[i] ? held[i] - need[i] : 0, want = back == 0 && state[i] == 0 ? need[i] - held[i] : 0;
-        const int wanted = (int)(before & 0xFFFFFFFF);
-        if (want > 0 && wanted > avail - want) state[i] = 1;  // the running sum with its own passes what there is
-        else if (want > 0) atomicMax(&handed_out, wanted + want);
-        pushed[r] = (int)(before >> 32);
-        plan[r] = Plan{need[i], held[i], wanted, state[i]};
-        if (writes) p.status[r] = state[i];
-        before += ((int64_t)back << 32) + want;
+        if (want > 0 && before.b + (int64_t)want > avail) state[i] = 1;
+        else if (want > 0) atomicMax(&handed_out, before.b + want);
+        if (r >= base && r < base + count) {
+            plan[r - base] = Plan{need[i], held[i], before.b, state[i]};
+            to[r - base] = (int64_t)fc + before.a;
+            p.status[r] = state[i];
+        }
+        before.a += back;
+        before.b += want;
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        const int tokens = (int)(total < p.tokens ? total : p.tokens);
-        plan[R] = Plan{avail, handed_out, tokens, 0};
-        if (writes) p.offsets[R] = tokens;
+        // more on the stack than it has places: blocks that no request held
+        plan[count] = Plan{avail < INT_MAX ? (int)avail : INT_MAX, handed_out, tokens, 0};
+        if (base + count >= R) p.offsets[R] = tokens;
     }
     __syncthreads();
-    return fc;
 }
 
 // One wave: the blocks that request r gives back, onto the stack.
@@ -208,41 +226,43 @@ __device__ __forceinline__ void pad(const TableArgs &p, int64_t t, int64_t step)
 __global__ void __launch_bounds__(TABLE_THREADS) small_kernel(TableArgs p)
 {
     __shared__ Plan plan[SMALL_REQUESTS + 1];
-    __shared__ int pushed[SMALL_REQUESTS], begin[SMALL_REQUESTS + 1];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int fc = make_plan(p, plan, pushed, true);
+    __shared__ int64_t to[SMALL_REQUESTS];
+    __shared__ int begin[SMALL_REQUESTS + 1];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+    make_plan(p, 0, p.requests, plan, to);
     const int avail = plan[p.requests][0], tokens = plan[p.requests][2];
-    if (threadIdx.x <= p.requests) begin[threadIdx.x] = p.offsets[threadIdx.x];
-    for (int r = wave; r < p.requests; r += TABLE_WAVES) push(p, r, plan[r], (int64_t)fc + pushed[r], lane);
+    if ((int)threadIdx.x <= p.requests) begin[threadIdx.x] = p.offsets[threadIdx.x];
+    for (int r = wave; r < p.requests; r += waves) push(p, r, plan[r], to[r], lane);
     __syncthreads();
-    // each entry's last reader before its writer: a token reads only what is
-    // its request's and stays, or the stack
+    // nothing that a token reads is written here: what its request keeps, and
+    // the stack
     if (p.parents != nullptr) {
-        for (int r = wave; r < p.requests; r += TABLE_WAVES) tree(p, r, plan[r], avail, begin[r], begin[r + 1] - begin[r], lane);
+        for (int r = wave; r < p.requests; r += waves) tree(p, r, plan[r], avail, begin[r], begin[r + 1] - begin[r], lane);
     } else {
-        for (int t = threadIdx.x; t < tokens; t += TABLE_THREADS) {
+        for (int t = threadIdx.x; t < tokens; t += blockDim.x) {
             const int r = owner_of(begin, p.requests, t), n = p.lens[r];
             const int64_t pos = (int64_t)(n > 0 ? n : 0) + (t - begin[r]);
             write_token(p, t, slot_of(p, r, plan[r], avail, pos), pos);
         }
     }
-    for (int r = wave; r < p.requests; r += TABLE_WAVES) pop(p, r, plan[r], avail, lane);
-    pad(p, tokens + threadIdx.x, TABLE_THREADS);
+    for (int r = wave; r < p.requests; r += waves) pop(p, r, plan[r], avail, lane);
+    pad(p, tokens + threadIdx.x, blockDim.x);
     if (threadIdx.x == 0) *p.free_count = avail - plan[p.requests][1];
 }
 
-// 16 requests a workgroup.
+// A request a wave.
 __global__ void __launch_bounds__(TABLE_THREADS) push_kernel(TableArgs p)
 {
-    __shared__ Plan plan[GBA_MAX_REQUESTS + 1];
-    __shared__ int pushed[GBA_MAX_REQUESTS];
-    const int lane = threadIdx.x & 63, r = blockIdx.x * TABLE_WAVES + (threadIdx.x >> 6);
-    const int fc = make_plan(p, plan, pushed, blockIdx.x == 0);
-    if (r < p.requests) {
-        push(p, r, plan[r], (int64_t)fc + pushed[r], lane);
-        if (lane == 0) p.plan[r] = plan[r];
+    __shared__ Plan plan[TABLE_WAVES + 1];
+    __shared__ int64_t to[TABLE_WAVES];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, base = blockIdx.x * waves;
+    const int count = p.requests - base < waves ? p.requests - base : waves;
+    make_plan(p, base, count, plan, to);
+    if (wave < count) {
+        push(p, base + wave, plan[wave], to[wave], lane);
+        if (lane == 0) p.plan[base + wave] = plan[wave];
     }
-    if (blockIdx.x == 0 && threadIdx.x == 0) p.plan[p.requests] = plan[p.requests];
+    if (base + count >= p.requests && threadIdx.x == 0) p.plan[p.requests] = plan[count];
 }
 
 // The first workgroups: four requests each.  The others, for chains: 256
@@ -314,8 +334,10 @@ extern "C" gba_status gba_tables_step(const gba_block_tables *b, const int32_t *
     a.block_size = (int)b->block_size;
     a.tokens = (int)tokens;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (b->requests <= SMALL_REQUESTS && tokens <= SMALL_TOKENS) return launch(small_kernel, dim3(1), dim3(TABLE_THREADS), s, a);
-    const gba_status st = launch(push_kernel, dim3((unsigned)div_up(b->requests, TABLE_WAVES)), dim3(TABLE_THREADS), s, a);
+    if (b->requests <= SMALL_REQUESTS && tokens <= SMALL_TOKENS)
+        return launch(small_kernel, dim3(1), dim3(b->requests <= 4 && tokens <= 256 ? 256 : TABLE_THREADS), s, a);
+    const int threads = b->requests <= 256 ? 256 : TABLE_THREADS;
+    const gba_status st = launch(push_kernel, dim3((unsigned)div_up(b->requests, threads / 64)), dim3(threads), s, a);
     if (st != GBA_OK) return st;
     const int groups = (int)div_up(b->requests, 4);
     return launch(pop_kernel, dim3((unsigned)(groups + (parents != nullptr ? 0 : div_up(tokens, 256)))), dim3(256), s, a, groups);
