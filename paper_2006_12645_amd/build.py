@@ -4,7 +4,8 @@ The entry points (csrc/gba_api.hip), one kernel-instantiation unit per
 operand-layout pair and kernel variant (csrc/gba_gemm_unit.hip compiled with
 GBA_LA, GBA_LB, GBA_PRO, GBA_DUAL set) and the operators of a decoding step
 (csrc/decode, one unit each) are compiled in parallel, then linked into
-``paper_2006_12645_amd/libgba.so``.  Every hipcc line carries
+``paper_2006_12645_amd/libgba.so``; then the Python extension of those operators
+(_gba_decode.so) is compiled with g++.  Every hipcc line carries
 ``-Xclang -target-feature -Xclang -packed-fp32-ops`` so the device compiler
 never forms packed fp32 instructions.
 """
@@ -19,6 +20,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libgba.so")
+BINDING = os.path.join(PKG, "_gba_decode.so")
 ARCH = "gfx950"
 
 # (source, extra defines, object name)
@@ -73,7 +75,28 @@ def build(verbose: bool = False) -> str:
     subprocess.run(cmd, check=True)
     _check_no_missing_kernels(tmp)
     os.replace(tmp, LIB)
+    _build_binding(verbose)
     return LIB
+
+
+def _build_binding(verbose):
+    """The Python extension that decode.py calls through (csrc/decode/gba_bind.cpp: host code,
+    against torch's headers and libgba.so)."""
+    import sysconfig
+
+    import torch
+    root = os.path.dirname(torch.__file__)
+    include = os.path.join(root, "include")
+    tmp = BINDING + ".tmp"
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, "-isystem", include,
+           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+           os.path.join(CSRC, "decode", "gba_bind.cpp"), "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python",
+           "-ltorch_cpu", "-lc10", "-L", PKG, "-lgba", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    subprocess.run(cmd, check=True)
+    os.replace(tmp, BINDING)
 
 
 def _check_no_missing_kernels(lib):

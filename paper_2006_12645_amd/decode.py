@@ -6,11 +6,13 @@ Argument marshalling over libgba.so, like :mod:`paper_2006_12645_amd.gba`:
 every step of the computation is a HIP kernel, launched on `stream` or torch's
 current one.  The stored forms are those of include/gba.h.  The three handles
 (Q4Weight, BlockTables, PagedCache) check the tensors a program keeps once and
-hold them; a call checks what it is given.  Calls read nothing back from the
-GPU and may be captured in a HIP graph.
+hold them; a call checks what it is given, in the extension _gba_decode, since
+these calls are bound by the host.  Calls read nothing back from the GPU and may
+be captured in a HIP graph.
 """
 import ctypes
 import math
+import os
 from typing import NamedTuple, Optional
 
 import torch
@@ -25,30 +27,32 @@ def _gpu(name, t, dtype):
         raise TypeError(f"{name} must be a CUDA tensor of {dtype}")
 
 
-def _ints(name, t, shape, dtype=torch.int32):
+def _ints(name, t, shape):
     """A contiguous int32 CUDA tensor of this shape."""
-    if t.dtype is not dtype or not t.is_cuda:
+    if t.dtype is not torch.int32 or not t.is_cuda:
         raise TypeError(f"{name} must be an int32 CUDA tensor")
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
 
 
-_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+_raw_stream = torch._C._cuda_getCurrentRawStream
+
+_binding = None
 
 
-def _stream_of(stream, index):
-    """The HIP stream to launch on: `stream`, else torch's current one of device `index`."""
-    if stream is None and _raw_stream is not None:
-        return _raw_stream(index)
-    return gba._stream_handle(stream, torch.device("cuda", index))
-
-
-def _empty(shape, dtype, device, stream):
-    """torch.empty, of the memory of the stream that the call runs on."""
-    if stream is None:
-        return torch.empty(shape, dtype=dtype, device=device)
-    with torch.cuda.stream(stream):
-        return torch.empty(shape, dtype=dtype, device=device)
+def _calls():
+    """The extension with the calls (loaded once, after libgba.so).  Raises if
+    it has not been built."""
+    global _binding
+    if _binding is None:
+        gba.lib()
+        path = os.path.join(gba.PKG, "_gba_decode.so")
+        if not os.path.exists(path):
+            raise RuntimeError(f"{path} is missing: build it with `python -c 'import __graft_entry__ as g; g.build()'`")
+        from . import _gba_decode
+        _gba_decode.set_error(gba.GbaError)
+        _binding = _gba_decode
+    return _binding
 
 
 class Q4Weight:
@@ -81,8 +85,7 @@ class Q4Weight:
         self.K, self.N, self.group, self.dtype, self.device = K, N, group, scales.dtype, scales.device
         self._desc = gba.Q4WeightDesc(DTYPES[scales.dtype], group, K, N, codes.data_ptr(), scales.data_ptr(),
                                       None if zeros is None else zeros.data_ptr())
-        self._ref = ctypes.byref(self._desc)
-        self._index, self._call = scales.device.index, gba.lib().gba_q4_linear
+        self._at, self._index, self._linear = ctypes.addressof(self._desc), scales.device.index, _calls().linear
 
 
 def q4_pack(codes, stream=None):
@@ -90,9 +93,10 @@ def q4_pack(codes, stream=None):
     _gpu("codes", codes, torch.uint8)
     K, N = codes.shape
     ld = gba._row_major_ld(codes, "codes")
-    packed = _empty((-(-N // 16), -(-K // 128), 64, 4), torch.int32, codes.device, stream)
-    gba._check(gba.lib().gba_q4_pack(K, N, codes.data_ptr(), ld, packed.data_ptr(), gba._stream_handle(stream, codes.device)),
-               "gba_q4_pack")
+    with torch.cuda.stream(stream):  # (None: as it is)
+        packed = torch.empty((-(-N // 16), -(-K // 128), 64, 4), dtype=torch.int32, device=codes.device)
+        gba._check(gba.lib().gba_q4_pack(K, N, codes.data_ptr(), ld, packed.data_ptr(), gba._stream_handle(stream, codes.device)),
+                   "gba_q4_pack")
     return packed
 
 
@@ -110,39 +114,10 @@ def q4_linear(x, w, bias=None, act="none", out=None, stream=None):
     x, bias (N,) and out (M, N; allocated when None) are of the weight's
     dtype, x and out row-major with any row stride.
     """
-    # A call of a few rows is bound by this function and the launch: plain
-    # comparisons, and the weight's handle holds what does not change.
-    M, K = x.shape
-    dtype, N = w.dtype, w.N
-    if K != w.K:
-        raise ValueError(f"x has {K} columns, the weight {w.K} rows")
-    if x.dtype is not dtype or not x.is_cuda:
-        raise TypeError(f"x must be a CUDA tensor of the weight's dtype, {dtype}")
-    lda, unit = x.stride()
-    if M <= 1:
-        lda = K if K > 0 else 1
-    if unit != 1 and K > 1 or lda < K:
-        raise ValueError("x must be a row-major (M, K) matrix")
-    b = None
-    if bias is not None:
-        if bias.dtype is not dtype or not bias.is_cuda:
-            raise TypeError(f"bias must be a CUDA tensor of the weight's dtype, {dtype}")
-        if bias.dim() != 1 or bias.shape[0] != N or (N > 1 and bias.stride(0) != 1):
-            raise ValueError("bias must be a contiguous (N,) vector")
-        b = bias.data_ptr()
-    if out is None:
-        out = x.new_empty((M, N)) if stream is None else _empty((M, N), dtype, x.device, stream)
-        ldc = N if N > 0 else 1
-    else:
-        if out.dtype is not dtype or not out.is_cuda:
-            raise TypeError(f"out must be a CUDA tensor of the weight's dtype, {dtype}")
-        if out.shape != (M, N) or (N > 1 and out.stride(1) != 1):
-            raise ValueError("out must be a row-major (M, N) matrix")
-        ldc = gba._row_major_ld(out, "out")
-    status = w._call(w._ref, M, x.data_ptr(), lda, b, gba.ACTS[act], out.data_ptr(), ldc, _stream_of(stream, w._index))
-    if status:
-        raise gba.GbaError(status, "gba_q4_linear")
-    return out
+    if stream is not None:
+        with torch.cuda.stream(stream):  # its memory for what is allocated
+            return w._linear(w._at, w._index, x, bias, out, gba.ACTS[act], stream.cuda_stream)
+    return w._linear(w._at, w._index, x, bias, out, gba.ACTS[act], _raw_stream(w._index))
 
 
 class StepMaps(NamedTuple):
@@ -172,18 +147,12 @@ class BlockTables:
         if block_size < 1 or tokens < 0:
             raise ValueError("block_size must be positive and tokens not negative")
         self.table, self.held, self.free_blocks, self.free_count = table, held, free_blocks, free_count
-        self.block_size, self.tokens, self.tree = block_size, tokens, tree
+        self.block_size, self.tokens, self.tree = block_size, tokens, bool(tree)
         self.requests, self.device = requests, table.device
         self._plan = torch.empty(4 * (requests + 1), dtype=torch.int32, device=table.device)  # the step's own scratch
-        self._sizes = [requests + 1, tokens, tokens, requests]
         self._desc = gba.BlockTablesDesc(requests, width, free_blocks.shape[0], block_size, table.data_ptr(), held.data_ptr(),
                                          free_blocks.data_ptr(), free_count.data_ptr(), self._plan.data_ptr())
-        self._ref = ctypes.byref(self._desc)
-        self._index, self._call, self._shape = table.device.index, gba.lib().gba_tables_step, (requests,)
-        # where the maps stand in one allocation: each at a multiple of 16 bytes
-        self._at = [0]
-        for n in self._sizes:
-            self._at.append(self._at[-1] + -(-n // 4) * 4)
+        self._at, self._index, self._step = ctypes.addressof(self._desc), table.device.index, _calls().step
 
     @classmethod
     def empty(cls, requests, width, num_blocks, block_size, *, tokens, tree=False, device="cuda"):
@@ -193,11 +162,12 @@ class BlockTables:
                    torch.arange(num_blocks - 1, -1, -1, **i32), torch.full((1,), num_blocks, **i32), block_size,
                    tokens=tokens, tree=tree)
 
-    def maps(self, stream=None):
+    def maps(self):
         """Uninitialised StepMaps for step(out=...)."""
-        flat = _empty(self._at[4], torch.int32, self.device, stream)
-        mask = _empty((self.tokens, 1), torch.int64, self.device, stream) if self.tree else None
-        return StepMaps(*(flat.narrow(0, at, n) for at, n in zip(self._at, self._sizes)), mask)
+        i32 = dict(dtype=torch.int32, device=self.device)
+        R, T = self.requests, self.tokens
+        mask = torch.empty((T, 1), dtype=torch.int64, device=self.device) if self.tree else None
+        return StepMaps(torch.empty(R + 1, **i32), torch.empty(T, **i32), torch.empty(T, **i32), torch.empty(R, **i32), mask)
 
     def step(self, lens, new, parents=None, out=None, stream=None):
         """Room for each request's new[r] tokens after the lens[r] that it
@@ -208,28 +178,10 @@ class BlockTables:
         (tokens,), each new token's parent among its request's new ones, -1
         for a root.  out: StepMaps to write (a captured graph's).
         """
-        T = self.tokens
-        _ints("lens", lens, self._shape)
-        _ints("new", new, self._shape)
-        if (parents is not None) != self.tree:
-            raise ValueError("parents come with tree=True" if parents is not None else "a tree's steps need parents")
-        if parents is not None:
-            _ints("parents", parents, (T,))
-        if out is None:
-            out = self.maps(stream)
-        else:
-            for name, t, n in zip(out._fields, out, self._sizes):
-                _ints(name, t, (n,))
-            if self.tree:
-                m = out.mask
-                if m is None or m.dtype is not torch.int64 or not m.is_cuda or m.shape != (T, 1) or not m.is_contiguous():
-                    raise ValueError("out.mask must be a contiguous int64 (tokens, 1) CUDA tensor")
-        status = self._call(self._ref, lens.data_ptr(), new.data_ptr(), None if parents is None else parents.data_ptr(), T,
-                            out.offsets.data_ptr(), out.slots.data_ptr(), out.positions.data_ptr(), out.status.data_ptr(),
-                            out.mask.data_ptr() if self.tree else None, _stream_of(stream, self._index))
-        if status:
-            raise gba.GbaError(status, "gba_tables_step")
-        return out
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return StepMaps(*self._step(self._at, self._index, lens, new, parents, self.tokens, self.tree, out, stream.cuda_stream))
+        return StepMaps(*self._step(self._at, self._index, lens, new, parents, self.tokens, self.tree, out, _raw_stream(self._index)))
 
 
 class PagedCache:
@@ -246,29 +198,15 @@ class PagedCache:
             raise ValueError("dim must be contiguous")
         self.k, self.v, self.dtype, self.device = k, v, k.dtype, k.device
         self.num_blocks, self.block_size, self.heads, self.dim = k.shape
+        self._scale = 1.0 / math.sqrt(max(self.dim, 1))
         self._desc = gba.PagedCacheDesc(DTYPES[k.dtype], *k.shape, k.data_ptr(), v.data_ptr(), *k.stride()[:3], *v.stride()[:3])
-        self._ref = ctypes.byref(self._desc)
-        L = gba.lib()
-        self._index, self._store, self._attend = k.device.index, L.gba_cache_store, L.gba_tree_attention
+        self._at, self._index = ctypes.addressof(self._desc), k.device.index
+        self._store, self._attend = _calls().store, _calls().attend
 
     def store(self, k, v, slots, stream=None):
         """Write the rows k[t], v[t] (tokens, heads, dim) at slots[t] (int32;
         tokens whose slot is outside the cache are left out)."""
-        dtype, tokens = self.dtype, slots.shape[0]
-        want = (tokens, self.heads, self.dim)
-        if k.dtype is not dtype or v.dtype is not dtype or not k.is_cuda or not v.is_cuda:
-            raise TypeError(f"k and v must be CUDA tensors of the cache's dtype, {dtype}")
-        if k.shape != want or v.shape != want:
-            raise ValueError(f"k and v must be {want}, got {tuple(k.shape)} and {tuple(v.shape)}")
-        kt, kh, k1 = k.stride()
-        vt, vh, v1 = v.stride()
-        if (k1 != 1 or v1 != 1) and self.dim > 1:
-            raise ValueError("dim must be contiguous in k and v")
-        _ints("slots", slots, (tokens,))
-        status = self._store(self._ref, tokens, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, slots.data_ptr(),
-                             _stream_of(stream, self._index))
-        if status:
-            raise gba.GbaError(status, "gba_cache_store")
+        self._store(self._at, self._index, k, v, slots, _raw_stream(self._index) if stream is None else stream.cuda_stream)
 
 
 # Scratch of calls with workspace="auto", one per (device, stream): calls in a
@@ -278,26 +216,15 @@ _scratch = {}
 _retired = []
 
 
-def _scratch_for(nbytes, device, stream):
-    key = (device.index, gba._stream_handle(stream, device))
-    ws = _scratch.get(key)
-    if ws is None or ws.numel() < nbytes:
-        if gba.stream_capturing(torch.cuda.current_stream(device) if stream is None else stream):
-            raise RuntimeError(f"workspace='auto' would allocate {nbytes} bytes while the stream is being captured into a "
-                               "graph; pass a uint8 CUDA tensor of at least that size as `workspace`, or make one call "
-                               "before the capture")
-        if ws is not None:
-            _retired.append(ws)
-        ws = _empty(max(nbytes, 1 << 20), torch.uint8, device, stream)
-        _scratch[key] = ws
-    return ws
-
-
-def attention_workspace_size(desc):
-    """Bytes of workspace a filled AttentionDesc would use to split long requests."""
-    n = ctypes.c_size_t(0)
-    gba._check(gba.lib().gba_tree_attention_workspace_size(ctypes.byref(desc), ctypes.byref(n)), "gba_tree_attention_workspace_size")
-    return n.value
+def _more_scratch(nbytes, device, key):
+    """A larger scratch buffer of the current stream."""
+    if torch.cuda.is_current_stream_capturing():
+        raise RuntimeError(f"workspace='auto' would allocate {nbytes} bytes while the stream is being captured into a graph; "
+                           "pass a uint8 CUDA tensor of at least that size as `workspace`, or make one call before the capture")
+    if key in _scratch:
+        _retired.append(_scratch[key])
+    _scratch[key] = torch.empty(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
+    return _scratch[key]
 
 
 def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=None, out=None, workspace="auto", stream=None):
@@ -313,38 +240,17 @@ def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=
     stream), None (long requests are not split) or a uint8 CUDA tensor.
     Rows of padded tokens are not written.
     """
-    dtype = cache.dtype
-    tokens, heads, dim = q.shape
-    requests, width = table.shape
-    for name, t in (("q", q), ("out", out)):
-        if t is not None and (t.dtype is not dtype or not t.is_cuda):
-            raise TypeError(f"{name} must be a CUDA tensor of the cache's dtype, {dtype}")
-    if dim != cache.dim or heads % max(cache.heads, 1) != 0:
-        raise ValueError(f"q must be (tokens, a multiple of {cache.heads}, {cache.dim}), got {tuple(q.shape)}")
-    _ints("table", table, (requests, width))
-    _ints("lens", lens, (requests,))
-    _ints("offsets", offsets, (requests + 1,))
-    if mask is not None:
-        if mask.dtype is not torch.int64 or not mask.is_cuda:
-            raise TypeError("mask must be an int64 CUDA tensor")
-        if mask.numel() != tokens or not mask.is_contiguous():
-            raise ValueError("mask must be one contiguous word for each token")
-    if out is None:
-        out = _empty((tokens, heads, dim), dtype, q.device, stream)
-    elif out.shape != q.shape:
-        raise ValueError("out must have the shape of q")
-    if dim > 1 and (q.stride(2) != 1 or out.stride(2) != 1):
-        raise ValueError("dim must be contiguous in q and out")
-    qs, os = q.stride(), out.stride()
-    d = gba.AttentionDesc(cache._desc, requests, width, tokens, max_new, heads, 1.0 / math.sqrt(dim) if scale is None else scale,
-                          q.data_ptr(), qs[0], qs[1], out.data_ptr(), os[0], os[1], table.data_ptr(), lens.data_ptr(),
-                          offsets.data_ptr(), None if mask is None else mask.data_ptr(), None, 0)
-    if workspace is not None:
-        need = attention_workspace_size(d)
-        if need > 0:
-            ws = _scratch_for(need, q.device, stream) if isinstance(workspace, str) else workspace
-            if ws.dtype is not torch.uint8 or not ws.is_cuda:
-                raise TypeError("workspace must be a uint8 CUDA tensor")
-            d.workspace, d.workspace_bytes = ws.data_ptr(), ws.numel()
-    gba._check(gba.lib().gba_tree_attention(ctypes.byref(d), gba._stream_handle(stream, q.device)), "gba_tree_attention")
-    return out
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return tree_attention(q, cache, table, lens, offsets, max_new=max_new, mask=mask, scale=scale, out=out, workspace=workspace)
+    index = cache._index
+    raw = _raw_stream(index)
+    auto = isinstance(workspace, str)
+    ws = _scratch.get((index, raw)) if auto else workspace
+    if scale is None:
+        scale = cache._scale
+    got = cache._attend(cache._at, index, q, table, lens, offsets, max_new, mask, scale, out, ws, auto, raw)
+    if type(got) is int:  # the bytes that it needs
+        ws = _more_scratch(got, cache.device, (index, raw))
+        got = cache._attend(cache._at, index, q, table, lens, offsets, max_new, mask, scale, out, ws, False, raw)
+    return got
