@@ -90,10 +90,10 @@ __device__ __forceinline__ void q4_store(const Q4Args &p, const f4 (&acc)[MT][NT
     }
 }
 
-// Up to 16 rows.  STEPS: 32-deep steps of a group.  AHEAD: chunks held in
-// registers.
-template <class T, int NT, int STEPS, bool ZEROS, int AHEAD>
-__global__ void __launch_bounds__(64 * WAVES) q4_kernel(Q4Args p)
+// Up to 16 rows.  STEPS: 32-deep steps of a group.  W: waves.  AHEAD: chunks
+// that each holds in registers.
+template <class T, int NT, int STEPS, bool ZEROS, int W, int AHEAD>
+__global__ void __launch_bounds__(64 * W) q4_kernel(Q4Args p)
 {
     constexpr int MT = 1;
     typedef typename T::elem elem;
@@ -101,7 +101,7 @@ __global__ void __launch_bounds__(64 * WAVES) q4_kernel(Q4Args p)
     constexpr int GROUPS = 4 / STEPS;              // of a chunk
     constexpr int ROWS = 16 * MT, LOADS = ROWS / 4;  // a load: four rows of 256 bytes
     constexpr int CORNER = ROWS * 256, PART = MT * NT * 1024;
-    __shared__ __attribute__((aligned(16))) char smem[WAVES * (CORNER > PART ? CORNER : PART)];
+    __shared__ __attribute__((aligned(16))) char smem[W * (CORNER > PART ? CORNER : PART)];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
     const int nb0 = blockIdx.x * NT, row0 = blockIdx.y * ROWS;
     char *corner = smem + wave * CORNER;
@@ -181,18 +181,18 @@ __global__ void __launch_bounds__(64 * WAVES) q4_kernel(Q4Args p)
 
 #pragma unroll
     for (int d = 0; d < AHEAD; ++d)
-        if (wave + WAVES * d < p.KB) load(d, wave + WAVES * d);
-    for (int kb = wave; kb < p.KB; kb += WAVES * AHEAD) {
+        if (wave + W * d < p.KB) load(d, wave + W * d);
+    for (int kb = wave; kb < p.KB; kb += W * AHEAD) {
 #pragma unroll
         for (int d = 0; d < AHEAD; ++d) {
-            const int at = kb + WAVES * d;
+            const int at = kb + W * d;
             if (at < p.KB) use(d);
-            if (at + WAVES * AHEAD < p.KB) load(d, at + WAVES * AHEAD);
+            if (at + W * AHEAD < p.KB) load(d, at + W * AHEAD);
         }
     }
 
     __syncthreads();
-    q4_store<T, MT, NT, WAVES>(p, acc, smem, row0, nb0);
+    q4_store<T, MT, NT, W>(p, acc, smem, row0, nb0);
 }
 
 // 16 MT rows, MT 2 or 4, of which a wave could not hold the next chunks in
@@ -357,25 +357,30 @@ __global__ void __launch_bounds__(64 * WAVES) q4_rows_kernel(Q4Args p)
 }
 
 template <class T, int MT, int NT, bool DIRECT>
-gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
+gba_status run_rows(const Q4Args &a, int group, hipStream_t s)
 {
     const dim3 grid((unsigned)div_up(a.NB, NT), (unsigned)div_up(a.M, 16 * MT)), block(64 * WAVES);
     const bool z = a.zeros != nullptr;
-    if constexpr (MT == 1) {
-        // one chunk of four column blocks or two of fewer: more waves fit with
-        // fewer registers (1 x 8192 x 32768: 28.5 us against 32.2 with twice
-        // as many chunks ahead)
-        constexpr int AHEAD = NT == 4 ? 1 : 2;
-        if (group == 32) return z ? launch(q4_kernel<T, NT, 1, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 1, false, AHEAD>, grid, block, s, a);
-        if (group == 64) return z ? launch(q4_kernel<T, NT, 2, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 2, false, AHEAD>, grid, block, s, a);
-        return z ? launch(q4_kernel<T, NT, 4, true, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 4, false, AHEAD>, grid, block, s, a);
-    } else {
+    // groups of 32 and two column blocks of 64 rows need more registers than
+    // there are (64 x 8192 x 8192: 75 us against 41 on one)
+    if constexpr (MT * NT < 8)
         if (group == 32)
             return z ? launch(q4_rows_kernel<T, MT, NT, 1, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 1, false, DIRECT>, grid, block, s, a);
-        if (group == 64)
-            return z ? launch(q4_rows_kernel<T, MT, NT, 2, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 2, false, DIRECT>, grid, block, s, a);
-        return z ? launch(q4_rows_kernel<T, MT, NT, 4, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 4, false, DIRECT>, grid, block, s, a);
-    }
+    if (group == 64)
+        return z ? launch(q4_rows_kernel<T, MT, NT, 2, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 2, false, DIRECT>, grid, block, s, a);
+    return z ? launch(q4_rows_kernel<T, MT, NT, 4, true, DIRECT>, grid, block, s, a) : launch(q4_rows_kernel<T, MT, NT, 4, false, DIRECT>, grid, block, s, a);
+}
+
+template <class T, int NT, int W, int AHEAD>
+gba_status run_few(const Q4Args &a, int group, hipStream_t s)
+{
+    const dim3 grid((unsigned)div_up(a.NB, NT)), block(64 * W);
+    const bool z = a.zeros != nullptr;
+    // groups of 32, two column blocks: more than the 128 registers of 16 waves
+    if constexpr (NT != 2 || W != 16)
+        if (group == 32) return z ? launch(q4_kernel<T, NT, 1, true, W, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 1, false, W, AHEAD>, grid, block, s, a);
+    if (group == 64) return z ? launch(q4_kernel<T, NT, 2, true, W, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 2, false, W, AHEAD>, grid, block, s, a);
+    return z ? launch(q4_kernel<T, NT, 4, true, W, AHEAD>, grid, block, s, a) : launch(q4_kernel<T, NT, 4, false, W, AHEAD>, grid, block, s, a);
 }
 
 // Which kernel: one 16-row block with its chunks in registers up to 16 rows,
@@ -386,15 +391,20 @@ template <class T>
 gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
 {
     if (a.M <= 16) {
-        if (a.NB >= 1024) return run_q4<T, 1, 4, true>(a, group, s);
-        return a.NB >= 512 ? run_q4<T, 1, 2, true>(a, group, s) : run_q4<T, 1, 1, true>(a, group, s);
+        // One chunk ahead on four column blocks, two on fewer: more waves fit
+        // with fewer registers (1 x 8192 x 32768: 28.5 us against 32.2 with
+        // twice as many ahead).  16 waves with one ahead where each has a
+        // chunk: 1 x 8192 x 8192 9.4 us against 10.6 with 8, 16 x 8192 x 1024
+        // 6.9 against 8.2; half of them idle, 1024 x 32768 12.1 against 7.7.
+        if (a.NB >= 1024) return run_few<T, 4, WAVES, 1>(a, group, s);
+        if (a.KB >= 16 && a.NB < 512) return run_few<T, 1, 16, 1>(a, group, s);
+        if (a.KB >= 16 && group != 32) return run_few<T, 2, 16, 1>(a, group, s);
+        return a.NB >= 512 ? run_few<T, 2, WAVES, 2>(a, group, s) : run_few<T, 1, WAVES, 2>(a, group, s);
     }
     const bool direct = a.lda % 8 == 0 && a.K % 8 == 0 && a.lda < (1 << 23) && aligned_to(a.A, 16);
-    if (!direct) return a.M <= 32 ? run_q4<T, 2, 1, false>(a, group, s) : run_q4<T, 4, 1, false>(a, group, s);
-    // groups of 32 and two column blocks need more registers than there are
-    // (64 x 8192 x 8192: 75 us against 41)
-    if (a.NB >= 512 && (a.M <= 32 || group != 32)) return a.M <= 32 ? run_q4<T, 2, 2, true>(a, group, s) : run_q4<T, 4, 2, true>(a, group, s);
-    return a.M <= 32 ? run_q4<T, 2, 1, true>(a, group, s) : run_q4<T, 4, 1, true>(a, group, s);
+    if (!direct) return a.M <= 32 ? run_rows<T, 2, 1, false>(a, group, s) : run_rows<T, 4, 1, false>(a, group, s);
+    if (a.NB >= 512 && (a.M <= 32 || group != 32)) return a.M <= 32 ? run_rows<T, 2, 2, true>(a, group, s) : run_rows<T, 4, 2, true>(a, group, s);
+    return a.M <= 32 ? run_rows<T, 2, 1, true>(a, group, s) : run_rows<T, 4, 1, true>(a, group, s);
 }
 
 // One thread a word.
@@ -444,7 +454,7 @@ extern "C" gba_status gba_q4_linear(const gba_q4_weight *w, int64_t M, const voi
         !aligned_to(bias, 2) || !aligned_to(C, 2))
         return GBA_EUNSUPPORTED;
     // the launch runtime takes grids of less than 2^32 threads a dimension
-    if (div_up(N, 16) > (int64_t)UINT_MAX / (64 * WAVES)) return GBA_EUNSUPPORTED;
+    if (div_up(N, 16) > (int64_t)UINT_MAX / 1024) return GBA_EUNSUPPORTED;
     Q4Args a;
     a.codes = static_cast<const u4 *>(w->codes);
     a.scales = w->scales;

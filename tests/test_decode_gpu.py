@@ -64,6 +64,26 @@ def test_linear_whole_numbers(group, zeros, dtype):
             assert torch.equal(got.cpu(), D.activated(want, act).to(dtype)), (M, K, N, act)
 
 
+# Every way a request may run: 1, 2 and 4 column blocks a workgroup (from 512 and
+# 1024 of them on), 8 and 16 waves (from 16 chunks of K on), 16, 32 and 64 rows,
+# rows that are copied straight to LDS and rows that are not.
+WAYS = [(3, 300, 1000), (3, 2100, 1000), (2, 300, 8200), (2, 2100, 8200), (2, 140, 16400), (2, 2100, 16400), (20, 520, 100), (20, 520, 8200),
+        (50, 520, 100), (50, 520, 8200), (20, 519, 8200), (50, 519, 100)]
+
+
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("way", range(len(WAYS)))
+def test_linear_every_way(way, group, zeros):
+    M, K, N = WAYS[way]
+    announce("linear way", M, K, N, group, zeros)
+    g = torch.Generator().manual_seed(way)
+    w, ref = weight(g, K, N, group, (HALF, BF16)[way % 2], zeros, True)
+    x = torch.randint(-3, 4, (M, K), generator=g).to(w.dtype)
+    want = (x.double().cuda() @ ref.cuda()).to(w.dtype)
+    assert torch.equal(decode.q4_linear(x.cuda(), w), want)
+
+
 @pytest.mark.parametrize("act", ["none", "relu", "sigmoid", "tanh"])
 @pytest.mark.parametrize("dtype", [HALF, BF16], ids=["f16", "bf16"])
 def test_linear_rounding(dtype, act):
