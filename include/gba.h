@@ -576,9 +576,11 @@ typedef struct gba_attention {
  * past max_new.
  *
  * Workspace: with at least gba_tree_attention_workspace_size bytes, 256-byte
- * aligned, long requests are split across workgroups and joined by a second
- * kernel; with less each request and head is one workgroup's work.  It need
- * not be cleared, and calls that may overlap need separate ones.
+ * aligned, long requests are split across workgroups and their parts joined;
+ * with less each request and head is one workgroup's work.  Its first 256 KB
+ * hold counters: zero-filled before its first use, they are zeros again when a
+ * call completes, whatever its sizes.  Calls that may overlap need separate
+ * ones.
  *
  * dim a multiple of 8 up to 256; q, out, K and V 16-byte aligned with strides
  * that are multiples of 8 (out: 4).

@@ -19,8 +19,9 @@
 // straight into its own part of LDS, one tile ahead, and waits for nothing but
 // its own copies; the waves of a workgroup take the tiles of a run of keys in
 // turn and meet once, at its end.  Runs are cut to one length for all
-// requests, from the sum of their lengths, which every wave reads for itself;
-// the runs of one request are joined by a second kernel.
+// requests, from the sum of their lengths, which every wave reads for itself.
+// The runs of one request are joined in their order, by a second kernel, or,
+// where there are few of them, by the workgroup that ends last.
 #include "gba_decode.hpp"
 #include "gba_kernel.hpp"
 
@@ -39,6 +40,7 @@ struct AttentionArgs {
     int row_tiles;     // of a request and head
     int slots;         // runs of keys there is room for: at least as many as there are
     int target;        // runs to aim at (0: one for each request)
+    int32_t *arrived;    // [slots][heads][row_tiles], zeros: runs that have ended, at a request's first one; or null
     int32_t *first_run;  // [requests][2]: a request's first run and how many it has
     float *part;       // [slots][heads][row_tiles]: rows x dim sums, then as many maxima and sums of weights
 };
@@ -101,6 +103,7 @@ __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirs
 // with number `first`; r = -1 where there is no such run.
 struct Run {
     int r, n, first, from, to;
+    Request q;
 };
 
 // Every run but a request's last is of one length, a multiple of `step`:
@@ -112,11 +115,12 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
     Run u;
     if (p.target == 0) {
         const Request q = request_of(p, x);
-        u.r = uniform(q.fresh) > 0 ? x : -1;
+        u.q = {uniform(q.first), uniform(q.fresh), uniform(q.kept), uniform(q.end)};
+        u.r = u.q.fresh > 0 ? x : -1;
         u.n = 1;
         u.first = x;
         u.from = 0;
-        u.to = uniform(q.end);
+        u.to = u.q.end;
         return u;
     }
     float keys = 0.f;
@@ -145,8 +149,9 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
             u.n = __builtin_amdgcn_readlane(n, l);
             u.first = before + __builtin_amdgcn_readlane(upto, l) - u.n;
             u.from = (x - u.first) * length;
-            const int end = __builtin_amdgcn_readlane(q.end, l);
-            u.to = end - u.from > length ? u.from + length : end;
+            u.q = {__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.fresh, l), __builtin_amdgcn_readlane(q.kept, l),
+                   __builtin_amdgcn_readlane(q.end, l)};
+            u.to = u.q.end - u.from > length ? u.from + length : u.q.end;
             return u;
         }
         before += __builtin_amdgcn_readlane(upto, 63);
@@ -277,12 +282,9 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     if (x >= p.slots) return;
     const Run run = run_of(p, x, lane, KEYS * KG);
     if (run.r < 0) return;
-    Request rq = request_of(p, run.r);
-    rq.first = uniform(rq.first);
-    rq.fresh = uniform(rq.fresh);
-    rq.kept = uniform(rq.kept);
+    const Request rq = run.q;
     const int rows = rq.fresh * p.share, row0 = row_tile * ROWS;
-    if (p.target != 0 && run.first == x && head == 0 && row_tile == 0 && threadIdx.x == 0) {
+    if (p.target != 0 && p.arrived == nullptr && run.first == x && head == 0 && row_tile == 0 && threadIdx.x == 0) {
         p.first_run[2 * run.r] = x;
         p.first_run[2 * run.r + 1] = run.n;
     }
@@ -706,6 +708,62 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             }
         }
     }
+    if constexpr (RG <= 2) {
+        if (whole_request || p.arrived == nullptr) return;
+        // Every wave's stores are done at the barrier; one thread's release
+        // makes them visible to other XCDs before it counts the run, and who
+        // counts the last one acquires those of all others.
+        __shared__ int last;
+        wait_vm_lgkm0<0>();
+        __syncthreads();
+        const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
+        if (threadIdx.x == 0) {
+            last = __hip_atomic_fetch_add(p.arrived + place, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
+            if (last) __hip_atomic_store(p.arrived + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+        __syncthreads();
+        if (!last) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
+        const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
+        for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * WAVES) {
+            const int row = j / FOURS, d = 4 * (j % FOURS);
+            if (row0 + row >= rows || d >= p.dim) continue;
+            const float *sum_at = first_part + row * p.dim + d, *top_at = first_part + ROWS * p.dim + row, *l_at = top_at + ROWS;
+            float m = -INFINITY, l = 0.f;
+            f4 o = {0.f, 0.f, 0.f, 0.f};
+            for (int i = 0; i < run.n; i += 4) {
+                f4 v[4];
+                float t[4], w[4], next = m;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int64_t at = (i + u < run.n ? i + u : i) * stride;
+                    v[u] = *reinterpret_cast<const f4 *>(sum_at + at);
+                    t[u] = i + u < run.n ? top_at[at] : -INFINITY;
+                    w[u] = l_at[at];
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) next = fmaxf(next, t[u]);
+                if (next == -INFINITY) continue;
+                const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+                l *= keep;
+                o *= keep;
+                m = next;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float share = t[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t[u] - next);
+                    l += share * w[u];
+                    o += share * v[u];
+                }
+            }
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
+            four_t r4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+            *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r4;
+        }
+    }
 }
 
 // The runs of a request, added in their order; one wave a token and query
@@ -808,8 +866,18 @@ gba_status validate(const gba_attention &d)
 struct Shape {
     bool whole;
     int dp, rt, rg, row_tiles, target, slots;
-    size_t header, bytes;  // of the workspace
+    bool counts;           // runs are joined by the workgroup that ends last
+    size_t header, bytes;  // of the workspace: what stands before the sums, all
 };
+
+// A workgroup's release writes back its XCD's L2: that costs less than the
+// second kernel while there are few (one request of 1000 keys: 9.3 us against
+// 10.8, two: 9.8 and 10.9), and more from about a hundred on (16 trees of 8 over
+// 1000 keys: 19.9 us against 16.3; 64 requests of up to 8192: 94 and 81).
+constexpr int FEW_RUNS = 64;
+
+// The workspace begins with the counters, zeros whatever calls used it before.
+constexpr size_t COUNTERS = 65536, COUNTER_BYTES = COUNTERS * sizeof(int32_t);
 
 // Runs to aim at.  A compute unit has room for one workgroup (two of dim 64),
 // and each request and head adds half a run on average, its last one.  Few
@@ -842,11 +910,14 @@ Shape shape_of(const gba_attention &d)
     s.row_tiles = (int)div_up(rows, 16 * s.rt * s.rg);
     s.target = 0;
     s.slots = (int)d.requests;
+    s.counts = false;
     s.header = s.bytes = 0;
     if (d.requests <= SPLIT_REQUESTS && d.width * c.block_size > SHORTEST) {
         s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
-        s.header = (size_t)div_up(d.requests * 8, 256) * 256;
+        s.counts = s.rg <= 2 && d.requests * c.heads * s.row_tiles * div_up(d.width * c.block_size, SHORTEST) <= FEW_RUNS &&
+                   (size_t)s.slots * c.heads * s.row_tiles <= COUNTERS;
+        s.header = COUNTER_BYTES + (size_t)div_up(d.requests * 8, 256) * 256;
         s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt * s.rg) * (c.dim + 2) * sizeof(float);
     }
     return s;
@@ -859,7 +930,7 @@ gba_status run_attention(const AttentionArgs &a, hipStream_t s)
     constexpr int threads = threads_of<DP, RG>();
     if (groups > (int64_t)UINT_MAX / threads || div_up((int64_t)a.tokens * a.q_heads, 4) > (int64_t)UINT_MAX / 256) return GBA_EUNSUPPORTED;
     const gba_status st = launch(attention_kernel<T, DP, RT, RG, WHOLE>, dim3((unsigned)groups), dim3(threads), s, a);
-    if (st != GBA_OK || a.target == 0) return st;
+    if (st != GBA_OK || a.target == 0 || a.arrived != nullptr) return st;
     return launch(join_kernel<T, DP>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, 16 * RT * RG);
 }
 
@@ -917,6 +988,7 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     if (sh.target != 0 && (d.workspace == nullptr || d.workspace_bytes < sh.bytes)) {
         sh.target = 0;
         sh.slots = (int)d.requests;
+        sh.counts = false;
     }
     AttentionArgs a;
     a.q = d.q;
@@ -953,7 +1025,8 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     a.row_tiles = sh.row_tiles;
     a.slots = sh.slots;
     a.target = sh.target;
-    a.first_run = static_cast<int32_t *>(d.workspace);
+    a.arrived = sh.counts ? static_cast<int32_t *>(d.workspace) : nullptr;
+    a.first_run = sh.target != 0 ? reinterpret_cast<int32_t *>(static_cast<char *>(d.workspace) + COUNTER_BYTES) : nullptr;
     a.part = sh.target != 0 ? reinterpret_cast<float *>(static_cast<char *>(d.workspace) + sh.header) : nullptr;
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return c.dtype == GBA_F16 ? run_attention<F16>(a, sh, s) : run_attention<BF16>(a, sh, s);

@@ -217,13 +217,14 @@ _retired = []
 
 
 def _more_scratch(nbytes, device, key):
-    """A larger scratch buffer of the current stream."""
+    """A larger scratch buffer of the current stream, zeros."""
     if torch.cuda.is_current_stream_capturing():
         raise RuntimeError(f"workspace='auto' would allocate {nbytes} bytes while the stream is being captured into a graph; "
-                           "pass a uint8 CUDA tensor of at least that size as `workspace`, or make one call before the capture")
+                           "pass a zero-filled uint8 CUDA tensor of at least that size as `workspace`, or make one call "
+                           "before the capture")
     if key in _scratch:
         _retired.append(_scratch[key])
-    _scratch[key] = torch.empty(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
+    _scratch[key] = torch.zeros(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
     return _scratch[key]
 
 
@@ -237,7 +238,8 @@ def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=
     tokens.  mask: int64 (tokens, 1) or (tokens,), which of its request's new
     tokens each one sees (a StepMaps'); None: those up to itself.  scale:
     1 / sqrt(dim) by default.  workspace: "auto" (a scratch buffer of this
-    stream), None (long requests are not split) or a uint8 CUDA tensor.
+    stream), None (long requests are not split) or a uint8 CUDA tensor, zeros before
+    its first use.
     Rows of padded tokens are not written.
     """
     if stream is not None:

@@ -430,14 +430,15 @@ def test_attention_on_another_stream_and_in_a_graph():
     there = decode.tree_attention(*args, max_new=4, mask=mask, stream=side)
     side.synchronize()
     assert torch.equal(got, there)
-    out, ws = torch.empty_like(got), torch.empty(64 << 20, dtype=torch.uint8, device="cuda")
+    out, ws = torch.empty_like(got), torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.graph(graph):
         decode.tree_attention(*args, max_new=4, mask=mask, out=out, workspace=ws)
     for _ in range(3):
         out.zero_()
-        ws.fill_(255)
+        ws[1 << 18:].fill_(255)  # all but the counters
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(out, got)
+        assert not ws[: 1 << 18].any()
     D.check_attention(out, ref, spread, BF16)
