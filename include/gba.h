@@ -570,8 +570,9 @@ typedef struct gba_attention {
  * and zeros where it sees none.  The weights exp(s_p - m) are rounded to the
  * cache's dtype for the second product, as its matrix instructions take them,
  * and their sum is that of the rounded ones.
- * What the cache holds at other positions is never used, whatever it is (a
- * position whose block is outside the cache counts as not seen).  Rows of out
+ * What the cache holds at positions that a token does not see has no effect
+ * on its rows, infinities and NaN included (a position whose block is outside
+ * the cache counts as not seen).  Rows of out
  * that belong to no request are not written; neither are those of a request
  * past max_new.
  *

@@ -13,13 +13,15 @@ namespace gba {
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
-// fp16 and bf16: the matrix instruction, and the bits of 16 + q for a code q
-// (the code in the top bits of the fraction: no conversion is needed).
+// fp16 and bf16: the matrix instruction, the bits of 16 + q for a code q (the
+// code in the top bits of the fraction: no conversion is needed), and
+// those of infinity and of the exponent's lowest bit, all twice.
 struct F16 {
     typedef _Float16 elem;
     typedef h8 vec8;
     static constexpr unsigned SIXTEEN = 0x4C004C00u;  // 16.0 twice
     static constexpr int TOP = 6;                     // lowest bit of the four fraction bits that hold a code
+    static constexpr unsigned INFINITE = 0x7C007C00u, EXPONENT_ONE = 0x04000400u;
     static __device__ __forceinline__ f4 mfma(vec8 a, vec8 b, f4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -30,6 +32,7 @@ struct BF16 {
     typedef b8 vec8;
     static constexpr unsigned SIXTEEN = 0x41804180u;
     static constexpr int TOP = 3;
+    static constexpr unsigned INFINITE = 0x7F807F80u, EXPONENT_ONE = 0x00800080u;
     static __device__ __forceinline__ f4 mfma(vec8 a, vec8 b, f4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

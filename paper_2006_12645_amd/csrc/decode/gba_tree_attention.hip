@@ -226,6 +226,14 @@ __device__ __forceinline__ void read_transposed(const unsigned *at, u4 (&v)[4])
     for (int i = 0; i < 4; ++i) v[i] = u4{r[2 * i][0], r[2 * i][1], r[2 * i + 1][0], r[2 * i + 1][1]};
 }
 
+// Two 16-bit floats: 0x8000 for each that is infinite or NaN (the exponent's top
+// carries into the sign's place).
+template <class T>
+__device__ __forceinline__ unsigned not_finite(unsigned w)
+{
+    return ((w & T::INFINITE) + T::EXPONENT_ONE) & 0x80008000u;
+}
+
 template <int N>
 struct Const {
     static constexpr int value = N;
@@ -272,6 +280,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = 16 * RT * RG;
     __shared__ __attribute__((aligned(16))) char smem[lds_bytes<DP, RT, RG>()];
     __shared__ float tops[WAVES][16 * RT], sums[WAVES][16 * RT];
+    __shared__ int odd_from[RG > 1 ? KG : WAVES];  // first key of the first tile whose V has been cleaned
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), rg = wave % RG, kg = wave / RG;
     const int c = lane & 15, g = lane >> 4;
@@ -409,6 +418,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         return there;
     };
     if (rounds > 0) look_up(0);
+    if (lane == 0 && (RG == 1 || rg == 0)) odd_from[RG > 1 ? kg : wave] = INT_MAX;  // (before the first meeting)
 
     // ---- this wave's rows: as the second operand, row c of each block; dim
     // 32 s + 8 g on
@@ -487,15 +497,22 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             four(Const<12>{});
         }
     };
-    // The weights of tile n, of which the keys in `there` exist.
-    auto soften = [&](int n, unsigned there) {
+    // The weights of tile n, of which the keys in `there` exist; whether a row
+    // does not see one of those.
+    auto soften = [&](int n, unsigned there) -> bool {
+        bool unseen = false;
         const int first_draft = key0(n) - rq.kept;  // of the new tokens, or below 0
         if (there != 0xFFFFFFFFu || first_draft + KEYS > 0) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                const unsigned seen = (there & seen_of(masked, sees[i], index[i], first_draft)) >> (4 * g);
+                const unsigned all = there & seen_of(masked, sees[i], index[i], first_draft), seen = all >> (4 * g);
+                unseen |= all != there;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) score[i][e >> 2][e & 3] = (seen >> (16 * (e >> 2) + (e & 3))) & 1 ? score[i][e >> 2][e & 3] : -INFINITY;
+                for (int e = 0; e < 8; ++e) {  // (as bits: a score that is left out may be NaN)
+                    const float is = score[i][e >> 2][e & 3];
+                    const unsigned bits = (seen >> (16 * (e >> 2) + (e & 3))) & 1 ? __builtin_bit_cast(unsigned, is) : 0xFF800000u;
+                    score[i][e >> 2][e & 3] = __builtin_bit_cast(float, bits);
+                }
             }
         }
         float most[RT];
@@ -529,6 +546,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
                 weight[i][e] = (elem)__builtin_amdgcn_exp2f(__builtin_fmaf(score[i][e >> 2][e & 3], p.scale2, -base2[i]));
             weights[i] = T::mfma(ones, weight[i], weights[i]);
         }
+        return __ballot(unseen) != 0;
     };
     auto multiply_v = [&](auto off, unsigned slot) {
 #pragma unroll
@@ -541,6 +559,29 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
 #pragma unroll
                 for (int i = 0; i < RT; ++i) out[i][b + j] = T::mfma(__builtin_bit_cast(vec8, v[j]), weight[i], out[i][b + j]);
         }
+    };
+    // Where a row does not see a key that is there, 0 times what V holds has to
+    // be 0, whatever that is: what is not finite is taken out of such a tile in
+    // LDS, and added at the end to the rows that see it.  The `copies` of
+    // tiles from n on from number `first` on.  Waves that share tiles share this, in
+    // every stage with new tokens.
+    auto clean = [&](int n, unsigned slot, int first, int copies) {
+        for (int i = first; i < first + copies; ++i) {
+            u4 *v = reinterpret_cast<u4 *>(mine + slot + i / COPIES * S::PAIR + TILE + 1024 * (i % COPIES) + 16 * lane);
+            u4 x = *v;
+            unsigned odd = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const unsigned bits = not_finite<T>(x[e]);
+                odd |= bits;
+                x[e] &= ~((bits << 1) - (bits >> 15));
+            }
+            if (odd != 0) {
+                *v = x;
+                atomicMin(&odd_from[RG > 1 ? kg : wave], key0(n + i / COPIES));
+            }
+        }
+        lanes_meet();
     };
 
     if constexpr (WHOLE && RG == 1) {
@@ -564,9 +605,10 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             if (n + 2 - entries_from == 32) look_up(n + 2);
             const unsigned after = keys_of(n + 2);
             copy(n + 2, 0);
-            soften(n, now);
+            const bool unseen = soften(n, now);
             wait_vm_lgkm0<3 * COPIES>();
             lanes_meet();
+            if (unseen) clean(n, slot, 0, COPIES);
             multiply_v(Const<0>{}, slot);
             copy(n + 2, 1);
             now = next;
@@ -590,9 +632,14 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             for (int j = 0; j < SUB; ++j) now[j] = ahead[j];
             wait_vm_lgkm0<0>();
             __builtin_amdgcn_s_barrier();  // every wave's share is there, and the other stage has been read
+            const unsigned slot = (round & 1) * (SUB * S::PAIR);
+            if (run.from + (int64_t)(KEYS * KG * SUB) * (round + 1) > rq.kept) {
+                clean(round * SUB, slot, SUB * COPIES / RG * rg, SUB * COPIES / RG);
+                wait_vm_lgkm0<0>();
+                __builtin_amdgcn_s_barrier();
+            }
             stage((round + 1) * SUB);
             lanes_meet();
-            const unsigned slot = (round & 1) * (SUB * S::PAIR);
             auto tile = [&](auto j) {
                 constexpr int J = decltype(j)::value;
                 if (now[J] != 0) {
@@ -621,16 +668,36 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             if (n + 1 < count) next = fetch(n + 1);
             lanes_meet();
             multiply_k(Const<0>{}, 0);
-            soften(n, now);
+            const bool unseen = soften(n, now);
+            if (unseen) clean(n, 0, 0, COPIES);
             multiply_v(Const<0>{}, 0);
         }
     }
+
+    wait_vm_lgkm0<0>();
+    if (RG > 1) __syncthreads();  // no copies are under way, and the tiles have been read
+
+    // What has been taken out of V from key `from` on, for elements d .. d + 3
+    // of a row.
+    auto odd_at = [&](int from, int row, int d) {
+        f4 o = {0.f, 0.f, 0.f, 0.f};
+        const int own = row / p.share;
+        const uint64_t bits = masked ? p.mask[rq.first + own] : 0;
+        for (int pos = from; pos < run.to; ++pos) {
+            const int page = pos / p.block_size, block = entries[page], draft = pos - rq.kept;
+            if (block < 0 || block >= p.num_blocks || (draft >= 0 && !(masked ? draft < 64 && (bits >> draft & 1) : draft <= own))) continue;
+            const uint16_t *v = reinterpret_cast<const uint16_t *>(v_head) + block * p.v_block + (pos - page * p.block_size) * p.v_token + d;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (not_finite<T>(v[e]) != 0) o[e] += (float)__builtin_bit_cast(elem, v[e]);
+        }
+        return o;
+    };
 
     const bool whole_request = run.n == 1;
     typedef elem four_t __attribute__((ext_vector_type(4)));
     float *part = whole_request ? nullptr : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * ROWS * (int64_t)(p.dim + 2);
     if constexpr (KG == 1) {  // one key group: the sums are these
-        wait_vm_lgkm0<0>();
 #pragma unroll
         for (int i = 0; i < RT; ++i) {
             const int row = wave_row0 + 16 * i + c;
@@ -656,13 +723,23 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
                 part[ROWS * (p.dim + 1) + row - row0] = l;
             }
         }
+        const int odd = uniform(odd_from[0]);
+        if (odd == INT_MAX) return;
+        for (int row = wave_row0 + c; row < rows && row < wave_row0 + 16 * RT; row += 16)
+            for (int d = 4 * g; d < p.dim; d += 16) {
+                const f4 more = odd_at(odd, row, d);
+                elem *to = static_cast<elem *>(p.out) + (int64_t)(rq.first + row / p.share) * p.out_token + (int64_t)(head * p.share + row % p.share) * p.out_head + d;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    if (whole_request) to[e] = (elem)((float)to[e] + more[e]);
+                    else part[(row - row0) * p.dim + d + e] += more[e];
+                }
+            }
         return;
     }
 
     // ---- the key groups' sums, joined through LDS: row c, chunks of four of
     // dim, chunk j of a row at j ^ c
-    wait_vm_lgkm0<0>();
-    if (RG > 1) __syncthreads();  // the tiles have been read
     lanes_meet();
     char *sums_of_wave = smem + wave * (16 * RT * 4 * DP);
     if (RG == 1) sums_of_wave = mine;
@@ -677,6 +754,10 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             *reinterpret_cast<f4 *>(sums_of_wave + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = out[i][b];
     }
     __syncthreads();
+    int odd = INT_MAX;
+#pragma unroll
+    for (int w = 0; w < (RG > 1 ? KG : WAVES); ++w) odd = min(odd, odd_from[w]);
+    odd = uniform(odd);
     constexpr int FOURS = DP / 4;
     for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * WAVES) {
         const int row = j / FOURS, four = j % FOURS, d = 4 * four, w0 = row / (16 * RT), r = row % (16 * RT);
@@ -693,6 +774,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             l += share * sums[from][r];
             o += share * *reinterpret_cast<const f4 *>(smem + (RG == 1 ? from * S::GROUP : from * (16 * RT * 4 * DP)) + r * (4 * DP) + 16 * (four ^ (r & 15)));
         }
+        if (odd != INT_MAX) o += odd_at(odd, row0 + row, d);
         if (whole_request) {
             const float inv = l > 0.f ? 1.f / l : 0.f;
             const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
