@@ -91,7 +91,9 @@ __device__ __forceinline__ void q4_store(const Q4Args &p, const f4 (&acc)[MT][NT
 }
 
 // Up to 16 rows.  STEPS: 32-deep steps of a group.  W: waves.  AHEAD: chunks
-// that each holds in registers.
+// that each holds in registers.  Bound by HBM for a large W: 1 x 8192 x 32768,
+// 139 MB, 28.5 to 30.8 us (4.5 to 4.9 TB/s); 1 x 8192 x 8192, 36 MB, 10.0 us (3.6);
+// 1 x 1024 x 1024 2.6 us, latency.
 template <class T, int NT, int STEPS, bool ZEROS, int W, int AHEAD>
 __global__ void __launch_bounds__(64 * W) q4_kernel(Q4Args p)
 {
@@ -200,7 +202,10 @@ __global__ void __launch_bounds__(64 * W) q4_kernel(Q4Args p)
 // straight to the wave's own part of LDS, AHEAD half chunks (16 MT rows of 64
 // k) before it is used; rows beyond M and k beyond K are read past the end of
 // a buffer, which gives zeros.  Else one half chunk ahead is in registers.
-// The codes, scales and zeros of the next two chunks stay in registers.
+// The codes, scales and zeros of the next two chunks stay in registers.  Bound by
+// instructions, about 430 a chunk and wave (48 of them matrix instructions), and
+// by all of A going through each compute unit: 64 x 8192 x 8192, groups of 64 with
+// zeros, 20.8 to 23.9 us (360 to 410 TFLOP/s, 1.7 to 1.9 TB/s).
 template <int MT, int NT, bool DIRECT>
 struct Q4Lds {
     static constexpr int AHEAD = MT == 4 || !DIRECT ? 1 : 3, SLOTS = DIRECT ? AHEAD + 1 : 1;
@@ -385,8 +390,10 @@ gba_status run_few(const Q4Args &a, int group, hipStream_t s)
 
 // Which kernel: one 16-row block with its chunks in registers up to 16 rows,
 // else blocks of 32 or 64 rows.  Column blocks of a workgroup: as many as
-// leave 256 workgroups (a workgroup reads all of its rows of A, so fewer,
-// wider ones read less).
+// leave 256 workgroups, since a workgroup reads all of its rows of A (1 x 8192 x
+// 8192: 10.0 us with two, 13.3 with one; 1 x 4096 x 4096 4.6 with one, 5.5 with two;
+// 64 x 8192 x 8192 23.9 with two, 35.5 with one; 32 x 4096 x 4096 7.6 with one, 8.6
+// with two).
 template <class T>
 gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
 {

@@ -16,7 +16,7 @@
 // instruction, of ones and the rounded weights.
 //
 // Few rows read a whole cache: the bound is HBM.  A wave copies its tiles
-// straight into its own part of LDS, one tile ahead, and waits for nothing but
+// straight into its own part of LDS, two tiles ahead, and waits for nothing but
 // its own copies; the waves of a workgroup take the tiles of a run of keys in
 // turn and meet once, at its end.  Runs are cut to one length for all
 // requests, from the sum of their lengths, which every wave reads for itself.
@@ -265,9 +265,55 @@ constexpr int threads_of()
     return 64 * Shared<DP, RG>::WAVES;
 }
 
+// Four elements of a row of `n` runs, added in their order.
+template <class T>
+__device__ __forceinline__ void join_runs(const float *sum_at, const float *top_at, const float *l_at, int64_t stride, int n, typename T::elem *to)
+{
+    typedef typename T::elem elem;
+    typedef elem four_t __attribute__((ext_vector_type(4)));
+    float m = -INFINITY, l = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; i += 4) {
+        f4 v[4];
+        float t[4], w[4], next = m;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int64_t at = (i + u < n ? i + u : i) * stride;
+            v[u] = *reinterpret_cast<const f4 *>(sum_at + at);
+            t[u] = i + u < n ? top_at[at] : -INFINITY;
+            w[u] = l_at[at];
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) next = fmaxf(next, t[u]);
+        if (next == -INFINITY) continue;
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+        l *= keep;
+        o *= keep;
+        m = next;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float share = t[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t[u] - next);
+            l += share * w[u];
+            o += share * v[u];
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    four_t r4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+    *reinterpret_cast<four_t *>(to) = r4;
+}
+
 // DP: dim, padded.  RT: blocks of 16 rows of a wave.  WHOLE: 16 consecutive
 // keys, from a multiple of 16 on, are in one block, and go straight to LDS;
 // else (RG 1 only) they pass through registers, which hold the next tile.
+//
+// RG 1 is bound by HBM: 64 requests of 16 to 8192 keys, 8 key heads of 128, 349
+// MB: 76 us (4.6 TB/s); two of 100000 to 131071, 16 of 64, 976 MB: 200 us
+// (4.9 TB/s); one of 1000 keys, bound by the latency of lengths, table, tiles and
+// join: 9.0 us.  RG 8 by a tile's instructions and LDS waits, about 2500 clocks
+// of which 1088 are matrix instructions: 16 trees of 64 tokens over 500 to 4096
+// keys, 8 key heads of 128 with four query heads each, 45 us (390 TFLOP/s).
 template <class T, int DP, int RT, int RG, bool WHOLE>
 __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) attention_kernel(AttentionArgs p)
 {
@@ -811,46 +857,53 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * WAVES) {
             const int row = j / FOURS, d = 4 * (j % FOURS);
             if (row0 + row >= rows || d >= p.dim) continue;
-            const float *sum_at = first_part + row * p.dim + d, *top_at = first_part + ROWS * p.dim + row, *l_at = top_at + ROWS;
-            float m = -INFINITY, l = 0.f;
-            f4 o = {0.f, 0.f, 0.f, 0.f};
-            for (int i = 0; i < run.n; i += 4) {
-                f4 v[4];
-                float t[4], w[4], next = m;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const int64_t at = (i + u < run.n ? i + u : i) * stride;
-                    v[u] = *reinterpret_cast<const f4 *>(sum_at + at);
-                    t[u] = i + u < run.n ? top_at[at] : -INFINITY;
-                    w[u] = l_at[at];
-                }
-#pragma unroll
-                for (int u = 0; u < 4; ++u) next = fmaxf(next, t[u]);
-                if (next == -INFINITY) continue;
-                const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
-                l *= keep;
-                o *= keep;
-                m = next;
-#pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float share = t[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t[u] - next);
-                    l += share * w[u];
-                    o += share * v[u];
-                }
-            }
-            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const float *top_at = first_part + ROWS * p.dim + row;
             const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
-            four_t r4;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
-            *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r4;
+            join_runs<T>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
+                         static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d);
         }
     }
 }
 
-// The runs of a request, added in their order; one wave a token and query
+// A token's request and its runs: false where there is nothing to join.
+__device__ __forceinline__ bool runs_of(const AttentionArgs &p, int t, int lane, int &x0, int &n, Request &rq)
+{
+    int r = 0;  // the number of requests that end at or before t
+    for (int base = 0; base < p.requests; base += 64)
+        r += __popcll(__ballot(base + lane < p.requests && p.offsets[base + lane + 1] <= t));
+    if (r >= p.requests) return false;
+    x0 = p.first_run[2 * r];
+    n = p.first_run[2 * r + 1];
+    rq = request_of(p, r);
+    return rq.fresh != 0 && t >= rq.first && n > 1;
+}
+
+// The runs of a request, added in their order: many rows, each of few runs; a
+// workgroup a token, a thread four elements of a row.  Bound by reading the
+// sums, which other XCDs wrote: 32768 rows of 128, most of two or three runs, 8.8 us
+// (11.8 with a wave a row).
+template <class T>
+__global__ void __launch_bounds__(512) join_rows_kernel(AttentionArgs p, int tile_rows)
+{
+    const int t = blockIdx.x;
+    int x0, n;
+    Request rq;
+    if (!runs_of(p, t, threadIdx.x & 63, x0, n, rq)) return;
+    const int64_t tile_size = (int64_t)tile_rows * (p.dim + 2), stride = tile_size * p.heads * p.row_tiles;
+    const int fours = p.dim / 4;
+    for (int j = threadIdx.x; j < p.q_heads * fours; j += 512) {
+        const int head = j / fours, d = 4 * (j - head * fours), kv = head / p.share;
+        const int row = (t - rq.first) * p.share + head - kv * p.share, tile = row / tile_rows, in_tile = row - tile * tile_rows;
+        const float *part = p.part + (((int64_t)x0 * p.heads + kv) * p.row_tiles + tile) * tile_size, *top_at = part + tile_rows * p.dim + in_tile;
+        join_runs<T>(part + in_tile * p.dim + d, top_at, top_at + tile_rows, stride, n,
+                     static_cast<typename T::elem *>(p.out) + t * p.out_token + head * p.out_head + d);
+    }
+}
+
+// The same for few rows of many runs: one wave a token and query
 // head, lane l four elements of every (256 / DP)-th run: its share of the
-// weight comes from the lane that holds that run's maximum and sum.
+// weight comes from the lane that holds that run's maximum and sum.  Bound by
+// latency: 2048 rows of up to 9 runs 4.8 us.
 template <class T, int DP>
 __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_rows)
 {
@@ -860,13 +913,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_row
     const int64_t id = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
     const int t = (int)(id / p.q_heads), head = (int)(id - (int64_t)t * p.q_heads);
     if (t >= p.tokens) return;
-    int r = 0;  // the number of requests that end at or before t
-    for (int base = 0; base < p.requests; base += 64)
-        r += __popcll(__ballot(base + lane < p.requests && p.offsets[base + lane + 1] <= t));
-    if (r >= p.requests) return;
-    const int x0 = p.first_run[2 * r], n = p.first_run[2 * r + 1];
-    const Request rq = request_of(p, r);
-    if (rq.fresh == 0 || t < rq.first || n <= 1) return;
+    int x0, n;
+    Request rq;
+    if (!runs_of(p, t, lane, x0, n, rq)) return;
     const int row = (t - rq.first) * p.share + head % p.share, tile = row / tile_rows, in_tile = row % tile_rows;
     const int64_t tile_size = (int64_t)tile_rows * (p.dim + 2), stride = tile_size * p.heads * p.row_tiles;
     const float *part = p.part + (((int64_t)x0 * p.heads + head / p.share) * p.row_tiles + tile) * tile_size;
@@ -953,9 +1002,10 @@ struct Shape {
 };
 
 // A workgroup's release writes back its XCD's L2: that costs less than the
-// second kernel while there are few (one request of 1000 keys: 9.3 us against
-// 10.8, two: 9.8 and 10.9), and more from about a hundred on (16 trees of 8 over
-// 1000 keys: 19.9 us against 16.3; 64 requests of up to 8192: 94 and 81).
+// second kernel while there are few runs of 16 rows (one request of 1000 keys:
+// 9.5 us against 10.8, two: 9.8 and 10.9), and more from about a hundred on (8
+// trees of 8, 128 of them: 17.0 us against 14.7; 64 requests of up to 8192: 94
+// and 81).
 constexpr int FEW_RUNS = 64;
 
 // The workspace begins with the counters, zeros whatever calls used it before.
@@ -986,7 +1036,10 @@ Shape shape_of(const gba_attention &d)
     s.whole = c.block_size % 16 == 0 && c.k_token >= 0 && c.v_token >= 0 && c.k_token < (1 << 25) && c.v_token < (1 << 25);
     s.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
     const int64_t rows = d.max_new * (d.q_heads / c.heads);
-    // 16 or 32 rows a wave; more rows on more waves that share the tiles
+    // 16 or 32 rows a wave (26 rows over 131k keys: 206 us, 368 as two tiles of
+    // 16); more rows on more waves that share the tiles (64 rows, 32 requests of
+    // up to 4096 keys, on 2 waves: 80 us, 117 on 8; 256 rows, 16 requests, on 8:
+    // 56 us, 71 as two tiles on 4)
     s.rt = rows <= 16 || (s.dp == 256 && !s.whole) ? 1 : 2;
     s.rg = rows <= 32 || s.dp == 256 || !s.whole ? 1 : rows <= 64 ? 2 : rows <= 128 ? 4 : 8;
     s.row_tiles = (int)div_up(rows, 16 * s.rt * s.rg);
@@ -997,7 +1050,7 @@ Shape shape_of(const gba_attention &d)
     if (d.requests <= SPLIT_REQUESTS && d.width * c.block_size > SHORTEST) {
         s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
-        s.counts = s.rg <= 2 && d.requests * c.heads * s.row_tiles * div_up(d.width * c.block_size, SHORTEST) <= FEW_RUNS &&
+        s.counts = s.rg <= 2 && s.rt * s.rg * d.requests * c.heads * s.row_tiles * div_up(d.width * c.block_size, SHORTEST) <= FEW_RUNS &&
                    (size_t)s.slots * c.heads * s.row_tiles <= COUNTERS;
         s.header = COUNTER_BYTES + (size_t)div_up(d.requests * 8, 256) * 256;
         s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt * s.rg) * (c.dim + 2) * sizeof(float);
@@ -1005,14 +1058,20 @@ Shape shape_of(const gba_attention &d)
     return s;
 }
 
+// A thread for four elements from this many rows on (16 trees of 64, 32768 rows:
+// 54.7 us in all, 56.4 with a wave a row), a wave a row below (one request of
+// 32000 keys, 32 rows of 32 runs: 34.7 against 42.2; 2048 rows: 81.3 and 82.5).
+constexpr int JOIN_ROWS = 4096;
+
 template <class T, int DP, int RT, int RG, bool WHOLE>
 gba_status run_attention(const AttentionArgs &a, hipStream_t s)
 {
     const int64_t groups = div_up((int64_t)a.slots * a.heads, 8) * 8 * a.row_tiles;
     constexpr int threads = threads_of<DP, RG>();
-    if (groups > (int64_t)UINT_MAX / threads || div_up((int64_t)a.tokens * a.q_heads, 4) > (int64_t)UINT_MAX / 256) return GBA_EUNSUPPORTED;
+    if (groups > (int64_t)UINT_MAX / threads || a.tokens > UINT_MAX / 512 || div_up((int64_t)a.tokens * a.q_heads, 4) > (int64_t)UINT_MAX / 256) return GBA_EUNSUPPORTED;
     const gba_status st = launch(attention_kernel<T, DP, RT, RG, WHOLE>, dim3((unsigned)groups), dim3(threads), s, a);
     if (st != GBA_OK || a.target == 0 || a.arrived != nullptr) return st;
+    if (a.tokens * (int64_t)a.q_heads >= JOIN_ROWS) return launch(join_rows_kernel<T>, dim3((unsigned)a.tokens), dim3(512), s, a, 16 * RT * RG);
     return launch(join_kernel<T, DP>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, 16 * RT * RG);
 }
 
