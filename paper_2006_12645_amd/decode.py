@@ -238,8 +238,9 @@ def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=
     tokens.  mask: int64 (tokens, 1) or (tokens,), which of its request's new
     tokens each one sees (a StepMaps'); None: those up to itself.  scale:
     1 / sqrt(dim) by default.  workspace: "auto" (a scratch buffer of this
-    stream), None (long requests are not split) or a uint8 CUDA tensor, zeros before
-    its first use.
+    stream, which a graph captured on it goes on using: its replays must not
+    overlap the stream's other calls), None (long requests are not split) or a
+    uint8 CUDA tensor, zeros before its first use.
     Rows of padded tokens are not written.
     """
     if stream is not None:
