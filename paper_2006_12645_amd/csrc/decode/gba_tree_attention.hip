@@ -964,6 +964,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_row
     *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + t * p.out_token + head * p.out_head + d) = r4;
 }
 
+constexpr float LOG2_E = 1.44269504088896340736f;
+
 gba_status validate(const gba_attention &d)
 {
     const gba_paged_cache &c = d.cache;
@@ -972,6 +974,7 @@ gba_status validate(const gba_attention &d)
         d.max_new < 0 || d.q_heads < 0)
         return GBA_EINVAL;
     if (d.workspace != nullptr && !aligned_to(d.workspace, 256)) return GBA_EINVAL;
+    if ((__builtin_bit_cast(uint32_t, d.scale * LOG2_E) & 0x7F800000u) == 0x7F800000u) return GBA_EINVAL;  // infinite or NaN
     if (d.requests > GBA_MAX_REQUESTS || d.width > INT_MAX || d.tokens > INT_MAX || c.num_blocks > INT_MAX ||
         c.block_size > INT_MAX || d.q_heads > 65535 || c.heads > 65535 || c.num_blocks * c.block_size > INT_MAX ||
         d.requests * d.width > INT_MAX || d.width * c.block_size > INT_MAX)
@@ -1160,7 +1163,7 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     a.num_blocks = (int)c.num_blocks;
     a.block_size = (int)c.block_size;
     a.dim = (int)c.dim;
-    const float scale2 = d.scale * 1.44269504088896340736f;
+    const float scale2 = d.scale * LOG2_E;
     a.sign = scale2 > 0.f ? 1.f : scale2 < 0.f ? -1.f : 0.f;
     a.scale2 = scale2 > 0.f ? scale2 : scale2 < 0.f ? -scale2 : 1.f;
     a.row_tiles = sh.row_tiles;

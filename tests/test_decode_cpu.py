@@ -175,3 +175,9 @@ def test_q4_groups_is_the_documented_layout():
     for g in range(3):
         for j in range(20):
             assert out[j // 16, g, j % 16] == per_group[g, j]
+
+
+@pytest.mark.parametrize("scale", [float("nan"), float("inf"), -float("inf"), 3e38])
+def test_attention_refuses_a_scale_that_is_not_finite(scale):
+    assert attention(scale=scale) == EINVAL
+    assert attention(scale=scale, tokens=0) == EINVAL
