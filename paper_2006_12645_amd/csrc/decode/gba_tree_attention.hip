@@ -347,11 +347,12 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
 
     // ---- copies of a tile: 1 KB each, lane l the chunk at byte 16 l
     char *mine = smem + kg * S::GROUP;
-    const int tiles = (run.to - run.from + KEYS - 1) / KEYS;
+    const int tiles = (int)(((unsigned)(run.to - run.from) + KEYS - 1) / KEYS);
     const int count = tiles > kg ? (tiles - kg + KG - 1) / KG : 0;  // of this group
     const int rounds = (tiles + KG * SUB - 1) / (KG * SUB);           // stages of every group, where waves meet
     const int32_t *entries = p.table + (int64_t)run.r * p.width;
-    auto key0 = [&](int n) { return run.from + KEYS * (kg + KG * n); };
+    // (unsigned: tiles past the run's end are looked up too, and a run may end just below 2^31)
+    auto key0 = [&](int n) -> unsigned { return (unsigned)run.from + KEYS * (unsigned)(kg + KG * n); };
     const int in_copy = lane / CPR, place = lane % CPR;
     constexpr int PER_HALF = COPIES / 2;
     const char *k_head = reinterpret_cast<const char *>(static_cast<const elem *>(p.k) + head * p.k_head);
@@ -390,16 +391,16 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     int entry = -1, within = 0;
     u4 k_next[WHOLE ? 1 : COPIES], v_next[WHOLE ? 1 : COPIES];
     auto look_up = [&](int n) {
-        const int pos = WHOLE ? key0(n + lane / 2) + 16 * (lane & 1) : key0(n) + (lane & 31);
+        const unsigned pos = WHOLE ? key0(n + lane / 2) + 16 * (lane & 1) : key0(n) + (lane & 31);
         entry = -1;
-        if (pos < run.to) {
-            const int page = pos / p.block_size;
-            within = pos - page * p.block_size;
+        if (pos < (unsigned)run.to) {
+            const int page = (int)(pos / (unsigned)p.block_size);
+            within = (int)pos - page * p.block_size;
             const int b = entries[page];
             entry = b >= 0 && b < p.num_blocks ? b : -1;
         }
         if constexpr (WHOLE) {
-            const int left = run.to - pos, keys = entry < 0 ? 0 : left < 16 ? left : 16;
+            const int left = run.to - (int)pos, keys = entry < 0 ? 0 : left < 16 ? left : 16;
             bits = (1u << keys) - 1;
             k_from = keys ? 2 * (entry * p.k_block + within * p.k_token) : 0;
             v_from = keys ? 2 * (entry * p.v_block + within * p.v_token) : 0;
@@ -547,7 +548,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     // does not see one of those.
     auto soften = [&](int n, unsigned there) -> bool {
         bool unseen = false;
-        const int first_draft = key0(n) - rq.kept;  // of the new tokens, or below 0
+        const int first_draft = (int)key0(n) - rq.kept;  // of the new tokens, or below 0
         if (there != 0xFFFFFFFFu || first_draft + KEYS > 0) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
@@ -624,7 +625,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             }
             if (odd != 0) {
                 *v = x;
-                atomicMin(&odd_from[RG > 1 ? kg : wave], key0(n + i / COPIES));
+                atomicMin(&odd_from[RG > 1 ? kg : wave], (int)key0(n + i / COPIES));
             }
         }
         lanes_meet();
