@@ -56,7 +56,7 @@ template <class T>
 __device__ __forceinline__ u4 load_row8(const typename T::elem *row, int k, int K)
 {
     typedef u4 unaligned __attribute__((aligned(2)));
-    if (k + 8 <= K) return *reinterpret_cast<const unaligned *>(row + k);
+    if (k <= K - 8) return *reinterpret_cast<const unaligned *>(row + k);  // (k + 8 may be 2^31)
     typename T::vec8 r;
 #pragma unroll
     for (int e = 0; e < 8; ++e) r[e] = k + e < K ? row[k + e] : (typename T::elem)0.f;
@@ -265,10 +265,10 @@ __global__ void __launch_bounds__(64 * WAVES) q4_rows_kernel(Q4Args p)
     // half chunk u; DIRECT: those past the wave's last one are of length 0, so
     // that the number of copies under way is always the same
     auto copy = [&](int u) {
-        const int k0 = (wave + WAVES * (u >> 1)) * 128 + 64 * (u & 1);
+        const unsigned k0 = (unsigned)(wave + WAVES * (u >> 1)) * 128 + 64 * (u & 1);  // past the last one it may pass 2^31
         const bool real = (u >> 1) < count;
         if constexpr (DIRECT) {
-            const bool past = k0 + 8 * piece >= p.K;
+            const bool past = k0 + 8 * piece >= (unsigned)p.K;
             const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc(const_cast<elem *>(A + (real ? k0 : 0)), (short)0,
                                                                                 real ? MAX_RECORDS : 0, RSRC_WORD3);
 #pragma unroll
@@ -279,7 +279,7 @@ __global__ void __launch_bounds__(64 * WAVES) q4_rows_kernel(Q4Args p)
             for (int j = 0; j < L::COPIES; ++j)
                 if (8 * j < rows) {
                     const int row = 8 * j + (lane >> 3);
-                    next[j] = load_row8<T>(A + (row < rows ? row : rows - 1) * p.lda, k0 + 8 * piece, p.K);
+                    next[j] = load_row8<T>(A + (row < rows ? row : rows - 1) * p.lda, (int)k0 + 8 * piece, p.K);
                 }
         }
     };

@@ -41,3 +41,23 @@ def test_attention_of_a_request_of_nearly_2_31_tokens(count, share, dim, block, 
     got = decode.tree_attention(q.cuda(), decode.PagedCache(k.cuda(), v.cuda()), table, torch.tensor([n], **i32),
                                 torch.tensor([0, count], **i32), max_new=count, workspace=workspace)
     D.check_attention(got, ref, spread, BF16)
+
+
+@pytest.mark.parametrize("zeros", [False, True], ids=["sym", "zeros"])
+def test_product_with_nearly_2_31_rows_of_weights(zeros):
+    """The last whole eight k before 2^31 are beyond K; NaN stands there."""
+    print("CASE long product", zeros, flush=True)
+    K, N = 2 ** 31 - 100, 3
+    chunks = -(-K // 128)
+    f16 = dict(dtype=HALF, device="cuda")
+    row = torch.zeros(2 ** 31 + 64, **f16)
+    at = [0, 12345, K // 2, K - 1000, K - 29, K - 2, K - 1]
+    for i, k in enumerate(at):
+        row[k] = i + 1
+    row[K:] = math.nan
+    codes = torch.zeros((1, chunks, 64, 4), dtype=torch.int32, device="cuda")  # every code is 0
+    scales = torch.full((1, chunks, 16), 0.125, **f16)
+    z = torch.full((1, chunks, 16), 4.0, **f16) if zeros else None
+    w = decode.Q4Weight(codes, scales, z, K=K, N=N, group=128)
+    got = decode.q4_linear(row[:K].view(1, K), w)
+    assert got.tolist() == [[-0.125 * (4 if zeros else 8) * 28] * N]
