@@ -574,7 +574,9 @@ typedef struct gba_attention {
  * on its rows, infinities and NaN included (a position whose block is outside
  * the cache counts as not seen).  Rows of out
  * that belong to no request are not written; neither are those of a request
- * past max_new.
+ * past max_new.  Where offsets fall, a request has no new tokens, and rows that
+ * several requests claim may be left unwritten; whatever they are, nothing
+ * outside the arrays is read or written.
  *
  * Workspace: with at least gba_tree_attention_workspace_size bytes, 256-byte
  * aligned, long requests are split across workgroups and their parts joined;

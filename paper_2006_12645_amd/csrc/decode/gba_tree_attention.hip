@@ -49,7 +49,8 @@ constexpr int KEYS = 32;        // of a tile
 constexpr int SHORTEST = 256;   // keys of a run, but a request's last
 constexpr float SLACK = 8.f;
 
-// A request's new tokens and keys, none for one with too many.
+// A request's new tokens and keys, none for one with too many, or whose
+// offsets fall or begin past the tokens.
 struct Request {
     int first, fresh, kept, end;
 };
@@ -58,8 +59,8 @@ __device__ __forceinline__ Request request_of(const AttentionArgs &p, int r)
 {
     Request q;
     q.first = p.offsets[r];
-    q.fresh = min(p.offsets[r + 1], p.tokens) - q.first;
-    if (q.first < 0 || q.fresh < 0 || q.fresh > p.max_new) q.fresh = 0;
+    q.fresh = q.first < 0 ? 0 : min(max(p.offsets[r + 1], 0), p.tokens) - q.first;
+    if (q.fresh < 0 || q.fresh > p.max_new) q.fresh = 0;
     q.kept = max(p.lens[r], 0);
     q.end = (int)min((int64_t)q.kept + q.fresh, (int64_t)p.width * p.block_size);
     return q;
@@ -876,7 +877,8 @@ __device__ __forceinline__ bool runs_of(const AttentionArgs &p, int t, int lane,
     x0 = p.first_run[2 * r];
     n = p.first_run[2 * r + 1];
     rq = request_of(p, r);
-    return rq.fresh != 0 && t >= rq.first && n > 1;
+    // (where offsets fall, the one that is found may not be the token's)
+    return rq.fresh != 0 && t >= rq.first && t - rq.first < rq.fresh && n > 1;
 }
 
 // The runs of a request, added in their order: many rows, each of few runs; a
