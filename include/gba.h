@@ -590,10 +590,11 @@ typedef struct gba_attention {
  * Errors: GBA_EINVAL for desc == NULL, a bad enum, negative sizes, block_size
  * < 1, q_heads no multiple of heads, heads == 0 with tokens, a NULL pointer
  * that is read or written, a scale that is infinite or NaN (or above 2^127), a
- * workspace not 256-byte aligned; GBA_EUNSUPPORTED for other dims, alignments or strides, num_blocks *
- * block_size, requests * width, width * block_size or tokens above 2^31-1,
- * more than GBA_MAX_REQUESTS requests, or max_new > 64 with a mask; GBA_EHIP
- * if a launch fails.
+ * workspace not 256-byte aligned; GBA_EUNSUPPORTED for other dims, alignments
+ * or strides, num_blocks * block_size, requests * width, width * block_size or
+ * tokens above 2^31-1, the smaller of max_new and tokens times q_heads / heads
+ * above 2^31-256, more than GBA_MAX_REQUESTS requests, or max_new > 64 with a
+ * mask; GBA_EHIP if a launch fails.
  */
 gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t stream);
 gba_status gba_tree_attention_workspace_size(const gba_attention *desc, size_t *bytes);

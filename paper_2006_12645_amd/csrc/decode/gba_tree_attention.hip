@@ -969,6 +969,9 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_row
 
 constexpr float LOG2_E = 1.44269504088896340736f;
 
+// No request has more new tokens than there are rows.
+int64_t most_new(const gba_attention &d) { return d.max_new < d.tokens ? d.max_new : d.tokens; }
+
 gba_status validate(const gba_attention &d)
 {
     const gba_paged_cache &c = d.cache;
@@ -986,6 +989,7 @@ gba_status validate(const gba_attention &d)
     if (d.tokens == 0 || d.requests == 0 || d.q_heads == 0 || d.max_new == 0 || c.dim == 0) return GBA_OK;
     if (c.heads == 0 || d.q_heads % c.heads != 0) return GBA_EINVAL;
     if (c.dim % 8 != 0 || c.dim > 256) return GBA_EUNSUPPORTED;
+    if (most_new(d) * (d.q_heads / c.heads) > INT_MAX - 255) return GBA_EUNSUPPORTED;  // rows of a request and head, in tiles of up to 256
     if (d.q == nullptr || d.out == nullptr || d.lens == nullptr || d.offsets == nullptr) return GBA_EINVAL;
     if (d.width > 0 && d.table == nullptr) return GBA_EINVAL;
     if (c.num_blocks > 0 && (c.k == nullptr || c.v == nullptr)) return GBA_EINVAL;
@@ -1041,7 +1045,7 @@ Shape shape_of(const gba_attention &d)
     // 16 keys in one block, and their offsets in a buffer of 32 bits
     s.whole = c.block_size % 16 == 0 && c.k_token >= 0 && c.v_token >= 0 && c.k_token < (1 << 25) && c.v_token < (1 << 25);
     s.dp = c.dim <= 64 ? 64 : c.dim <= 128 ? 128 : 256;
-    const int64_t rows = d.max_new * (d.q_heads / c.heads);
+    const int64_t rows = most_new(d) * (d.q_heads / c.heads);
     // 16 or 32 rows a wave (26 rows over 131k keys: 206 us, 368 as two tiles of
     // 16); more rows on more waves that share the tiles (64 rows, 32 requests of
     // up to 4096 keys, on 2 waves: 80 us, 117 on 8; 256 rows, 16 requests, on 8:
@@ -1159,7 +1163,7 @@ extern "C" gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t
     a.requests = (int)d.requests;
     a.width = c.num_blocks > 0 ? (int)d.width : 0;  // an empty cache: no keys
     a.tokens = (int)d.tokens;
-    a.max_new = (int)d.max_new;
+    a.max_new = (int)most_new(d);
     a.q_heads = (int)d.q_heads;
     a.heads = (int)c.heads;
     a.share = (int)(d.q_heads / c.heads);

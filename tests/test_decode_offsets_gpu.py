@@ -39,3 +39,11 @@ def test_offsets_of_any_size(tail):
     b.q = b.q[:8]
     ref, spread = D.attention(b.q, b.k, b.v, b.table[:2], [30, 40], [3, 5], None, b.scale)
     D.check_attention(attend(b, [0, 3] + tail, 8, 8), ref, spread, HALF)
+
+
+@pytest.mark.parametrize("max_new", [64, 10 ** 6, 2 ** 31, 2 ** 32, 2 ** 32 + 1, 2 ** 60])
+def test_a_bound_on_new_tokens_beyond_any_request(max_new):
+    print("CASE large max_new", max_new, flush=True)
+    b = D.Batch(4, [30, 900, 50], [3, 5, 1], heads=2, share=2, dim=64, block=16, dtype=HALF)
+    ref, spread = b.reference()
+    D.check_attention(attend(b, b.offsets.tolist(), max_new, 9), ref, spread, HALF)
