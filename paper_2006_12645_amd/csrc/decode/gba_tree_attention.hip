@@ -59,8 +59,9 @@ __device__ __forceinline__ Request request_of(const AttentionArgs &p, int r)
 {
     Request q;
     q.first = p.offsets[r];
-    q.fresh = q.first < 0 ? 0 : min(max(p.offsets[r + 1], 0), p.tokens) - q.first;
-    if (q.fresh < 0 || q.fresh > p.max_new) q.fresh = 0;
+    const int end = min(p.offsets[r + 1], p.tokens);
+    q.fresh = (int)((unsigned)end - (unsigned)q.first);
+    if (q.first < 0 || end < q.first || q.fresh > p.max_new) q.fresh = 0;
     q.kept = max(p.lens[r], 0);
     q.end = (int)min((int64_t)q.kept + q.fresh, (int64_t)p.width * p.block_size);
     return q;
