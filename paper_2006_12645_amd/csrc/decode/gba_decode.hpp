@@ -15,13 +15,16 @@ typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 // fp16 and bf16: the matrix instruction, the bits of 16 + q for a code q (the
 // code in the top bits of the fraction: no conversion is needed), and
-// those of infinity and of the exponent's lowest bit, all twice.
+// those of infinity and of the exponent's lowest bit, all twice.  SLACK, LIFT:
+// how far, in powers of two, a softmax weight may pass that of the running
+// maximum before the maximum moves, and what that one's weight is.
 struct F16 {
     typedef _Float16 elem;
     typedef h8 vec8;
     static constexpr unsigned SIXTEEN = 0x4C004C00u;  // 16.0 twice
     static constexpr int TOP = 6;                     // lowest bit of the four fraction bits that hold a code
     static constexpr unsigned INFINITE = 0x7C007C00u, EXPONENT_ONE = 0x04000400u;
+    static constexpr float SLACK = 4.f, LIFT = 11.f;
     static __device__ __forceinline__ f4 mfma(vec8 a, vec8 b, f4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -33,6 +36,7 @@ struct BF16 {
     static constexpr unsigned SIXTEEN = 0x41804180u;
     static constexpr int TOP = 3;
     static constexpr unsigned INFINITE = 0x7F807F80u, EXPONENT_ONE = 0x00800080u;
+    static constexpr float SLACK = 8.f, LIFT = 0.f;
     static __device__ __forceinline__ f4 mfma(vec8 a, vec8 b, f4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

@@ -10,10 +10,15 @@
 // between lanes.  V^T comes from transposing LDS reads.
 //
 // One pass: every row has a running maximum m and sum l.  m follows the scores
-// only when one passes it by more than 2^8 (in the base-2 exponent), so that
-// the accumulators are seldom scaled; weights then stay below 2^8, and their
-// relative rounding is the same at any size.  l is one more matrix
-// instruction, of ones and the rounded weights.
+// only when one passes it by more than SLACK (in the base-2 exponent), so that
+// the accumulators are seldom scaled.  Weights are 2^(score - m + LIFT), in 16
+// bits for the matrix instruction.  In bf16 (slack 8, lift 0) their relative
+// rounding is the same at any size.  In fp16 they have to stay below 2^16 and
+// lose bits below 2^-14: a slack of 4 and a lift of 11 use that range up, so
+// that the keys after a dominant one keep 11 bits down to 2^-25 of its weight
+// and none vanishes above 2^-36 (a slack of 8 and a lift of 7: 16 trees of 64
+// 52 us, not 53, but 4 bits fewer; 1 and 14: 57.5).  l is one more matrix
+// instruction, of ones and the rounded weights, and has the same factor 2^LIFT.
 //
 // Few rows read a whole cache: the bound is HBM.  A wave copies its tiles
 // straight into its own part of LDS, two tiles ahead, and waits for nothing but
@@ -47,7 +52,6 @@ struct AttentionArgs {
 
 constexpr int KEYS = 32;        // of a tile
 constexpr int SHORTEST = 256;   // keys of a run, but a request's last
-constexpr float SLACK = 8.f;
 
 // A request's new tokens and keys, none for one with too many, or whose
 // offsets fall or begin past the tokens.
@@ -578,10 +582,10 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 const float now = fmaxf(across_max(most[i]), top[i]);
-                const float next = now == -INFINITY ? 0.f : now;
+                const float next = now == -INFINITY ? 0.f : now - T::LIFT;
                 const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
                 top[i] = now;
-                limit[i] = now + SLACK;
+                limit[i] = now + T::SLACK;
                 base2[i] = next;
                 weights[i] *= keep;
 #pragma unroll
