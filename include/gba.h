@@ -572,8 +572,9 @@ typedef struct gba_attention {
  * and their sum is that of the rounded ones.
  * What the cache holds at positions that a token does not see has no effect
  * on its rows, infinities and NaN included (a position whose block is outside
- * the cache counts as not seen).  Rows of out
- * that belong to no request are not written; neither are those of a request
+ * the cache counts as not seen, and so does one with a score of -infinity).  A
+ * row with a NaN among the scores that it sees is NaN, however its request is
+ * split.  Rows of out that belong to no request are not written; neither are those of a request
  * past max_new.  Where offsets fall, a request has no new tokens, and rows that
  * several requests claim may be left unwritten; whatever they are, nothing
  * outside the arrays is read or written.

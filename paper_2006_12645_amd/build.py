@@ -31,9 +31,7 @@ UNITS = [("gba_api.hip", [], "gba_api.o"), ("gba_thin_unit.hip", [], "gba_thin.o
      [f"-DGBA_LA={la}", f"-DGBA_LB={lb}", f"-DGBA_PRO={pro}", f"-DGBA_DUAL={dual}"],
      f"gba_gemm_{'RC'[la]}{'RC'[lb]}_p{pro}d{dual}.o")
     for la in (0, 1) for lb in (0, 1) for pro in (0, 1) for dual in (0, 1)] + [
-    (os.path.join("decode", f"gba_{name}.hip"), flags, f"gba_{name}.o")
-    # attention: a maximum is one instruction where its operands cannot be NaN
-    for name, flags in (("q4", []), ("tables", []), ("cache", []), ("tree_attention", ["-fno-honor-nans"]))]
+    (os.path.join("decode", f"gba_{name}.hip"), [], f"gba_{name}.o") for name in ("q4", "tables", "cache", "tree_attention")]
 HIPCC_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall",
                "-Wno-unused-function", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                "-I", INCLUDE, "-I", CSRC]

@@ -179,11 +179,15 @@ __device__ __forceinline__ int swap_v(int key)
     return DP == 64 ? ((key >> 1) & 3) << 1 : (key & 7) << 1;
 }
 
+// The larger one, NaN if either is: one instruction, where fmaxf takes
+// two more to make its operands quiet.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
 // The largest of the four lanes that hold one row.
 __device__ __forceinline__ float across_max(float x)
 {
-    x = fmaxf(x, __shfl_xor(x, 32));
-    return fmaxf(x, __shfl_xor(x, 16));
+    x = larger(x, __shfl_xor(x, 32));
+    return larger(x, __shfl_xor(x, 16));
 }
 
 // Which of 32 keys from new token `first` on (below 0: from the cached ones)
@@ -271,7 +275,9 @@ constexpr int threads_of()
     return 64 * Shared<DP, RG>::WAVES;
 }
 
-// Four elements of a row of `n` runs, added in their order.
+// Four elements of a row of `n` runs, added in their order.  A run's maximum is
+// -infinity where the row sees none of its keys, and where all of its scores
+// are NaN: its sums, zeros or NaN, are added all the same.
 template <class T>
 __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_at, const float *l_at, int64_t stride, int n, typename T::elem *to)
 {
@@ -290,8 +296,7 @@ __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_
             w[u] = l_at[at];
         }
 #pragma unroll
-        for (int u = 0; u < 4; ++u) next = fmaxf(next, t[u]);
-        if (next == -INFINITY) continue;
+        for (int u = 0; u < 4; ++u) next = larger(next, t[u]);
         const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
         l *= keep;
         o *= keep;
@@ -574,14 +579,14 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         for (int i = 0; i < RT; ++i) {
             most[i] = score[i][0][0];
 #pragma unroll
-            for (int e = 1; e < 8; ++e) most[i] = fmaxf(most[i], score[i][e >> 2][e & 3]);
+            for (int e = 1; e < 8; ++e) most[i] = larger(most[i], score[i][e >> 2][e & 3]);
             most[i] *= p.scale2;
             past |= most[i] > limit[i];
         }
         if (__ballot(past)) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
-                const float now = fmaxf(across_max(most[i]), top[i]);
+                const float now = larger(across_max(most[i]), top[i]);
                 const float next = now == -INFINITY ? 0.f : now - T::LIFT;
                 const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
                 top[i] = now;
@@ -817,7 +822,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         if (row0 + row >= rows || d >= p.dim) continue;
         float m = tops[w0][r];
 #pragma unroll
-        for (int w = 1; w < KG; ++w) m = fmaxf(m, tops[w0 + w * RG][r]);
+        for (int w = 1; w < KG; ++w) m = larger(m, tops[w0 + w * RG][r]);
         f4 o = {0.f, 0.f, 0.f, 0.f};
         float l = 0.f;
 #pragma unroll
@@ -937,9 +942,8 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_row
         const float top = lane < here ? tops[(base + lane) * stride] : -INFINITY;
         const float sum = lane < here ? sums[(base + lane) * stride] : 0.f;
         float next = top;
-        for (int s = 32; s; s >>= 1) next = fmaxf(next, __shfl_xor(next, s));
-        next = fmaxf(next, m);
-        if (next == -INFINITY) continue;
+        for (int s = 32; s; s >>= 1) next = larger(next, __shfl_xor(next, s));
+        next = larger(next, m);
         const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
         const float share = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next);
         m = next;
