@@ -290,10 +290,13 @@ __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_
         float t[4], w[4], next = m;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            const int64_t at = (i + u < n ? i + u : i) * stride;
-            v[u] = *reinterpret_cast<const f4 *>(sum_at + at);
-            t[u] = i + u < n ? top_at[at] : -INFINITY;
-            w[u] = l_at[at];
+            const bool real = i + u < n;
+            const int64_t at = (real ? i + u : i) * stride;
+            const f4 sums = *reinterpret_cast<const f4 *>(sum_at + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = real ? sums[e] : 0.f;
+            t[u] = real ? top_at[at] : -INFINITY;
+            w[u] = real ? l_at[at] : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) next = larger(next, t[u]);
@@ -955,9 +958,11 @@ __global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_row
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int from = i + u * AT_ONCE + which;
-                const float w = __shfl(share, from & 63);
-                f[u] = from < here ? w : 0.f;
-                v[u] = *reinterpret_cast<const f4 *>(mine + (base + (from < here ? from : 0)) * stride);
+                const bool real = from < here;
+                f[u] = __shfl(share, from & 63);
+                const f4 sums = *reinterpret_cast<const f4 *>(mine + (base + (real ? from : 0)) * stride);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] = real ? sums[e] : 0.f;
             }
 #pragma unroll
             for (int u = 0; u < 4; ++u) o += f[u] * v[u];

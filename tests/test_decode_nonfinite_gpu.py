@@ -65,3 +65,20 @@ def test_a_key_that_is_nan(name, ws, dtype):
     put(b, 0, b.lens[0] // 2, k=math.nan)
     got = attend(b, ws).isnan().cpu()
     assert got[: b.counts[0]].all() and not got[b.counts[0]:].any()
+
+
+@pytest.mark.parametrize("dtype", [HALF, BF16], ids=["f16", "bf16"])
+@pytest.mark.parametrize("place", [0.0, 0.4, 0.95])
+@pytest.mark.parametrize("name,ws", CALLS)
+def test_a_value_that_is_infinite(name, ws, place, dtype):
+    """A cached value that every row of its request sees: its elements are what
+    the formula says, the others as without it."""
+    print("CASE infinite value", name, ws, place, dtype, flush=True)
+    b = batch(name, dtype, 7)
+    put(b, 0, int(place * b.lens[0]), v=-math.inf)
+    ref, spread = b.reference()
+    got = attend(b, ws)
+    finite = ref.isfinite()
+    assert torch.equal(ref.isneginf(), got.isneginf().cpu()) and not got.isnan().any() and not got.isposinf().any()
+    zero = torch.zeros_like(ref)
+    D.check_attention(torch.where(finite, got.double().cpu(), zero), torch.where(finite, ref, zero), torch.where(finite, spread, zero), dtype)
