@@ -193,10 +193,11 @@ __device__ __forceinline__ int slot_of(const TableArgs &p, int r, const Plan &q,
 // One wave: the tokens of request r, a tree, one a lane.  A token's mask is its
 // own bit and those of its ancestors, found by doubling: six rounds in which
 // every token takes the mask of the token it points to and then points to where
-// that one points.
+// that one points.  T may be less than the request asks for: a tree of more than
+// 64 has status 2 or 3.
 __device__ __forceinline__ void tree(const TableArgs &p, int r, const Plan &q, int avail, int first, int T, int lane)
 {
-    if (T > 64) {
+    if (q[3] >= 2 && p.count[r] > 64) {
         for (int i = lane; i < T; i += 64) {
             write_token(p, first + i, -1, -1);
             p.mask[first + i] = 0;
