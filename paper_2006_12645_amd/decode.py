@@ -211,20 +211,23 @@ class PagedCache:
 
 # Scratch of calls with workspace="auto", one per (device, stream): calls in a
 # stream's order share one.  A smaller one that was replaced is kept, since a
-# graph captured earlier may hold its address.
+# graph captured earlier may hold its address; as sizes at least double, those
+# kept are together smaller than the one in use.
 _scratch = {}
 _retired = []
 
 
 def _more_scratch(nbytes, device, key):
-    """A larger scratch buffer of the current stream, zeros."""
+    """A larger scratch buffer of the current stream, of at least nbytes, zeros."""
     if torch.cuda.is_current_stream_capturing():
         raise RuntimeError(f"workspace='auto' would allocate {nbytes} bytes while the stream is being captured into a graph; "
                            "pass a zero-filled uint8 CUDA tensor of at least that size as `workspace`, or make one call "
                            "before the capture")
+    size = max(nbytes, 1 << 20)
     if key in _scratch:
         _retired.append(_scratch[key])
-    _scratch[key] = torch.zeros(max(nbytes, 1 << 20), dtype=torch.uint8, device=device)
+        size = max(size, 2 * _scratch[key].numel())
+    _scratch[key] = torch.zeros(size, dtype=torch.uint8, device=device)
     return _scratch[key]
 
 
