@@ -5,7 +5,8 @@ operand-layout pair and kernel variant (csrc/gba_gemm_unit.hip compiled with
 GBA_LA, GBA_LB, GBA_PRO, GBA_DUAL set) and the operators of a decoding step
 (csrc/decode, one unit each) are compiled in parallel, then linked into
 ``paper_2006_12645_amd/libgba.so``; then the Python extension of those operators
-(_gba_decode.so) is compiled with g++.  Every hipcc line carries
+(_gba_decode.so) is compiled with g++, if torch and Python's headers are there:
+the library needs neither.  Every hipcc line carries
 ``-Xclang -target-feature -Xclang -packed-fp32-ops`` so the device compiler
 never forms packed fp32 instructions.
 """
@@ -82,13 +83,23 @@ def _build_binding(verbose):
     against torch's headers and libgba.so)."""
     import sysconfig
 
-    import torch
+    headers = sysconfig.get_paths()["include"]
+    try:
+        import torch
+        missing = None if os.path.exists(os.path.join(headers, "Python.h")) else "Python's headers are missing"
+    except ImportError as e:
+        missing = str(e)
+    if missing is not None:
+        if os.path.exists(BINDING):
+            os.remove(BINDING)  # an earlier library's
+        print(f"{os.path.basename(BINDING)}, the extension of paper_2006_12645_amd/decode.py, is not built: {missing}", flush=True)
+        return
     root = os.path.dirname(torch.__file__)
     include = os.path.join(root, "include")
     tmp = BINDING + ".tmp"
     cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-I", INCLUDE, "-isystem", include,
-           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", sysconfig.get_paths()["include"],
+           "-isystem", os.path.join(include, "torch", "csrc", "api", "include"), "-isystem", headers,
            os.path.join(CSRC, "decode", "gba_bind.cpp"), "-o", tmp, "-L", os.path.join(root, "lib"), "-ltorch_python",
            "-ltorch_cpu", "-lc10", "-L", PKG, "-lgba", "-Wl,-rpath,$ORIGIN"]
     if verbose:
