@@ -428,7 +428,9 @@ gba_status gba_q4_pack(int64_t K, int64_t N, const void *codes, int64_t ld, void
  * A (row-major, lda >= K), bias (N, or NULL) and C (row-major, ldc >= N) are
  * of the weight's dtype.  Products are exact and summed in fp32; scales are
  * applied to each group's fp32 sum.  Meant for up to 64 rows, which share one
- * pass over the weights; more rows run as blocks of 64.
+ * pass over the weights; more rows run as blocks of 64.  Where that sum is not
+ * finite, as with infinities or NaN in A, C is what the formula gives in 64 bits;
+ * an activation of NaN is NaN.
  * A and C need the alignment of an element only.
  * M == 0 or N == 0: nothing is launched.  K == 0: C = act(bias).
  * Errors: GBA_EINVAL for w == NULL, a bad enum or group, negative sizes, a

@@ -6,7 +6,8 @@
 //     sum_k a_k (q_k - z) = sum_k a_k (16 + q_k) - (16 + z) sum_k a_k
 // and both sums are matrix instructions, the second one of A and ones, for all
 // columns of a wave at once.  The products are exact and the sums fp32; the
-// scale multiplies a group's fp32 sum.
+// scale multiplies a group's fp32 sum.  Where an element's sum is not finite,
+// the first form is computed for it instead.
 //
 // The bound is reading W once.  A workgroup owns 16 NT columns and 16 MT rows;
 // its waves take the 128-deep chunks of K in turn and never wait for each
@@ -63,9 +64,37 @@ __device__ __forceinline__ u4 load_row8(const typename T::elem *row, int k, int 
     return __builtin_bit_cast(u4, r);
 }
 
+// sum_k a_k s (q_k - z) of one element, as it is written and in 64 bits.
+template <class T>
+__device__ __forceinline__ float q4_plainly(const Q4Args &p, int group, int row, int col)
+{
+    typedef typename T::elem elem;
+    const int nb = col / 16, j = col % 16;
+    const elem *a = static_cast<const elem *>(p.A) + row * p.lda;
+    const uint32_t *codes = reinterpret_cast<const uint32_t *>(p.codes) + (int64_t)nb * p.KB * 256 + j * 4;
+    const int64_t at = (int64_t)nb * p.GB * 16 + j;
+    const elem *scales = static_cast<const elem *>(p.scales) + at, *zeros = static_cast<const elem *>(p.zeros) + at;
+    double all = 0.;
+    for (int g = 0; g < p.GB; ++g) {
+        const double zero = p.zeros != nullptr ? (double)(float)zeros[(int64_t)g * 16] : 8.;
+        double sum = 0.;
+        for (int i = 0; i < group && g * group + i < p.K; i += 8) {
+            const int k = g * group + i;
+            const uint32_t w = codes[(int64_t)(k / 128) * 256 + k % 32 / 8 * 64 + k % 128 / 32];
+            for (int e = 0; e < 8 && k + e < p.K; ++e) sum += (double)(float)a[k + e] * ((double)((w >> (4 * (e / 2) + 16 * (e % 2))) & 15) - zero);
+        }
+        all += (double)(float)scales[(int64_t)g * 16] * sum;
+    }
+    return (float)all;
+}
+
 // The waves' sums, added in wave order, bias, activation, and the one rounding.
+// A sum that is not finite says little: infinity times 16 + q less infinity
+// times 16 + z is NaN, and so is what the two sums of large inputs leave where
+// each passes the largest float.  Such elements are computed again, plainly (one
+// infinite input, 1 x 8192 x 32768: 0.65 ms).
 template <class T, int MT, int NT, int W>
-__device__ __forceinline__ void q4_store(const Q4Args &p, const f4 (&acc)[MT][NT], char *smem, int row0, int nb0)
+__device__ __forceinline__ void q4_store(const Q4Args &p, int group, const f4 (&acc)[MT][NT], char *smem, int row0, int nb0)
 {
     typedef typename T::elem elem;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -76,18 +105,34 @@ __device__ __forceinline__ void q4_store(const Q4Args &p, const f4 (&acc)[MT][NT
         for (int n = 0; n < NT; ++n) part[((wave * MT + t) * NT + n) * 64 + lane] = acc[t][n];
     __syncthreads();
     const float *sums = reinterpret_cast<const float *>(smem);
-    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * W) {
+    auto element = [&](int i, int &row, int &col) {
         const int t = i / (256 * NT), r = i / (16 * NT) % 16, n = i / 16 % NT, j = i % 16;
-        const int row = row0 + 16 * t + r, col = 16 * (nb0 + n) + j;
-        float x[1] = {0.f};
+        row = row0 + 16 * t + r;
+        col = 16 * (nb0 + n) + j;
+        float x = 0.f;
 #pragma unroll
-        for (int w = 0; w < W; ++w) x[0] += sums[(((w * MT + t) * NT + n) * 64 + (r / 4) * 16 + j) * 4 + r % 4];
-        if (row < p.M && col < p.N) {
-            if (p.bias != nullptr) x[0] += (float)static_cast<const elem *>(p.bias)[col];
-            activate(p.act, x);
-            static_cast<elem *>(p.C)[row * p.ldc + col] = (elem)x[0];
-        }
+        for (int w = 0; w < W; ++w) x += sums[(((w * MT + t) * NT + n) * 64 + (r / 4) * 16 + j) * 4 + r % 4];
+        return x;
+    };
+    auto finite = [](float x) { return (__builtin_bit_cast(unsigned, x) & 0x7F800000u) != 0x7F800000u; };
+    auto store = [&](int row, int col, float sum) {
+        float x[1] = {sum};
+        if (p.bias != nullptr) x[0] += (float)static_cast<const elem *>(p.bias)[col];
+        if (x[0] == x[0]) activate(p.act, x);  // (NaN stays NaN)
+        static_cast<elem *>(p.C)[row * p.ldc + col] = (elem)x[0];
+    };
+    bool odd = false;
+    int row, col;
+    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * W) {
+        const float x = element(i, row, col);
+        if (row >= p.M || col >= p.N) continue;
+        odd |= !finite(x);
+        store(row, col, x);
     }
+    if (!odd) return;
+#pragma unroll 1
+    for (int i = threadIdx.x; i < 256 * MT * NT; i += 64 * W)
+        if (!finite(element(i, row, col)) && row < p.M && col < p.N) store(row, col, q4_plainly<T>(p, group, row, col));
 }
 
 // Up to 16 rows.  STEPS: 32-deep steps of a group.  W: waves.  AHEAD: chunks
@@ -194,7 +239,7 @@ __global__ void __launch_bounds__(64 * W) q4_kernel(Q4Args p)
     }
 
     __syncthreads();
-    q4_store<T, MT, NT, W>(p, acc, smem, row0, nb0);
+    q4_store<T, MT, NT, W>(p, 32 * STEPS, acc, smem, row0, nb0);
 }
 
 // 16 MT rows, MT 2 or 4, of which a wave could not hold the next chunks in
@@ -358,7 +403,7 @@ __global__ void __launch_bounds__(64 * WAVES) q4_rows_kernel(Q4Args p)
     }
     wait_vm_lgkm0<0>();
     __syncthreads();
-    q4_store<T, MT, NT, WAVES>(p, acc, smem, row0, nb0);
+    q4_store<T, MT, NT, WAVES>(p, 32 * STEPS, acc, smem, row0, nb0);
 }
 
 template <class T, int MT, int NT, bool DIRECT>
