@@ -589,7 +589,7 @@ typedef struct gba_attention {
  * ones.
  *
  * dim a multiple of 8 up to 256; q, out, K and V 16-byte aligned with strides
- * that are multiples of 8 (out: 4).
+ * that are multiples of 8 (out: 4), but in dimensions of one element.
  * Errors: GBA_EINVAL for desc == NULL, a bad enum, negative sizes, block_size
  * < 1, q_heads no multiple of heads, heads == 0 with tokens, a NULL pointer
  * that is read or written, a scale that is infinite or NaN (or above 2^127), a

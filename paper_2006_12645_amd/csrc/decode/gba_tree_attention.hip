@@ -1007,10 +1007,12 @@ gba_status validate(const gba_attention &d)
     if (d.q == nullptr || d.out == nullptr || d.lens == nullptr || d.offsets == nullptr) return GBA_EINVAL;
     if (d.width > 0 && d.table == nullptr) return GBA_EINVAL;
     if (c.num_blocks > 0 && (c.k == nullptr || c.v == nullptr)) return GBA_EINVAL;
-    const int64_t eights[] = {c.k_block, c.k_token, c.k_head, c.v_block, c.v_token, c.v_head, d.q_token, d.q_head};
-    for (int64_t s : eights)
-        if (s % 8 != 0) return GBA_EUNSUPPORTED;
-    if (d.out_token % 4 != 0 || d.out_head % 4 != 0) return GBA_EUNSUPPORTED;
+    // (a stride of a dimension of one element is not used)
+    const struct { int64_t extent, stride; int of; } strides[] = {
+        {c.num_blocks, c.k_block, 8}, {c.block_size, c.k_token, 8}, {c.heads, c.k_head, 8}, {c.num_blocks, c.v_block, 8}, {c.block_size, c.v_token, 8},
+        {c.heads, c.v_head, 8}, {d.tokens, d.q_token, 8}, {d.q_heads, d.q_head, 8}, {d.tokens, d.out_token, 4}, {d.q_heads, d.out_head, 4}};
+    for (const auto &s : strides)
+        if (s.extent > 1 && s.stride % s.of != 0) return GBA_EUNSUPPORTED;
     if (!aligned_to(d.q, 16) || !aligned_to(d.out, 16) || !aligned_to(c.k, 16) || !aligned_to(c.v, 16) ||
         !aligned_to(d.table, 4) || !aligned_to(d.lens, 4) || !aligned_to(d.offsets, 4) || !aligned_to(d.mask, 8))
         return GBA_EUNSUPPORTED;
