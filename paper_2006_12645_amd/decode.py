@@ -22,15 +22,16 @@ from . import gba
 DTYPES = {torch.float16: gba.GBA_F16, torch.bfloat16: gba.GBA_BF16}
 
 
-def _gpu(name, t, dtype):
+def _gpu(name, t, dtype, device=None):
     if t.dtype is not dtype or not t.is_cuda:
         raise TypeError(f"{name} must be a CUDA tensor of {dtype}")
+    if device is not None and t.device != device:
+        raise ValueError(f"{name} is on another device than what it is used with")
 
 
-def _ints(name, t, shape):
+def _ints(name, t, shape, device=None):
     """A contiguous int32 CUDA tensor of this shape."""
-    if t.dtype is not torch.int32 or not t.is_cuda:
-        raise TypeError(f"{name} must be an int32 CUDA tensor")
+    _gpu(name, t, torch.int32, device)
     if t.shape != shape or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous tensor of shape {tuple(shape)}, got {tuple(t.shape)}")
 
@@ -70,15 +71,14 @@ class Q4Weight:
             raise ValueError("group must be 32, 64 or 128")
         if scales.dtype not in DTYPES or not scales.is_cuda:
             raise TypeError("scales must be a float16 or bfloat16 CUDA tensor")
-        if codes.dtype is not torch.int32 or not codes.is_cuda:
-            raise TypeError("codes must be an int32 CUDA tensor")
+        _gpu("codes", codes, torch.int32, scales.device)
         columns, chunks, groups = -(-N // 16), -(-K // 128), -(-K // group)
         if codes.shape != (columns, chunks, 64, 4) or not codes.is_contiguous():
             raise ValueError(f"codes must be a contiguous {(columns, chunks, 64, 4)} tensor, got {tuple(codes.shape)}")
         for name, t in (("scales", scales), ("zeros", zeros)):
             if t is None:
                 continue
-            _gpu(name, t, scales.dtype)
+            _gpu(name, t, scales.dtype, scales.device)
             if t.shape != (columns, groups, 16) or not t.is_contiguous():
                 raise ValueError(f"{name} must be a contiguous {(columns, groups, 16)} tensor, got {tuple(t.shape)}")
         self.codes, self.scales, self.zeros = codes, scales, zeros
@@ -141,9 +141,9 @@ class BlockTables:
     def __init__(self, table, held, free_blocks, free_count, block_size, *, tokens, tree=False):
         requests, width = table.shape
         _ints("table", table, (requests, width))
-        _ints("held", held, (requests,))
-        _ints("free_blocks", free_blocks, free_blocks.shape[:1])
-        _ints("free_count", free_count, (1,))
+        _ints("held", held, (requests,), table.device)
+        _ints("free_blocks", free_blocks, free_blocks.shape[:1], table.device)
+        _ints("free_count", free_count, (1,), table.device)
         if block_size < 1 or tokens < 0:
             raise ValueError("block_size must be positive and tokens not negative")
         self.table, self.held, self.free_blocks, self.free_count = table, held, free_blocks, free_count
@@ -191,7 +191,7 @@ class PagedCache:
     def __init__(self, k, v):
         if k.dtype not in DTYPES or not k.is_cuda:
             raise TypeError("k must be a float16 or bfloat16 CUDA tensor")
-        _gpu("v", v, k.dtype)
+        _gpu("v", v, k.dtype, k.device)
         if k.dim() != 4 or v.shape != k.shape:
             raise ValueError("k and v must be (num_blocks, block_size, heads, dim)")
         if k.shape[3] > 1 and (k.stride(3) != 1 or v.stride(3) != 1):
