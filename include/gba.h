@@ -523,8 +523,9 @@ typedef struct gba_paged_cache {
  * gba_cache_store -- write new keys and values into the cache: for each token
  * t with 0 <= slots[t] < num_blocks * block_size, head h and element d
  *     K(slots[t], h, d) = k[t*k_token + h*k_head + d], and V from v likewise.
- * Tokens with any other slot are left out.  Two tokens with one slot leave
- * either's row.  k and v are of the cache's dtype (strides in elements).
+ * Tokens with any other slot are left out.  The others' slots differ: where two
+ * tokens have one, every element of its row is one or the other's, in K and in V,
+ * but the row may be a mixture of both.  k and v are of the cache's dtype (strides in elements).
  * Errors: GBA_EINVAL for cache == NULL, a bad enum, negative sizes, block_size
  * < 1, a NULL pointer that is read or written; GBA_EUNSUPPORTED for
  * num_blocks * block_size, tokens or heads * dim above 2^31-1, or an array of

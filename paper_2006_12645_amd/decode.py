@@ -205,7 +205,8 @@ class PagedCache:
 
     def store(self, k, v, slots, stream=None):
         """Write the rows k[t], v[t] (tokens, heads, dim) at slots[t] (int32;
-        tokens whose slot is outside the cache are left out)."""
+        tokens whose slot is outside the cache are left out, the others' slots
+        differ)."""
         self._store(self._at, self._index, k, v, slots, _raw_stream(self._index) if stream is None else stream.cuda_stream)
 
 
