@@ -114,7 +114,8 @@ struct Run {
 
 // Every run but a request's last is of one length, a multiple of `step`:
 // the mean of all keys over p.target runs, so there are no more than
-// p.target + p.requests.  The sum of the lengths is one in 24 bits; the
+// p.target + p.requests; a mean next to 2^31 or above makes one run of each
+// request.  The sum of the lengths is one in 24 bits; the
 // factor covers its rounding.
 __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, int step)
 {
@@ -136,8 +137,7 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
         if (q.fresh > 0) keys += (float)q.end;
     }
     const float mean = wave_total(keys) / (float)p.target * 1.00001f;
-    const int most = INT_MAX / step * step;
-    int length = mean < (float)(most - step) ? ((int)mean / step + 1) * step : most;
+    int length = mean < (float)(INT_MAX / step * step - step) ? ((int)mean / step + 1) * step : INT_MAX;
     if (length < SHORTEST) length = SHORTEST;
     length = uniform(length);
     u.r = -1;
