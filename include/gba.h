@@ -524,8 +524,9 @@ typedef struct gba_paged_cache {
  * t with 0 <= slots[t] < num_blocks * block_size, head h and element d
  *     K(slots[t], h, d) = k[t*k_token + h*k_head + d], and V from v likewise.
  * Tokens with any other slot are left out.  The others' slots differ: where two
- * tokens have one, every element of its row is one or the other's, in K and in V,
- * but the row may be a mixture of both.  k and v are of the cache's dtype (strides in elements).
+ * tokens have one, every element of its row is one or the other's, in K and in
+ * V, but the row may be a mixture of both.  k and v are of the cache's dtype
+ * (strides in elements).
  * Errors: GBA_EINVAL for cache == NULL, a bad enum, negative sizes, block_size
  * < 1, a NULL pointer that is read or written; GBA_EUNSUPPORTED for
  * num_blocks * block_size, tokens or heads * dim above 2^31-1, or an array of
@@ -597,8 +598,9 @@ typedef struct gba_attention {
  * workspace not 256-byte aligned; GBA_EUNSUPPORTED for other dims, alignments
  * or strides, num_blocks * block_size, requests * width, width * block_size or
  * tokens above 2^31-1, the smaller of max_new and tokens times q_heads / heads
- * above 2^31-256, more than GBA_MAX_REQUESTS requests, or max_new > 64 with a
- * mask; GBA_EHIP if a launch fails.
+ * above 2^31-256, more than GBA_MAX_REQUESTS requests, a launch of 2^32 threads
+ * or more (of tokens from 2^23 on), or max_new > 64 with a mask; GBA_EHIP if a
+ * launch fails.
  */
 gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t stream);
 gba_status gba_tree_attention_workspace_size(const gba_attention *desc, size_t *bytes);

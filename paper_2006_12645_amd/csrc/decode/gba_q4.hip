@@ -137,7 +137,7 @@ __device__ __forceinline__ void q4_store(const Q4Args &p, int group, const f4 (&
 
 // Up to 16 rows.  STEPS: 32-deep steps of a group.  W: waves.  AHEAD: chunks
 // that each holds in registers.  Bound by HBM for a large W: 1 x 8192 x 32768,
-// 139 MB, 28.5 to 30.8 us (4.5 to 4.9 TB/s); 1 x 8192 x 8192, 36 MB, 10.0 us (3.6);
+// 139 MB, 28.7 to 29.5 us (4.7 to 4.8 TB/s); 1 x 8192 x 8192, 35 MB, 9.3 us (3.7);
 // 1 x 1024 x 1024 2.6 us, latency.
 template <class T, int NT, int STEPS, bool ZEROS, int W, int AHEAD>
 __global__ void __launch_bounds__(64 * W) q4_kernel(Q4Args p)
@@ -250,7 +250,7 @@ __global__ void __launch_bounds__(64 * W) q4_kernel(Q4Args p)
 // The codes, scales and zeros of the next two chunks stay in registers.  Bound by
 // instructions, about 430 a chunk and wave (48 of them matrix instructions), and
 // by all of A going through each compute unit: 64 x 8192 x 8192, groups of 64 with
-// zeros, 20.8 to 23.9 us (360 to 410 TFLOP/s, 1.7 to 1.9 TB/s).
+// zeros, 21.1 to 23.7 us (360 to 410 TFLOP/s, 1.7 to 1.9 TB/s).
 template <int MT, int NT, bool DIRECT>
 struct Q4Lds {
     static constexpr int AHEAD = MT == 4 || !DIRECT ? 1 : 3, SLOTS = DIRECT ? AHEAD + 1 : 1;
@@ -436,8 +436,8 @@ gba_status run_few(const Q4Args &a, int group, hipStream_t s)
 // Which kernel: one 16-row block with its chunks in registers up to 16 rows,
 // else blocks of 32 or 64 rows.  Column blocks of a workgroup: as many as
 // leave 256 workgroups, since a workgroup reads all of its rows of A (1 x 8192 x
-// 8192: 10.0 us with two, 13.3 with one; 1 x 4096 x 4096 4.6 with one, 5.5 with two;
-// 64 x 8192 x 8192 23.9 with two, 35.5 with one; 32 x 4096 x 4096 7.6 with one, 8.6
+// 8192: 9.3 us with two, 12.0 with one; 1 x 4096 x 4096 4.5 with one, 5.3 with two;
+// 64 x 8192 x 8192 22.0 with two, 30.5 with one; 32 x 4096 x 4096 7.4 with one, 8.4
 // with two).
 template <class T>
 gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
@@ -446,7 +446,7 @@ gba_status run_q4(const Q4Args &a, int group, hipStream_t s)
         // One chunk ahead on four column blocks, two on fewer: more waves fit
         // with fewer registers (1 x 8192 x 32768: 28.5 us against 32.2 with
         // twice as many ahead).  16 waves with one ahead where each has a
-        // chunk: 1 x 8192 x 8192 9.4 us against 10.6 with 8, 16 x 8192 x 1024
+        // chunk: 1 x 8192 x 8192 9.3 us against 10.5 with 8, 16 x 8192 x 1024
         // 6.9 against 8.2; half of them idle, 1024 x 32768 12.1 against 7.7.
         if (a.NB >= 1024) return run_few<T, 4, WAVES, 1>(a, group, s);
         if (a.KB >= 16 && a.NB < 512) return run_few<T, 1, 16, 1>(a, group, s);
