@@ -599,8 +599,8 @@ typedef struct gba_attention {
  * or strides, num_blocks * block_size, requests * width, width * block_size or
  * tokens above 2^31-1, the smaller of max_new and tokens times q_heads / heads
  * above 2^31-256, more than GBA_MAX_REQUESTS requests, a launch of 2^32 threads
- * or more (of tokens from 2^23 on), or max_new > 64 with a mask; GBA_EHIP if a
- * launch fails.
+ * or more (with a workspace, of tokens from 2^23 on), or max_new > 64 with a
+ * mask; GBA_EHIP if a launch fails.
  */
 gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t stream);
 gba_status gba_tree_attention_workspace_size(const gba_attention *desc, size_t *bytes);

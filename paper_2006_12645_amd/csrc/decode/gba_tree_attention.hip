@@ -1094,10 +1094,11 @@ gba_status run_attention(const AttentionArgs &a, hipStream_t s)
 {
     const int64_t groups = div_up((int64_t)a.slots * a.heads, 8) * 8 * a.row_tiles;
     constexpr int threads = threads_of<DP, RG>();
-    if (groups > (int64_t)UINT_MAX / threads || a.tokens > UINT_MAX / 512 || div_up((int64_t)a.tokens * a.q_heads, 4) > (int64_t)UINT_MAX / 256) return GBA_EUNSUPPORTED;
+    const bool joins = a.target != 0 && a.arrived == nullptr, joins_rows = joins && a.tokens * (int64_t)a.q_heads >= JOIN_ROWS;
+    if (groups > (int64_t)UINT_MAX / threads || (joins_rows && a.tokens > UINT_MAX / 512)) return GBA_EUNSUPPORTED;
     const gba_status st = launch(attention_kernel<T, DP, RT, RG, WHOLE>, dim3((unsigned)groups), dim3(threads), s, a);
-    if (st != GBA_OK || a.target == 0 || a.arrived != nullptr) return st;
-    if (a.tokens * (int64_t)a.q_heads >= JOIN_ROWS) return launch(join_rows_kernel<T>, dim3((unsigned)a.tokens), dim3(512), s, a, 16 * RT * RG);
+    if (st != GBA_OK || !joins) return st;
+    if (joins_rows) return launch(join_rows_kernel<T>, dim3((unsigned)a.tokens), dim3(512), s, a, 16 * RT * RG);
     return launch(join_kernel<T, DP>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, 16 * RT * RG);
 }
 
