@@ -605,6 +605,25 @@ typedef struct gba_attention {
 gba_status gba_tree_attention(const gba_attention *desc, gba_stream_t stream);
 gba_status gba_tree_attention_workspace_size(const gba_attention *desc, size_t *bytes);
 
+/*
+ * gba_window_attention -- gba_tree_attention of a bounded part of the text.
+ *
+ * The text of a new token is the lens[r] cached positions of its request and
+ * then the new tokens that it sees, in their order (with mask == NULL those up
+ * to itself, with a mask those of its set bits below T).  Of this text it sees
+ * the last `window` positions -- its own among them, if it sees itself -- and
+ * the first `sinks`; everything else is as in gba_tree_attention.  Positions
+ * count whether or not their block is in the cache.
+ *
+ * The workspace is that of gba_tree_attention, of the size that
+ * gba_window_attention_workspace_size gives for the same window and sinks.
+ * Errors: those of gba_tree_attention, and GBA_EINVAL for window < 1 or
+ * sinks < 0.
+ */
+gba_status gba_window_attention(const gba_attention *desc, int64_t window, int64_t sinks, gba_stream_t stream);
+gba_status gba_window_attention_workspace_size(const gba_attention *desc, int64_t window, int64_t sinks,
+                                               size_t *bytes);
+
 /* Static, human-readable name of a status code. */
 const char *gba_status_string(gba_status status);
 

@@ -1,0 +1,383 @@
+// gba_attention.hpp -- what the kernels of attention over a paged cache share:
+// a request's keys, cut into runs of one length over all requests, and the
+// joins of a request's runs in their order.
+#pragma once
+
+#include "gba_decode.hpp"
+
+namespace gba {
+namespace {
+
+struct AttentionArgs {
+    const void *q, *k, *v;
+    void *out;
+    const int32_t *table, *lens, *offsets;
+    const uint64_t *mask;
+    int64_t k_block, k_token, k_head, v_block, v_token, v_head, q_token, q_head, out_token, out_head;
+    int requests, width, tokens, max_new, q_heads, heads, share, num_blocks, block_size, dim;
+    float scale2;      // |scale| * log2(e); its sign, or 0, goes to the queries
+    float sign;
+    int window, sinks; // (windows only) what a token sees of its text: the last ones and the first
+    int row_tiles;     // of a request and head
+    int slots;         // runs of keys there is room for: at least as many as there are
+    int target;        // runs to aim at (0: one for each request)
+    int32_t *arrived;    // [slots][heads][row_tiles], zeros: runs that have ended, at a request's first one; or null
+    int32_t *first_run;  // [requests][2]: a request's first run and how many it has
+    float *part;       // [slots][heads][row_tiles]: rows x dim sums, then as many maxima and sums of weights
+};
+
+constexpr int SHORTEST = 256;   // keys of a run, but a request's last
+
+// A request's new tokens and keys, none for one with too many, or whose
+// offsets fall or begin past the tokens.  With a window, keys are counted
+// without the `gap` from position `split` on that none of the rows sees: key v
+// is position v, or v + gap from split on.
+struct Request {
+    int first, fresh, kept, end;
+    int split, gap;
+};
+
+template <bool WINDOW>
+__device__ __forceinline__ unsigned position_of(const Request &q, unsigned key)
+{
+    return WINDOW && key >= (unsigned)q.split ? key + (unsigned)q.gap : key;
+}
+
+// Where the window begins of a token whose text is as long as `seen` positions
+// after the cached ones make it.
+__device__ __forceinline__ int begin_of(const AttentionArgs &p, int kept, int seen)
+{
+    const int64_t begin = (int64_t)kept + seen - p.window;
+    return (int)(begin < 0 ? 0 : begin < INT_MAX ? begin : INT_MAX);
+}
+
+// The keys of new tokens `from` to `to` of a request (of all of them with a
+// mask: the shortest text is the cached one), sinks and window in whole tiles
+// of TILE.
+template <int TILE>
+__device__ __forceinline__ void bound_keys(const AttentionArgs &p, int from, int to, Request &q)
+{
+    constexpr unsigned WHOLE = ~(unsigned)(TILE - 1);
+    const int64_t past = (int64_t)q.kept + to + 1;
+    if (p.mask == nullptr && past < q.end) q.end = (int)past;
+    const int low = (int)((unsigned)min(begin_of(p, q.kept, p.mask == nullptr ? from + 1 : 0), q.end) & WHOLE);
+    const unsigned sinks = ((unsigned)min(p.sinks, q.end) + (TILE - 1)) & WHOLE;
+    q.split = (int)min(sinks, (unsigned)INT_MAX & WHOLE);
+    q.gap = low > q.split ? low - q.split : 0;
+    q.end -= q.gap;  // (low is not past it)
+}
+
+__device__ __forceinline__ Request request_of(const AttentionArgs &p, int r)
+{
+    Request q;
+    q.first = p.offsets[r];
+    const int end = min(p.offsets[r + 1], p.tokens);
+    q.fresh = (int)((unsigned)end - (unsigned)q.first);
+    if (q.first < 0 || end < q.first || q.fresh > p.max_new) q.fresh = 0;
+    q.kept = max(p.lens[r], 0);
+    q.end = (int)min((int64_t)q.kept + q.fresh, (int64_t)p.width * p.block_size);
+    q.split = q.gap = 0;
+    return q;
+}
+
+// Running sums over a wave, in the order of its lanes.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int moved(int x)
+{
+    return __builtin_amdgcn_update_dpp(0, x, CTRL, ROWS, 0xF, false);
+}
+__device__ __forceinline__ int wave_sums(int x)
+{
+    x += moved<0x111, 0xF>(x);  // one lane up, within 16
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);  // lanes 15 and 47 to the 16 after them
+    x += moved<0x143, 0xC>(x);  // lane 31 to the 32 after it
+    return x;
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float moved(float x)
+{
+    return __builtin_bit_cast(float, moved<CTRL, ROWS>(__builtin_bit_cast(int, x)));
+}
+__device__ __forceinline__ float wave_total(float x)
+{
+    x += moved<0x111, 0xF>(x);
+    x += moved<0x112, 0xF>(x);
+    x += moved<0x114, 0xF>(x);
+    x += moved<0x118, 0xF>(x);
+    x += moved<0x142, 0xA>(x);
+    x += moved<0x143, 0xC>(x);
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+
+// Run number x: keys [from, to) of request r, one of the n runs that begin
+// with number `first`; r = -1 where there is no such run.
+struct Run {
+    int r, n, first, from, to;
+    Request q;
+};
+
+// Every run but a request's last is of one length, a multiple of `step`:
+// the mean of all keys over p.target runs, so there are no more than
+// p.target + p.requests; a mean next to 2^31 or above makes one run of each
+// request.  The sum of the lengths is one in 24 bits; the
+// factor covers its rounding.
+//
+// With a window, a run that is all of a request's is that of the row tile: its
+// `rows` rows from row0 on alone say which keys it has.
+template <bool WINDOW, int TILE>
+__device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, int step, int row0, int rows)
+{
+    Run u;
+    if (p.target == 0) {
+        Request q = request_of(p, x);
+        if constexpr (WINDOW) {
+            const int last = (int)(min((int64_t)row0 + rows, (int64_t)q.fresh * p.share) - 1) / p.share;
+            if (q.fresh > 0 && row0 < q.fresh * p.share) bound_keys<TILE>(p, row0 / p.share, last, q);
+        }
+        u.q = {uniform(q.first), uniform(q.fresh), uniform(q.kept), uniform(q.end), uniform(q.split), uniform(q.gap)};
+        u.r = u.q.fresh > 0 ? x : -1;
+        u.n = 1;
+        u.first = x;
+        u.from = 0;
+        u.to = u.q.end;
+        return u;
+    }
+    float keys = 0.f;
+    Request q = {0, 0, 0, 0, 0, 0};
+    auto look = [&](int r) {
+        q = request_of(p, r);
+        if constexpr (WINDOW) bound_keys<TILE>(p, 0, q.fresh - 1, q);
+    };
+    for (int r = lane; r < p.requests; r += 64) {
+        look(r);
+        if (q.fresh > 0) keys += (float)q.end;
+    }
+    const float mean = wave_total(keys) / (float)p.target * 1.00001f;
+    int length = mean < (float)(INT_MAX / step * step - step) ? ((int)mean / step + 1) * step : INT_MAX;
+    if (length < SHORTEST) length = SHORTEST;
+    length = uniform(length);
+    u.r = -1;
+    int before = 0;
+    for (int base = 0; base < p.requests; base += 64) {
+        const int r = base + lane;
+        if (p.requests > 64 && r < p.requests) look(r);
+        int n = 0;
+        if (r < p.requests && q.fresh > 0) n = q.end > length ? (q.end - 1) / length + 1 : 1;
+        const int upto = wave_sums(n);
+        const uint64_t past = __ballot(before + upto > x);
+        if (past != 0) {
+            const int l = __ffsll((unsigned long long)past) - 1;
+            u.r = base + l;
+            u.n = __builtin_amdgcn_readlane(n, l);
+            u.first = before + __builtin_amdgcn_readlane(upto, l) - u.n;
+            u.from = (x - u.first) * length;
+            u.q = {__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.fresh, l), __builtin_amdgcn_readlane(q.kept, l),
+                   __builtin_amdgcn_readlane(q.end, l), WINDOW ? __builtin_amdgcn_readlane(q.split, l) : 0,
+                   WINDOW ? __builtin_amdgcn_readlane(q.gap, l) : 0};
+            u.to = u.q.end - u.from > length ? u.from + length : u.q.end;
+            return u;
+        }
+        before += __builtin_amdgcn_readlane(upto, 63);
+    }
+    return u;
+}
+
+// The larger one, NaN if either is: one instruction, where fmaxf takes
+// two more to make its operands quiet.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// Bits of 32 positions: those from number n on (below 0: all of them).
+__device__ __forceinline__ unsigned bits_from(int n) { return n <= 0 ? 0xFFFFFFFFu : n >= 32 ? 0u : 0xFFFFFFFFu << n; }
+
+// The new tokens in a mask that are among the last `window` places of a text of
+// `kept` cached tokens and these, or among its first `sinks`.
+__device__ __forceinline__ uint64_t bounded_mask(const AttentionArgs &p, int kept, uint64_t mask)
+{
+    const int64_t firsts = (int64_t)p.sinks - kept;
+    uint64_t out = mask;
+    for (int i = 0, drop = __popcll(mask) - p.window; i < drop; ++i) {
+        const uint64_t lowest = mask & (0 - mask);
+        mask ^= lowest;
+        if (i >= firsts) out ^= lowest;
+    }
+    return out;
+}
+
+// Four elements of a row of `n` runs, added in their order.  A run's maximum is
+// -infinity where the row sees none of its keys, and where all of its scores
+// are NaN: its sums, zeros or NaN, are added all the same.
+template <class T>
+__device__ __forceinline__ void join_runs(const float *sum_at, const float *top_at, const float *l_at, int64_t stride, int n, typename T::elem *to)
+{
+    typedef typename T::elem elem;
+    typedef elem four_t __attribute__((ext_vector_type(4)));
+    float m = -INFINITY, l = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < n; i += 4) {
+        f4 v[4];
+        float t[4], w[4], next = m;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const bool real = i + u < n;
+            const int64_t at = (real ? i + u : i) * stride;
+            const f4 sums = *reinterpret_cast<const f4 *>(sum_at + at);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[u][e] = real ? sums[e] : 0.f;
+            t[u] = real ? top_at[at] : -INFINITY;
+            w[u] = real ? l_at[at] : 0.f;
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) next = larger(next, t[u]);
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+        l *= keep;
+        o *= keep;
+        m = next;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const float share = t[u] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(t[u] - next);
+            l += share * w[u];
+            o += share * v[u];
+        }
+    }
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    four_t r4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+    *reinterpret_cast<four_t *>(to) = r4;
+}
+
+// A token's request and its runs: false where there is nothing to join.
+__device__ __forceinline__ bool runs_of(const AttentionArgs &p, int t, int lane, int &x0, int &n, Request &rq)
+{
+    int r = 0;  // the number of requests that end at or before t
+    for (int base = 0; base < p.requests; base += 64)
+        r += __popcll(__ballot(base + lane < p.requests && p.offsets[base + lane + 1] <= t));
+    if (r >= p.requests) return false;
+    x0 = p.first_run[2 * r];
+    n = p.first_run[2 * r + 1];
+    rq = request_of(p, r);
+    // (where offsets fall, the one that is found may not be the token's)
+    return rq.fresh != 0 && t >= rq.first && t - rq.first < rq.fresh && n > 1;
+}
+
+// The runs of a request, added in their order: many rows, each of few runs; a
+// workgroup a token, a thread four elements of a row.  Bound by reading the
+// sums, which other XCDs wrote: 32768 rows of 128, most of two or three runs, 8.8 us
+// (11.8 with a wave a row).
+template <class T>
+__global__ void __launch_bounds__(512) join_rows_kernel(AttentionArgs p, int tile_rows)
+{
+    const int t = blockIdx.x;
+    int x0, n;
+    Request rq;
+    if (!runs_of(p, t, threadIdx.x & 63, x0, n, rq)) return;
+    const int64_t tile_size = (int64_t)tile_rows * (p.dim + 2), stride = tile_size * p.heads * p.row_tiles;
+    const int fours = p.dim / 4;
+    for (int j = threadIdx.x; j < p.q_heads * fours; j += 512) {
+        const int head = j / fours, d = 4 * (j - head * fours), kv = head / p.share;
+        const int row = (t - rq.first) * p.share + head - kv * p.share, tile = row / tile_rows, in_tile = row - tile * tile_rows;
+        const float *part = p.part + (((int64_t)x0 * p.heads + kv) * p.row_tiles + tile) * tile_size, *top_at = part + tile_rows * p.dim + in_tile;
+        join_runs<T>(part + in_tile * p.dim + d, top_at, top_at + tile_rows, stride, n,
+                     static_cast<typename T::elem *>(p.out) + t * p.out_token + head * p.out_head + d);
+    }
+}
+
+// The same for few rows of many runs: one wave a token and query
+// head, lane l four elements of every (256 / DP)-th run: its share of the
+// weight comes from the lane that holds that run's maximum and sum.  Bound by
+// latency: 2048 rows of up to 9 runs 4.8 us.
+template <class T, int DP>
+__global__ void __launch_bounds__(256) join_kernel(AttentionArgs p, int tile_rows)
+{
+    typedef typename T::elem elem;
+    constexpr int FOURS = DP / 4, AT_ONCE = 64 / FOURS;
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + uniform(threadIdx.x >> 6);
+    const int t = (int)(id / p.q_heads), head = (int)(id - (int64_t)t * p.q_heads);
+    if (t >= p.tokens) return;
+    int x0, n;
+    Request rq;
+    if (!runs_of(p, t, lane, x0, n, rq)) return;
+    const int row = (t - rq.first) * p.share + head % p.share, tile = row / tile_rows, in_tile = row % tile_rows;
+    const int64_t tile_size = (int64_t)tile_rows * (p.dim + 2), stride = tile_size * p.heads * p.row_tiles;
+    const float *part = p.part + (((int64_t)x0 * p.heads + head / p.share) * p.row_tiles + tile) * tile_size;
+    const float *tops = part + tile_rows * p.dim + in_tile, *sums = tops + tile_rows;
+    const int d = 4 * (lane % FOURS), which = lane / FOURS;
+    const float *mine = part + (int64_t)in_tile * p.dim + (d < p.dim ? d : 0);
+    float m = -INFINITY, l = 0.f;
+    f4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int base = 0; base < n; base += 64) {
+        const int here = n - base < 64 ? n - base : 64;
+        const float top = lane < here ? tops[(base + lane) * stride] : -INFINITY;
+        const float sum = lane < here ? sums[(base + lane) * stride] : 0.f;
+        float next = top;
+        for (int s = 32; s; s >>= 1) next = larger(next, __shfl_xor(next, s));
+        next = larger(next, m);
+        const float keep = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - next);
+        const float share = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(top - next);
+        m = next;
+        l = l * keep + share * sum;
+        o *= keep;
+        for (int i = 0; i < here; i += 4 * AT_ONCE) {
+            f4 v[4];
+            float f[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int from = i + u * AT_ONCE + which;
+                const bool real = from < here;
+                f[u] = __shfl(share, from & 63);
+                const f4 sums = *reinterpret_cast<const f4 *>(mine + (base + (real ? from : 0)) * stride);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[u][e] = real ? sums[e] : 0.f;
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) o += f[u] * v[u];
+        }
+    }
+    for (int s = 32; s; s >>= 1) l += __shfl_xor(l, s);
+    for (int s = 32; s >= FOURS; s >>= 1)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += __shfl_xor(o[e], s);
+    if (which != 0 || d >= p.dim) return;
+    typedef elem four_t __attribute__((ext_vector_type(4)));
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+    four_t r4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+    *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + t * p.out_token + head * p.out_head + d) = r4;
+}
+
+constexpr float LOG2_E = 1.44269504088896340736f;
+
+// A workgroup's release writes back its XCD's L2: that costs less than the
+// second kernel while there are few runs of 16 rows (one request of 1000 keys:
+// 9.5 us against 10.8, two: 9.8 and 10.9), and more from about a hundred on (8
+// trees of 8, 128 of them: 17.0 us against 14.7; 64 requests of up to 8192: 94
+// and 81).
+constexpr int FEW_RUNS = 64;
+
+// The workspace begins with the counters, zeros whatever calls used it before.
+constexpr size_t COUNTERS = 65536, COUNTER_BYTES = COUNTERS * sizeof(int32_t);
+
+constexpr int SPLIT_REQUESTS = 1024;           // above that each request is one run
+
+// A thread for four elements from this many rows on (16 trees of 64, 32768 rows:
+// 54.7 us in all, 56.4 with a wave a row), a wave a row below (one request of
+// 32000 keys, 32 rows of 32 runs: 34.7 against 42.2; 2048 rows: 81.3 and 82.5).
+constexpr int JOIN_ROWS = 4096;
+
+// Joins the runs of every request, where the last workgroup has not.
+template <class T, int DP>
+gba_status launch_joins(const AttentionArgs &a, int tile_rows, hipStream_t s)
+{
+    if (a.tokens * (int64_t)a.q_heads >= JOIN_ROWS) return launch(join_rows_kernel<T>, dim3((unsigned)a.tokens), dim3(512), s, a, tile_rows);
+    return launch(join_kernel<T, DP>, dim3((unsigned)div_up((int64_t)a.tokens * a.q_heads, 4)), dim3(256), s, a, tile_rows);
+}
+
+}  // namespace
+}  // namespace gba

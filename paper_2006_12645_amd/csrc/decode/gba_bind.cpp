@@ -205,12 +205,14 @@ PyObject *store(PyObject *, PyObject *const *a, Py_ssize_t n)
 }
 
 // (cache, device, q, table, lens, offsets, max_new, mask, scale, out,
-// workspace, wants_workspace, stream): the output, or the bytes of a workspace
-// that is to be passed
+// workspace, wants_workspace, stream, and where there is a window it and the
+// sinks): the output, or the bytes of a workspace that is to be passed
 PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
 {
     HANDLE_TH_ERRORS
-    count_is(n, 13);
+    if (n != 13) count_is(n, 15);
+    const bool bounded = n == 15;
+    const int64_t window = bounded ? number(a[13]) : 0, sinks = bounded ? number(a[14]) : 0;
     gba_attention d;
     d.cache = *handle<gba_paged_cache>(a[0]);
     const int64_t device = number(a[1]);
@@ -266,10 +268,12 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
     }
     if (a[11] == Py_True) {
         size_t need = 0;
-        check(gba_tree_attention_workspace_size(&d, &need), "gba_tree_attention");
+        check(bounded ? gba_window_attention_workspace_size(&d, window, sinks, &need) : gba_tree_attention_workspace_size(&d, &need),
+              bounded ? "gba_window_attention" : "gba_tree_attention");
         if (need > d.workspace_bytes) return PyLong_FromSize_t(need);
     }
-    check(gba_tree_attention(&d, stream_of(a[12])), "gba_tree_attention");
+    if (bounded) check(gba_window_attention(&d, window, sinks, stream_of(a[12])), "gba_window_attention");
+    else check(gba_tree_attention(&d, stream_of(a[12])), "gba_tree_attention");
     return THPVariable_Wrap(std::move(out));
     END_HANDLE_TH_ERRORS
 }

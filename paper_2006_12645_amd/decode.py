@@ -232,7 +232,8 @@ def _more_scratch(nbytes, device, key):
     return _scratch[key]
 
 
-def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=None, out=None, workspace="auto", stream=None):
+def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, window=None, sinks=0, scale=None, out=None, workspace="auto",
+                   stream=None):
     """Attention of each request's new tokens over the cache.
 
     q: (tokens, q_heads, dim) of the cache's dtype, q_heads a multiple of the
@@ -240,8 +241,10 @@ def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=
     table (requests, width), lens (requests,) (cached tokens before the new
     ones), offsets (requests + 1,): int32.  max_new: no request has more new
     tokens.  mask: int64 (tokens, 1) or (tokens,), which of its request's new
-    tokens each one sees (a StepMaps'); None: those up to itself.  scale:
-    1 / sqrt(dim) by default.  workspace: "auto" (a scratch buffer of this
+    tokens each one sees (a StepMaps'); None: those up to itself.  window: a
+    token sees the last `window` positions of its text (the cached ones, then
+    the new ones that it sees; its own among them) and the first `sinks`; None:
+    all of them.  scale: 1 / sqrt(dim) by default.  workspace: "auto" (a scratch buffer of this
     stream, which a graph captured on it goes on using: its replays must not
     overlap the stream's other calls), None (long requests are not split) or a
     uint8 CUDA tensor, zeros before its first use.
@@ -249,15 +252,22 @@ def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, scale=
     """
     if stream is not None:
         with torch.cuda.stream(stream):
-            return tree_attention(q, cache, table, lens, offsets, max_new=max_new, mask=mask, scale=scale, out=out, workspace=workspace)
+            return tree_attention(q, cache, table, lens, offsets, max_new=max_new, mask=mask, window=window, sinks=sinks, scale=scale, out=out,
+                                  workspace=workspace)
     index = cache._index
     raw = _raw_stream(index)
     auto = isinstance(workspace, str)
     ws = _scratch.get((index, raw)) if auto else workspace
     if scale is None:
         scale = cache._scale
-    got = cache._attend(cache._at, index, q, table, lens, offsets, max_new, mask, scale, out, ws, auto, raw)
+    if window is not None:
+        bounds = (window, sinks)
+    elif sinks != 0:
+        raise ValueError("sinks come with a window")
+    else:
+        bounds = ()
+    got = cache._attend(cache._at, index, q, table, lens, offsets, max_new, mask, scale, out, ws, auto, raw, *bounds)
     if type(got) is int:  # the bytes that it needs
         ws = _more_scratch(got, cache.device, (index, raw))
-        got = cache._attend(cache._at, index, q, table, lens, offsets, max_new, mask, scale, out, ws, False, raw)
+        got = cache._attend(cache._at, index, q, table, lens, offsets, max_new, mask, scale, out, ws, False, raw, *bounds)
     return got

@@ -100,6 +100,8 @@ SIGNATURES = {
     "gba_cache_store": (_int, [ctypes.POINTER(PagedCacheDesc), _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp]),
     "gba_tree_attention": (_int, [ctypes.POINTER(AttentionDesc), _vp]),
     "gba_tree_attention_workspace_size": (_int, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
+    "gba_window_attention": (_int, [ctypes.POINTER(AttentionDesc), _i64, _i64, _vp]),
+    "gba_window_attention_workspace_size": (_int, [ctypes.POINTER(AttentionDesc), _i64, _i64, ctypes.POINTER(ctypes.c_size_t)]),
     "gba_status_string": (_cp, [_int]),
     "gba_version": (_cp, []),
 }
