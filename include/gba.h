@@ -624,6 +624,103 @@ gba_status gba_window_attention(const gba_attention *desc, int64_t window, int64
 gba_status gba_window_attention_workspace_size(const gba_attention *desc, int64_t window, int64_t sinks,
                                                size_t *bytes);
 
+/*
+ * gba_q4_cache -- keys and values of num_blocks * block_size tokens in 4 bits.
+ * With width = 64, 128 or 256, the smallest that is not below dim, and groups =
+ * max(1, width / group), element d of a key or value is
+ *     scale (code - 8) + offset
+ * of the scale and offset of group d / group of its row.  Storage, of K and V
+ * each, contiguous:
+ *   codes   32-bit words [num_blocks][heads][block_size][width / 8]: a word
+ *           holds the codes of eight elements, the e-th in the four bits from
+ *           4 e on.  V: word w of a row has elements 8 w ... 8 w + 7.  K: word
+ *           (width / 32) g + s of a row has elements 8 (4 s + g) ... + 7, for
+ *           g < 4.
+ *   scales  pairs of elements [num_blocks][heads][block_size][groups][2] of type
+ *           dtype: scale and offset.
+ * What stands past dim is not used.  A scale or an offset that is not finite
+ * makes the values of its group NaN.
+ * group 32, 64 or 128; dim a multiple of 8 up to 256; block_size a multiple of
+ * 16; arrays 16-byte aligned.
+ */
+typedef struct gba_q4_cache {
+    gba_dtype dtype;
+    int group;
+    int64_t num_blocks, block_size, heads, dim;
+    void *k_codes, *v_codes, *k_scales, *v_scales;
+} gba_q4_cache;
+
+/*
+ * gba_q4_cache_store -- gba_cache_store into a gba_q4_cache: the rows k[t], v[t]
+ * of every token t with a slot in the cache, rounded to 4 bits.  Of a group's
+ * elements v with the ends low and high, in fp32 (fl) and the cache's type (r16),
+ * to the nearest, ties to even:
+ *     scale  = r16( fl( fl(high / 2 - low / 2) * fl(2 / 15) ) ), 0 if below 2^-100
+ *     offset = r16( fl( low + 8 scale ) )
+ *     code   = fl( fl(v - offset) * fl(1 / scale) ) to the nearest whole number,
+ *              plus 8, at least 0 and at most 15; 8 if scale is 0
+ * A group with an infinity or a NaN has scale 0 and offset NaN.  Slots as in
+ * gba_cache_store: of two tokens with one slot, each word, and each pair of a
+ * scale and an offset, is one or the other's.
+ *
+ * gba_q4_cache_load -- back: row t of k and v becomes scale (code - 8) + offset
+ * of the elements at slots[t], rounded once, to no further than the type's
+ * largest finite value, or zeros where the slot is not in the cache.
+ *
+ * Strides in elements; dim is contiguous in k and v.
+ * Errors: GBA_EINVAL for cache == NULL, a bad enum or group, negative sizes,
+ * block_size < 1, a NULL pointer that is read or written; GBA_EUNSUPPORTED for
+ * other dims, block sizes or alignments, num_blocks * block_size or tokens above
+ * 2^31-1, or more than 65535 heads; GBA_EHIP if the launch fails.
+ */
+gba_status gba_q4_cache_store(const gba_q4_cache *cache, int64_t tokens, const void *k, int64_t k_token,
+                              int64_t k_head, const void *v, int64_t v_token, int64_t v_head,
+                              const int32_t *slots, gba_stream_t stream);
+gba_status gba_q4_cache_load(const gba_q4_cache *cache, int64_t tokens, const int32_t *slots, void *k,
+                             int64_t k_token, int64_t k_head, void *v, int64_t v_token, int64_t v_head,
+                             gba_stream_t stream);
+
+/*
+ * gba_q4_attention -- one request of gba_q4_attend: that of gba_tree_attention
+ * over a cache in 4 bits, with window 0, or of gba_window_attention.
+ */
+typedef struct gba_q4_attention {
+    gba_q4_cache cache;
+    int64_t requests, width;      /* rows and row length of the block table */
+    int64_t tokens;               /* rows of q, out and mask */
+    int64_t max_new;              /* no request has more new tokens than this */
+    int64_t q_heads;              /* a multiple of cache.heads */
+    int64_t window, sinks;        /* window 0: a token sees all of its text */
+    float scale;
+    const void *q;
+    int64_t q_token, q_head;
+    void *out;
+    int64_t out_token, out_head;
+    const int32_t *table;         /* [requests][width] */
+    const int32_t *lens;          /* [requests]: cached tokens before the new ones */
+    const int32_t *offsets;       /* [requests + 1]: rows of q of each request */
+    const uint64_t *mask;         /* [tokens], or NULL */
+    void *workspace;
+    size_t workspace_bytes;
+} gba_q4_attention;
+
+/*
+ * gba_q4_attend -- attention of each request's new tokens over a cache in 4
+ * bits: the formula of gba_tree_attention, or with a window that of
+ * gba_window_attention, for the values that the codes stand for.  Those are not
+ * rounded; the softmax weights enter the second product with 16 bits, and their
+ * sum is in fp32.  What is said there of positions that a token does not see, of
+ * missing blocks, rows of no request, offsets and the workspace holds here too.
+ * A row whose query is not finite is NaN.
+ *
+ * q and out 16-byte aligned with strides that are multiples of 8 (out: 4), but in
+ * dimensions of one element.
+ * Errors: those of gba_tree_attention and of gba_q4_cache_store, and GBA_EINVAL
+ * for window < 0 or sinks < 0.
+ */
+gba_status gba_q4_attend(const gba_q4_attention *desc, gba_stream_t stream);
+gba_status gba_q4_attend_workspace_size(const gba_q4_attention *desc, size_t *bytes);
+
 /* Static, human-readable name of a status code. */
 const char *gba_status_string(gba_status status);
 

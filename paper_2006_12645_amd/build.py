@@ -32,7 +32,8 @@ UNITS = [("gba_api.hip", [], "gba_api.o"), ("gba_thin_unit.hip", [], "gba_thin.o
      [f"-DGBA_LA={la}", f"-DGBA_LB={lb}", f"-DGBA_PRO={pro}", f"-DGBA_DUAL={dual}"],
      f"gba_gemm_{'RC'[la]}{'RC'[lb]}_p{pro}d{dual}.o")
     for la in (0, 1) for lb in (0, 1) for pro in (0, 1) for dual in (0, 1)] + [
-    (os.path.join("decode", f"gba_{name}.hip"), [], f"gba_{name}.o") for name in ("q4", "tables", "cache", "tree_attention", "window_attention")]
+    (os.path.join("decode", f"gba_{name}.hip"), [], f"gba_{name}.o") for name in ("q4", "tables", "cache", "tree_attention", "window_attention",
+                                                                                       "q4_cache", "q4_attention")]
 HIPCC_FLAGS = ["--offload-arch=" + ARCH, "-O3", "-std=c++17", "-fPIC", "-Wall",
                "-Wno-unused-function", "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
                "-I", INCLUDE, "-I", CSRC]

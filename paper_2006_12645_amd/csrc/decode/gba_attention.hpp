@@ -4,6 +4,7 @@
 #pragma once
 
 #include "gba_decode.hpp"
+#include "gba_kernel.hpp"
 
 namespace gba {
 namespace {
@@ -191,6 +192,27 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
 // two more to make its operands quiet.
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
+// The largest of the four lanes that hold one row.
+__device__ __forceinline__ float across_max(float x)
+{
+    x = larger(x, __shfl_xor(x, 32));
+    return larger(x, __shfl_xor(x, 16));
+}
+
+// Which of 32 keys from new token `first` on (below 0: from the cached ones)
+// a row sees, if they exist: the bits of its mask, or with no mask those up to
+// its own token; all cached ones.
+__device__ __forceinline__ unsigned seen_of(bool masked, uint64_t mask, int index, int first)
+{
+    if (first <= -32) return 0xFFFFFFFFu;
+    if (!masked) {
+        const int n = index - first + 1;
+        return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1;
+    }
+    if (first < 0) return (unsigned)(mask << -first) | ((1u << -first) - 1);
+    return first < 64 ? (unsigned)(mask >> first) : 0u;
+}
+
 // Bits of 32 positions: those from number n on (below 0: all of them).
 __device__ __forceinline__ unsigned bits_from(int n) { return n <= 0 ? 0xFFFFFFFFu : n >= 32 ? 0u : 0xFFFFFFFFu << n; }
 
@@ -249,6 +271,38 @@ __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_
 #pragma unroll
     for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
     *reinterpret_cast<four_t *>(to) = r4;
+}
+
+// A workgroup whose sums of one run, ROWS rows of `row_tile`, are written: the
+// one that is the request's last joins them all.  Every wave's stores are done
+// at the barrier; one thread's release makes them visible to other XCDs before
+// it counts the run, and who counts the last one acquires those of all others.
+template <class T, int DP, int ROWS, int THREADS>
+__device__ __forceinline__ void join_by_last(const AttentionArgs &p, const Run &run, const Request &rq, int head, int row_tile, int rows)
+{
+    __shared__ int last;
+    wait_vm_lgkm0<0>();
+    __syncthreads();
+    const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
+    if (threadIdx.x == 0) {
+        last = __hip_atomic_fetch_add(p.arrived + place, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
+        if (last) __hip_atomic_store(p.arrived + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
+    const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
+    constexpr int FOURS = DP / 4;
+    const int row0 = row_tile * ROWS;
+    for (int j = threadIdx.x; j < ROWS * FOURS; j += THREADS) {
+        const int row = j / FOURS, d = 4 * (j % FOURS);
+        if (row0 + row >= rows || d >= p.dim) continue;
+        const float *top_at = first_part + ROWS * p.dim + row;
+        const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
+        join_runs<T>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
+                     static_cast<typename T::elem *>(p.out) + token * p.out_token + h * p.out_head + d);
+    }
 }
 
 // A token's request and its runs: false where there is nothing to join.

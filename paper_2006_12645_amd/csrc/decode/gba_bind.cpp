@@ -204,17 +204,12 @@ PyObject *store(PyObject *, PyObject *const *a, Py_ssize_t n)
     END_HANDLE_TH_ERRORS
 }
 
-// (cache, device, q, table, lens, offsets, max_new, mask, scale, out,
-// workspace, wants_workspace, stream, and where there is a window it and the
-// sinks): the output, or the bytes of a workspace that is to be passed
-PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+// What a call of attention is given, into a gba_attention or gba_q4_attention
+// whose cache is set: false where the workspace is too small, and `need` says
+// what it needs.  The arguments are those of attend().
+template <class D, class Need>
+bool describe(D &d, PyObject *const *a, at::Tensor &out, const char *what, Need workspace_size, size_t &need)
 {
-    HANDLE_TH_ERRORS
-    if (n != 13) count_is(n, 15);
-    const bool bounded = n == 15;
-    const int64_t window = bounded ? number(a[13]) : 0, sinks = bounded ? number(a[14]) : 0;
-    gba_attention d;
-    d.cache = *handle<gba_paged_cache>(a[0]);
     const int64_t device = number(a[1]);
     const at::ScalarType type = type_of(d.cache.dtype);
     const at::Tensor &q = tensor(a[2], "q"), &table = tensor(a[3], "table"), &lens = tensor(a[4], "lens"), &offsets = tensor(a[5], "offsets");
@@ -242,7 +237,6 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
     d.scale = (float)scale;
     d.workspace = nullptr;
     d.workspace_bytes = 0;
-    at::Tensor out;
     if (a[9] != Py_None) {
         out = tensor(a[9], "out");
         on_gpu(out, "out", type, device);
@@ -266,15 +260,117 @@ PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
         d.workspace = w.mutable_data_ptr();
         d.workspace_bytes = (size_t)w.numel();
     }
-    if (a[11] == Py_True) {
-        size_t need = 0;
-        check(bounded ? gba_window_attention_workspace_size(&d, window, sinks, &need) : gba_tree_attention_workspace_size(&d, &need),
-              bounded ? "gba_window_attention" : "gba_tree_attention");
-        if (need > d.workspace_bytes) return PyLong_FromSize_t(need);
-    }
-    if (bounded) check(gba_window_attention(&d, window, sinks, stream_of(a[12])), "gba_window_attention");
-    else check(gba_tree_attention(&d, stream_of(a[12])), "gba_tree_attention");
+    if (a[11] != Py_True) return true;
+    need = 0;
+    check(workspace_size(need), what);
+    return need <= d.workspace_bytes;
+}
+
+// (cache, device, q, table, lens, offsets, max_new, mask, scale, out,
+// workspace, wants_workspace, stream, and where there is a window it and the
+// sinks): the output, or the bytes of a workspace that is to be passed
+PyObject *attend(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 13) count_is(n, 15);
+    const bool bounded = n == 15;
+    const int64_t window = bounded ? number(a[13]) : 0, sinks = bounded ? number(a[14]) : 0;
+    const char *what = bounded ? "gba_window_attention" : "gba_tree_attention";
+    gba_attention d;
+    d.cache = *handle<gba_paged_cache>(a[0]);
+    at::Tensor out;
+    size_t need;
+    const auto size = [&](size_t &bytes) {
+        return bounded ? gba_window_attention_workspace_size(&d, window, sinks, &bytes) : gba_tree_attention_workspace_size(&d, &bytes);
+    };
+    if (!describe(d, a, out, what, size, need)) return PyLong_FromSize_t(need);
+    check(bounded ? gba_window_attention(&d, window, sinks, stream_of(a[12])) : gba_tree_attention(&d, stream_of(a[12])), what);
     return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// The same over a cache in 4 bits.
+PyObject *attend_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    if (n != 13) count_is(n, 15);
+    gba_q4_attention d;
+    d.cache = *handle<gba_q4_cache>(a[0]);
+    d.window = d.sinks = 0;
+    if (n == 15) {
+        d.window = number(a[13]);
+        d.sinks = number(a[14]);
+        if (d.window < 1) check(GBA_EINVAL, "gba_q4_attend");  // (0 is none in C)
+    }
+    at::Tensor out;
+    size_t need;
+    if (!describe(d, a, out, "gba_q4_attend", [&](size_t &bytes) { return gba_q4_attend_workspace_size(&d, &bytes); }, need))
+        return PyLong_FromSize_t(need);
+    check(gba_q4_attend(&d, stream_of(a[12])), "gba_q4_attend");
+    return THPVariable_Wrap(std::move(out));
+    END_HANDLE_TH_ERRORS
+}
+
+// A (tokens, heads, dim) tensor of a cache's rows.
+template <class C>
+void token_rows(const at::Tensor &t, const char *name, const C *c, int64_t device, int64_t tokens)
+{
+    on_gpu(t, name, type_of(c->dtype), device);
+    if (t.dim() != 3 || t.size(0) != tokens || t.size(1) != c->heads || t.size(2) != c->dim)
+        refuse(PyExc_ValueError, "%s must be (%lld, %lld, %lld)", name, (long long)tokens, (long long)c->heads, (long long)c->dim);
+    if (c->dim > 1 && t.stride(2) != 1) refuse(PyExc_ValueError, "dim must be contiguous in %s", name);
+}
+
+int64_t slot_count(const at::Tensor &slots, int64_t device)
+{
+    on_gpu(slots, "slots", at::kInt, device);
+    if (slots.dim() != 1 || !slots.is_contiguous()) refuse(PyExc_ValueError, "slots must be a contiguous vector");
+    return slots.size(0);
+}
+
+// (cache, device, k, v, slots, stream), of a cache in 4 bits
+PyObject *store_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count_is(n, 6);
+    const gba_q4_cache *c = handle<gba_q4_cache>(a[0]);
+    const int64_t device = number(a[1]);
+    const at::Tensor &k = tensor(a[2], "k"), &v = tensor(a[3], "v"), &slots = tensor(a[4], "slots");
+    const int64_t tokens = slot_count(slots, device);
+    token_rows(k, "k", c, device, tokens);
+    token_rows(v, "v", c, device, tokens);
+    check(gba_q4_cache_store(c, tokens, k.const_data_ptr(), k.stride(0), k.stride(1), v.const_data_ptr(), v.stride(0), v.stride(1),
+                             slots.const_data_ptr<int32_t>(), stream_of(a[5])),
+          "gba_q4_cache_store");
+    Py_RETURN_NONE;
+    END_HANDLE_TH_ERRORS
+}
+
+// (cache, device, slots, k or None, v or None, stream): k and v
+PyObject *load_q4(PyObject *, PyObject *const *a, Py_ssize_t n)
+{
+    HANDLE_TH_ERRORS
+    count_is(n, 6);
+    const gba_q4_cache *c = handle<gba_q4_cache>(a[0]);
+    const int64_t device = number(a[1]);
+    const at::Tensor &slots = tensor(a[2], "slots");
+    const int64_t tokens = slot_count(slots, device);
+    at::Tensor out[2];
+    for (int i = 0; i < 2; ++i) {
+        if (a[3 + i] == Py_None) {
+            out[i] = at::empty({tokens, c->heads, c->dim}, slots.options().dtype(type_of(c->dtype)));
+        } else {
+            out[i] = tensor(a[3 + i], i ? "v" : "k");
+            token_rows(out[i], i ? "v" : "k", c, device, tokens);
+        }
+    }
+    check(gba_q4_cache_load(c, tokens, slots.const_data_ptr<int32_t>(), out[0].mutable_data_ptr(), out[0].stride(0), out[0].stride(1),
+                            out[1].mutable_data_ptr(), out[1].stride(0), out[1].stride(1), stream_of(a[5])),
+          "gba_q4_cache_load");
+    PyObject *both = PyTuple_New(2);
+    if (both == nullptr) throw python_error();
+    for (int i = 0; i < 2; ++i) PyTuple_SET_ITEM(both, i, THPVariable_Wrap(std::move(out[i])));
+    return both;
     END_HANDLE_TH_ERRORS
 }
 
@@ -289,6 +385,9 @@ PyMethodDef methods[] = {{"linear", reinterpret_cast<PyCFunction>(linear), METH_
                          {"step", reinterpret_cast<PyCFunction>(step), METH_FASTCALL, nullptr},
                          {"store", reinterpret_cast<PyCFunction>(store), METH_FASTCALL, nullptr},
                          {"attend", reinterpret_cast<PyCFunction>(attend), METH_FASTCALL, nullptr},
+                         {"store_q4", reinterpret_cast<PyCFunction>(store_q4), METH_FASTCALL, nullptr},
+                         {"load_q4", reinterpret_cast<PyCFunction>(load_q4), METH_FASTCALL, nullptr},
+                         {"attend_q4", reinterpret_cast<PyCFunction>(attend_q4), METH_FASTCALL, nullptr},
                          {"set_error", set_error, METH_O, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 

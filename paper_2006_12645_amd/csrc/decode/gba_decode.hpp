@@ -25,6 +25,7 @@ struct F16 {
     static constexpr int TOP = 6;                     // lowest bit of the four fraction bits that hold a code
     static constexpr unsigned INFINITE = 0x7C007C00u, EXPONENT_ONE = 0x04000400u;
     static constexpr float SLACK = 4.f, LIFT = 11.f;
+    static constexpr float LARGEST = 65504.f;
     static __device__ __forceinline__ f4 mfma(vec8 a, vec8 b, f4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0);
@@ -37,6 +38,7 @@ struct BF16 {
     static constexpr int TOP = 3;
     static constexpr unsigned INFINITE = 0x7F807F80u, EXPONENT_ONE = 0x00800080u;
     static constexpr float SLACK = 8.f, LIFT = 0.f;
+    static constexpr float LARGEST = 0x1.FEp127f;
     static __device__ __forceinline__ f4 mfma(vec8 a, vec8 b, f4 c)
     {
         return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);

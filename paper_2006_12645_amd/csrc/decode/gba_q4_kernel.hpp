@@ -1,0 +1,470 @@
+// gba_q4_kernel.hpp -- attention over the paged cache in 4 bits.
+//
+// A value is scale (code - 8) + offset, with a scale and an offset for a group
+// of dim.  Codes become 16-bit floats 16 + code by a shift, a mask and an or, and
+// nothing else of a value is rounded: with x the query and X its sum over a group
+//     k.x = sum over groups of scale (sum (16 + code) x - 24 X) + offset X
+//     sum p v = sum (p scale) (16 + code) - 24 sum p scale + sum p offset
+// the first sum of each is a matrix instruction's, the rest fp32.  Weights
+// p scale enter it as two bf16 numbers, the second one what the first's rounding
+// left: bf16 has the range that scales need, and two of them 16 bits.
+//
+// Tiles of 64 keys.  Key 16 g + 4 h + e of a tile is row 4 g + e of the h-th
+// 16-key product, so that lane group g has the scores of keys 16 g .. 16 g + 15:
+// those of one nibble-transposing LDS read, of which lane c gets element c of 16
+// rows.  Their scales and offsets are in the lanes of the same row, a key each,
+// and reach the others as row broadcasts.  K goes from the cache to registers as
+// the products take it, V through a wave's own part of LDS.
+#pragma once
+
+#include <type_traits>
+
+#include "gba_attention.hpp"
+#include "gba_q4_cache.hpp"
+
+namespace gba {
+namespace {
+
+constexpr int Q4_KEYS = 64;   // of a tile
+constexpr int Q4_WAVES = 4;   // take the tiles of a run in turn
+
+struct Q4Args : AttentionArgs {  // k, v: the codes
+    const void *k_scales, *v_scales;
+};
+
+// Eight codes as 16 + code, in the order 0 4 1 5 2 6 3 7.
+template <class T>
+__device__ __forceinline__ u4 unpacked(unsigned x)
+{
+    constexpr unsigned MASK = 0x000F000Fu << T::TOP;
+    u4 v;
+    v[0] = ((x << T::TOP) & MASK) | T::SIXTEEN;
+    v[1] = ((T::TOP >= 4 ? x << (T::TOP >= 4 ? T::TOP - 4 : 0) : x >> (T::TOP < 4 ? 4 - T::TOP : 0)) & MASK) | T::SIXTEEN;
+    v[2] = ((x >> (8 - T::TOP)) & MASK) | T::SIXTEEN;
+    v[3] = ((x >> (12 - T::TOP)) & MASK) | T::SIXTEEN;
+    return v;
+}
+
+// What lane J of the 16 lanes of a row holds.
+template <int J>
+__device__ __forceinline__ float from_lane(float x)
+{
+    return __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x150 + J, 0xF, 0xF, true));
+}
+
+__device__ __forceinline__ int64_t shuffled(int64_t v, int lane)
+{
+    const unsigned lo = __shfl((unsigned)v, lane), hi = __shfl((unsigned)(v >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+__device__ __forceinline__ int64_t from_lane_uniform(int64_t v, int lane)
+{
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)v, lane), hi = __builtin_amdgcn_readlane((unsigned)(v >> 32), lane);
+    return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+// The sum over the four lanes that hold one row.
+__device__ __forceinline__ float across_sum(float x)
+{
+    x += __shfl_xor(x, 32);
+    return x + __shfl_xor(x, 16);
+}
+
+// What is computed from these comes after what is written before: left to
+// itself the compiler makes every broadcast of a tile first, and runs out of
+// registers.
+__device__ __forceinline__ void in_order(float &a, float &b) { asm volatile("" : "+v"(a), "+v"(b)); }
+__device__ __forceinline__ void in_order(f4 &a) { asm volatile("" : "+v"(a)); }
+
+template <int N, class F>
+__device__ __forceinline__ void each(F f)
+{
+    if constexpr (N > 0) {
+        each<N - 1>(f);
+        f(std::integral_constant<int, N - 1>{});
+    }
+}
+
+// Bytes of a workgroup's LDS: V's tiles, then the waves' sums.
+template <int DP, int RT>
+constexpr int q4_lds_bytes()
+{
+    return Q4_WAVES * 16 * RT * 4 * DP;  // (V's tiles take 64 DP / 2 bytes a wave)
+}
+
+// DP: dim, padded.  G: groups of dim.  RT: blocks of 16 rows of a wave.
+template <class T, int DP, int G, int RT>
+__global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q4_attention_kernel(Q4Args p)
+{
+    typedef typename T::elem elem;
+    typedef typename T::vec8 vec8;
+    typedef elem pair_t __attribute__((ext_vector_type(2)));
+    constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = 16 * RT, ROW = DP / 2, TILE = Q4_KEYS * ROW, LOADS = TILE / 1024;
+    static_assert(TILE <= 16 * RT * 4 * DP, "the sums are no smaller than a tile of V");
+    __shared__ __attribute__((aligned(16))) char smem[q4_lds_bytes<DP, RT>()];
+    __shared__ float tops[Q4_WAVES][ROWS], sums[Q4_WAVES][ROWS];
+
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
+    // The row tiles of one run and head have ids 8 apart: the same XCD's L2.
+    const int xcd = blockIdx.x & 7, rest = blockIdx.x >> 3;
+    const int row_tile = rest % p.row_tiles, item = rest / p.row_tiles * 8 + xcd;
+    const int head = item % p.heads, x = item / p.heads;
+    if (x >= p.slots) return;
+    const int row0 = row_tile * ROWS;
+    const Run run = run_of<true, Q4_KEYS>(p, x, lane, Q4_KEYS * Q4_WAVES, row0, ROWS);
+    if (run.r < 0) return;
+    const Request rq = run.q;
+    const int rows = rq.fresh * p.share;
+    if (p.target != 0 && p.arrived == nullptr && run.first == x && head == 0 && row_tile == 0 && threadIdx.x == 0) {
+        p.first_run[2 * run.r] = x;
+        p.first_run[2 * run.r + 1] = run.n;
+    }
+    if (row0 >= rows) return;
+
+    // ---- tiles: 16 keys are in one block.  A lane looks up a quarter of one of
+    // the next 16 tiles: the row of its first key in the cache (row 0 where there
+    // is none: codes are finite whatever they are) and how many keys exist.
+    char *mine = smem + wave * (16 * RT * 4 * DP);
+    const int tiles = (int)(((unsigned)(run.to - run.from) + Q4_KEYS - 1) / Q4_KEYS);
+    const int count = tiles > wave ? (tiles - wave + Q4_WAVES - 1) / Q4_WAVES : 0;
+    const int32_t *entries = p.table + (int64_t)run.r * p.width;
+    auto key0 = [&](int n) -> unsigned { return (unsigned)run.from + Q4_KEYS * (unsigned)(wave + Q4_WAVES * n); };
+    int64_t first_row = 0;
+    unsigned keys = 0;
+    int looked_up = 0;
+    auto look_up = [&](int n) {
+        const unsigned pos = key0(n + lane / 4) + 16 * (lane & 3);
+        first_row = 0;
+        keys = 0;
+        if (pos < (unsigned)run.to) {
+            const unsigned at = position_of<true>(rq, pos);
+            const int page = (int)(at / (unsigned)p.block_size), within = (int)at - page * p.block_size, b = entries[page];
+            if (b >= 0 && b < p.num_blocks) {
+                first_row = ((int64_t)b * p.heads + head) * p.block_size + within;
+                keys = min((unsigned)run.to - pos, 16u);
+            }
+        }
+        looked_up = n;
+    };
+    typedef unsigned words_t __attribute__((ext_vector_type(STEPS < 4 ? STEPS : 4)));
+    constexpr int PIECES = STEPS <= 4 ? 1 : STEPS / 4;
+    words_t k_next[4][PIECES];
+    u4 v_next[LOADS];
+    pair_t ks_next[G], vs_next[G];
+    unsigned there_next = 0;  // of keys 16 g .. 16 g + 15, those that exist
+    const char *k_codes = static_cast<const char *>(p.k), *v_codes = static_cast<const char *>(p.v);
+    auto fetch = [&](int n) {
+        if (n - looked_up == 16) look_up(n);
+        const int at = 4 * (n - looked_up);
+        const char *k = k_codes + shuffled(first_row, at + (c >> 2)) * ROW + (c & 3) * ROW + g * (ROW / 4);
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int i = 0; i < PIECES; ++i) k_next[h][i] = *reinterpret_cast<const words_t *>(k + 4 * h * ROW + 16 * i);
+        const int64_t pairs = (shuffled(first_row, at + g) + c) * G;
+        there_next = (1u << __shfl(keys, at + g)) - 1;
+        typedef elem pairs_t __attribute__((ext_vector_type(2 * G)));
+        const pairs_t ks = *reinterpret_cast<const pairs_t *>(static_cast<const pair_t *>(p.k_scales) + pairs);
+        const pairs_t vs = *reinterpret_cast<const pairs_t *>(static_cast<const pair_t *>(p.v_scales) + pairs);
+#pragma unroll
+        for (int i = 0; i < G; ++i) {
+            ks_next[i] = pair_t{ks[2 * i], ks[2 * i + 1]};
+            vs_next[i] = pair_t{vs[2 * i], vs[2 * i + 1]};
+        }
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {  // 1 KB each: 2048 / DP sixteens of keys
+            if constexpr (DP == 64) {
+                const int64_t row = shuffled(first_row, at + 2 * i + (lane >> 5));
+                v_next[i] = *reinterpret_cast<const u4 *>(v_codes + row * ROW + 16 * (lane & 31));
+            } else {
+                const int64_t row = from_lane_uniform(first_row, at + i * 128 / DP);
+                v_next[i] = *reinterpret_cast<const u4 *>(v_codes + row * ROW + 1024 * (i % (DP / 128)) + 16 * lane);
+            }
+        }
+    };
+    if (count > 0) {
+        look_up(0);
+        fetch(0);
+    }
+
+    // ---- this wave's rows, row c of each block: the second operand, dim
+    // 32 s + 8 g on in the order of `unpacked`
+    vec8 query[RT][STEPS];
+    float X[RT][G];
+    uint64_t sees[RT];
+    int index[RT], begin[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        const int row = row0 + 16 * i + c;
+        const bool real = row < rows;
+        index[i] = real ? row / p.share : 0;
+        const int token = rq.first + index[i];
+        const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? row % p.share : 0)) * p.q_head;
+#pragma unroll
+        for (int j = 0; j < G; ++j) X[i][j] = 0.f;
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            const int d = 32 * s + 8 * g;
+            vec8 y = {};
+            if (real && d < p.dim) y = *reinterpret_cast<const vec8 *>(q + d);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const elem signed_y = p.sign != 1.f ? (elem)((float)y[e] * p.sign) : y[e];
+                query[i][s][2 * (e % 4) + e / 4] = signed_y;
+                X[i][s / (STEPS / G)] += (float)signed_y;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < G; ++j) X[i][j] = across_sum(X[i][j]);
+        sees[i] = p.mask != nullptr ? p.mask[token] : 0;
+        if (p.mask != nullptr && rq.fresh < 64) sees[i] &= ((uint64_t)1 << rq.fresh) - 1;
+        begin[i] = begin_of(p, rq.kept, p.mask != nullptr ? __popcll(sees[i]) : index[i] + 1);
+        if (p.mask != nullptr) sees[i] = bounded_mask(p, rq.kept, sees[i]);
+    }
+    const bool masked = p.mask != nullptr;
+    const int latest = begin_of(p, rq.kept, rq.fresh);
+
+    f4 out[RT][BLOCKS] = {};
+    // of the keys of this lane group: sums of weights, of weights times scales and times offsets
+    float total[RT], scales[RT][G], offsets[RT][G], top[RT], limit[RT], base2[RT];
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        top[i] = limit[i] = -INFINITY;
+        base2[i] = total[i] = 0.f;
+#pragma unroll
+        for (int j = 0; j < G; ++j) scales[i][j] = offsets[i][j] = 0.f;
+    }
+
+    // 16-byte chunk of a row of V in LDS: chunk ^ swap, over the banks
+    constexpr int CHUNKS = DP / 32;
+    auto swap_of = [](int row) { return DP == 64 ? (row >> 2) & 1 : DP == 128 ? (row >> 1) & 3 : row & 7; };
+    typedef int i2 __attribute__((ext_vector_type(2)));
+    typedef __attribute__((address_space(3))) i2 lds_i2;
+
+    for (int n = 0; n < count; ++n) {
+        float ksc[G], kof[G], vsc[G], vof[G];
+        unsigned k_now[4][STEPS];
+#pragma unroll
+        for (int h = 0; h < 4; ++h)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) k_now[h][s] = k_next[h][s / 4][s % 4];
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            ksc[j] = (float)ks_next[j][0];
+            kof[j] = (float)ks_next[j][1];
+            vsc[j] = (float)vs_next[j][0];
+            vof[j] = (float)vs_next[j][1];
+        }
+        const unsigned there = there_next;
+        lanes_meet();  // the last tile's V has been read
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int chunk = 64 * i + lane, row = chunk / CHUNKS;
+            *reinterpret_cast<u4 *>(mine + row * ROW + 16 * ((chunk % CHUNKS) ^ swap_of(row))) = v_next[i];
+        }
+        if (n + 1 < count) fetch(n + 1);
+        lanes_meet();
+
+        // ---- scores: keys 16 g + 4 h + e, row c of each block
+        f4 score[RT][4];
+        each<4>([&](auto half) {
+            constexpr int H = decltype(half)::value;
+            for (int j = 0; j < G; ++j) in_order(ksc[j], kof[j]);
+            f4 part[RT][G];
+#pragma unroll
+            for (int i = 0; i < RT; ++i)
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    const float start = -24.f * X[i][j];
+                    part[i][j] = f4{start, start, start, start};
+                }
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                const vec8 a = __builtin_bit_cast(vec8, unpacked<T>(k_now[H][s]));
+#pragma unroll
+                for (int i = 0; i < RT; ++i) part[i][s / (STEPS / G)] = T::mfma(a, query[i][s], part[i][s / (STEPS / G)]);
+            }
+            each<4>([&](auto element) {
+                constexpr int E = decltype(element)::value;
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    const float sc = from_lane<4 * H + E>(ksc[j]), of = from_lane<4 * H + E>(kof[j]);
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        const float scaled = j == 0 ? sc * part[i][j][E] : __builtin_fmaf(sc, part[i][j][E], score[i][H][E]);
+                        score[i][H][E] = __builtin_fmaf(of, X[i][j], scaled);
+                    }
+                }
+            });
+#pragma unroll
+            for (int i = 0; i < RT; ++i) in_order(score[i][H]);
+        });
+        // ---- which keys a row sees
+        const int first = (int)position_of<true>(rq, key0(n));
+        const bool edge = __ballot(there != 0xFFFFu) != 0 || first > rq.kept - Q4_KEYS || (first < latest && (unsigned)first + (Q4_KEYS - 1) >= (unsigned)p.sinks);
+        unsigned seen[RT];
+#pragma unroll
+        for (int i = 0; i < RT; ++i) seen[i] = 0xFFFFu;
+        if (edge) {
+            const int mine_first = first + 16 * g;
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                seen[i] = there & seen_of(masked, sees[i], index[i], mine_first - rq.kept) &
+                          (bits_from(begin[i] - mine_first) | ~bits_from(p.sinks - mine_first) | (masked ? bits_from(rq.kept - mine_first) : 0u));
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {  // (as bits: a score that is left out may be NaN)
+                    const float is = score[i][e / 4][e % 4];
+                    const unsigned bits = (seen[i] >> e) & 1 ? __builtin_bit_cast(unsigned, is) : 0xFF800000u;
+                    score[i][e / 4][e % 4] = __builtin_bit_cast(float, bits);
+                }
+            }
+        }
+        // What a value stands for whose scale or offset is not finite is NaN, and
+        // 0 times it has to be 0 where it is not seen: it is taken out, and the
+        // offsets of the rows that see it are NaN.
+        float odd = 0.f;
+#pragma unroll
+        for (int j = 0; j < G; ++j) odd += 0.f * vsc[j] + 0.f * vof[j];
+        if (__ballot(odd != 0.f)) {
+#pragma unroll
+            for (int j = 0; j < G; ++j) {
+                const bool is = 0.f * vsc[j] + 0.f * vof[j] != 0.f;
+                const unsigned which = (unsigned)(__ballot(is) >> (16 * g)) & 0xFFFFu;
+                if (is) vsc[j] = vof[j] = 0.f;
+#pragma unroll
+                for (int i = 0; i < RT; ++i)
+                    if (which & seen[i]) offsets[i][j] = NAN;
+            }
+        }
+        // ---- softmax: the maximum moves when a score passes it by 2^8
+        float most[RT];
+        bool past = false;
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+            most[i] = score[i][0][0];
+#pragma unroll
+            for (int e = 1; e < 16; ++e) most[i] = larger(most[i], score[i][e / 4][e % 4]);
+            most[i] *= p.scale2;
+            past |= most[i] > limit[i];
+        }
+        if (__ballot(past)) {
+#pragma unroll
+            for (int i = 0; i < RT; ++i) {
+                const float now = larger(across_max(most[i]), top[i]);
+                const float next = now == -INFINITY ? 0.f : now;
+                const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
+                top[i] = now;
+                limit[i] = now + 8.f;
+                base2[i] = next;
+                total[i] *= keep;
+#pragma unroll
+                for (int j = 0; j < G; ++j) {
+                    scales[i][j] *= keep;
+                    offsets[i][j] *= keep;
+                }
+#pragma unroll
+                for (int b = 0; b < BLOCKS; ++b) out[i][b] *= keep;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < RT; ++i)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                score[i][e / 4][e % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i][e / 4][e % 4], p.scale2, -base2[i]));
+                total[i] += score[i][e / 4][e % 4];
+            }
+        // ---- weights of each group and its blocks of dim
+        each<G>([&](auto group) {
+            constexpr int J = decltype(group)::value;
+            in_order(vsc[J], vof[J]);
+            BF16::vec8 high[RT][2], low[RT][2];
+            each<16>([&](auto key) {
+                constexpr int E = decltype(key)::value, H = E / 4;
+                const float sc = from_lane<E>(vsc[J]), of = from_lane<E>(vof[J]);
+#pragma unroll
+                for (int i = 0; i < RT; ++i) {
+                    const float w = score[i][H][E % 4] * sc;
+                    const __bf16 hi = (__bf16)w;
+                    scales[i][J] += w;
+                    offsets[i][J] = __builtin_fmaf(score[i][H][E % 4], of, offsets[i][J]);
+                    high[i][H / 2][2 * (E % 4) + H % 2] = hi;
+                    low[i][H / 2][2 * (E % 4) + H % 2] = (__bf16)(w - (float)hi);
+                }
+            });
+#pragma unroll
+            for (int b = J * (BLOCKS / G); b < (J + 1) * (BLOCKS / G); ++b) {
+                const int row = lane;  // 16 g + c
+                const i2 words = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2 *)(mine + row * ROW + 16 * ((b >> 1) ^ swap_of(row)) + 8 * (b & 1)));
+#pragma unroll
+                for (int half = 0; half < 2; ++half) {
+                    const BF16::vec8 v = __builtin_bit_cast(BF16::vec8, unpacked<BF16>((unsigned)words[half]));
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) {
+                        out[i][b] = BF16::mfma(v, high[i][half], out[i][b]);
+                        out[i][b] = BF16::mfma(v, low[i][half], out[i][b]);
+                    }
+                }
+            }
+        });
+    }
+
+    // ---- this wave's sums, joined with the others' through LDS: row c, chunks of
+    // four of dim, chunk j of a row at j ^ c
+    lanes_meet();
+#pragma unroll
+    for (int i = 0; i < RT; ++i) {
+        total[i] = across_sum(total[i]);
+        if (g == 0) {
+            tops[wave][16 * i + c] = top[i];
+            sums[wave][16 * i + c] = total[i];
+        }
+#pragma unroll
+        for (int j = 0; j < G; ++j) {
+            const float rest_of = across_sum(offsets[i][j]) - 24.f * across_sum(scales[i][j]);
+#pragma unroll
+            for (int b = j * (BLOCKS / G); b < (j + 1) * (BLOCKS / G); ++b) {
+                const f4 o = out[i][b] + rest_of;
+                *reinterpret_cast<f4 *>(mine + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = o;
+            }
+        }
+    }
+    __syncthreads();
+    const bool whole_request = run.n == 1;
+    typedef elem four_t __attribute__((ext_vector_type(4)));
+    float *part = whole_request ? nullptr : p.part + (((int64_t)x * p.heads + head) * p.row_tiles + row_tile) * ROWS * (int64_t)(p.dim + 2);
+    constexpr int FOURS = DP / 4;
+    for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * Q4_WAVES) {
+        const int row = j / FOURS, four = j % FOURS, d = 4 * four;
+        if (row0 + row >= rows || d >= p.dim) continue;
+        float m = tops[0][row];
+#pragma unroll
+        for (int w = 1; w < Q4_WAVES; ++w) m = larger(m, tops[w][row]);
+        f4 o = {0.f, 0.f, 0.f, 0.f};
+        float l = 0.f;
+#pragma unroll
+        for (int w = 0; w < Q4_WAVES; ++w) {
+            const float share = tops[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[w][row] - m);
+            l += share * sums[w][row];
+            o += share * *reinterpret_cast<const f4 *>(smem + w * (16 * RT * 4 * DP) + row * (4 * DP) + 16 * (four ^ (row & 15)));
+        }
+        if (whole_request) {
+            const float inv = l > 0.f ? 1.f / l : 0.f;
+            const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
+            four_t r4;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
+            *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r4;
+        } else {
+            *reinterpret_cast<f4 *>(part + row * p.dim + d) = o;
+            if (four == 0) {
+                part[ROWS * p.dim + row] = m;
+                part[ROWS * (p.dim + 1) + row] = l;
+            }
+        }
+    }
+    if (whole_request || p.arrived == nullptr) return;
+    join_by_last<T, DP, ROWS, 64 * Q4_WAVES>(p, run, rq, head, row_tile, rows);
+}
+
+}  // namespace
+}  // namespace gba

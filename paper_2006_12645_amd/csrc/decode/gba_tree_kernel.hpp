@@ -55,27 +55,6 @@ __device__ __forceinline__ int swap_v(int key)
     return DP == 64 ? ((key >> 1) & 3) << 1 : (key & 7) << 1;
 }
 
-// The largest of the four lanes that hold one row.
-__device__ __forceinline__ float across_max(float x)
-{
-    x = larger(x, __shfl_xor(x, 32));
-    return larger(x, __shfl_xor(x, 16));
-}
-
-// Which of 32 keys from new token `first` on (below 0: from the cached ones)
-// a row sees, if they exist: the bits of its mask, or with no mask those up to
-// its own token; all cached ones.
-__device__ __forceinline__ unsigned seen_of(bool masked, uint64_t mask, int index, int first)
-{
-    if (first <= -32) return 0xFFFFFFFFu;
-    if (!masked) {
-        const int n = index - first + 1;
-        return n <= 0 ? 0u : n >= 32 ? 0xFFFFFFFFu : (1u << n) - 1;
-    }
-    if (first < 0) return (unsigned)(mask << -first) | ((1u << -first) - 1);
-    return first < 64 ? (unsigned)(mask >> first) : 0u;
-}
-
 // Reads of 16 bytes, OFF bytes past each address, in one block of assembly that
 // waits for them: before a load from LDS of its own the compiler waits for
 // every copy to LDS that is under way, the next tile's too.
@@ -704,30 +683,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     }
     if constexpr (RG <= 2) {
         if (whole_request || p.arrived == nullptr) return;
-        // Every wave's stores are done at the barrier; one thread's release
-        // makes them visible to other XCDs before it counts the run, and who
-        // counts the last one acquires those of all others.
-        __shared__ int last;
-        wait_vm_lgkm0<0>();
-        __syncthreads();
-        const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
-        if (threadIdx.x == 0) {
-            last = __hip_atomic_fetch_add(p.arrived + place, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
-            if (last) __hip_atomic_store(p.arrived + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (!last) return;
-        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
-        const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
-        const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
-        for (int j = threadIdx.x; j < ROWS * FOURS; j += 64 * WAVES) {
-            const int row = j / FOURS, d = 4 * (j % FOURS);
-            if (row0 + row >= rows || d >= p.dim) continue;
-            const float *top_at = first_part + ROWS * p.dim + row;
-            const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
-            join_runs<T>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
-                         static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d);
-        }
+        join_by_last<T, DP, ROWS, 64 * WAVES>(p, run, rq, head, row_tile, rows);
     }
 }
 

@@ -4,8 +4,8 @@ each request's new tokens over it (one token, a chain or a tree of drafts).
 
 Argument marshalling over libgba.so, like :mod:`paper_2006_12645_amd.gba`:
 every step of the computation is a HIP kernel, launched on `stream` or torch's
-current one.  The stored forms are those of include/gba.h.  The three handles
-(Q4Weight, BlockTables, PagedCache) check the tensors a program keeps once and
+current one.  The stored forms are those of include/gba.h.  The four handles
+(Q4Weight, BlockTables, PagedCache, Q4Cache) check the tensors a program keeps once and
 hold them; a call checks what it is given, in the extension _gba_decode, since
 these calls are bound by the host.  Calls read nothing back from the GPU and may
 be captured in a HIP graph.
@@ -210,6 +210,66 @@ class PagedCache:
         self._store(self._at, self._index, k, v, slots, _raw_stream(self._index) if stream is None else stream.cuda_stream)
 
 
+class Q4Cache:
+    """A PagedCache in 4 bits: an element is scale (code - 8) + offset, with a
+    scale and an offset for every `group` (32, 64 or 128) elements of a key or
+    value.
+
+    k, v: uint8 (num_blocks, heads, block_size, width / 2), two codes a byte;
+    k_scales, v_scales: fp16 or bf16 (num_blocks, heads, block_size, groups, 2),
+    scale and offset.  width is 64, 128 or 256, the smallest that holds dim, and
+    groups max(1, width / group); gba_q4_cache says where each element is.
+    block_size is a multiple of 16, dim of 8.
+    """
+
+    def __init__(self, k, v, k_scales, v_scales, *, dim, group=64):
+        if group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        if dim % 8 or not 0 < dim <= 256:
+            raise ValueError("dim must be a multiple of 8 up to 256")
+        _gpu("k", k, torch.uint8)
+        if k_scales.dtype not in DTYPES:
+            raise TypeError("k_scales must be a float16 or bfloat16 CUDA tensor")
+        width = 64 if dim <= 64 else 128 if dim <= 128 else 256
+        if k.dim() != 4 or k.shape[2] == 0 or k.shape[2] % 16:
+            raise ValueError(f"k must be (num_blocks, heads, a multiple of 16, {width // 2})")
+        codes, scales = (*k.shape[:3], width // 2), (*k.shape[:3], max(1, width // group), 2)
+        for name, t, dtype, shape in (("k", k, torch.uint8, codes), ("v", v, torch.uint8, codes),
+                                      ("k_scales", k_scales, k_scales.dtype, scales), ("v_scales", v_scales, k_scales.dtype, scales)):
+            _gpu(name, t, dtype, k.device)
+            if t.shape != shape or not t.is_contiguous():
+                raise ValueError(f"{name} must be a contiguous {tuple(shape)} tensor, got {tuple(t.shape)}")
+        self.k, self.v, self.k_scales, self.v_scales = k, v, k_scales, v_scales
+        self.num_blocks, self.heads, self.block_size, self.dim, self.group = *k.shape[:3], dim, group
+        self.dtype, self.device, self._scale = k_scales.dtype, k.device, 1.0 / math.sqrt(dim)
+        self._desc = gba.Q4CacheDesc(DTYPES[self.dtype], group, self.num_blocks, self.block_size, self.heads, dim, k.data_ptr(), v.data_ptr(),
+                                     k_scales.data_ptr(), v_scales.data_ptr())
+        self._at, self._index = ctypes.addressof(self._desc), k.device.index
+        self._store, self._load, self._attend = _calls().store_q4, _calls().load_q4, _calls().attend_q4
+
+    @classmethod
+    def empty(cls, num_blocks, block_size, heads, dim, dtype, *, group=64, device="cuda"):
+        """A cache that holds nothing yet."""
+        width = 64 if dim <= 64 else 128 if dim <= 128 else 256
+        lead = (num_blocks, heads, block_size)
+        codes = [torch.empty((*lead, width // 2), dtype=torch.uint8, device=device) for _ in range(2)]
+        scales = [torch.empty((*lead, max(1, width // group), 2), dtype=dtype, device=device) for _ in range(2)]
+        return cls(*codes, *scales, dim=dim, group=group)
+
+    def store(self, k, v, slots, stream=None):
+        """Round the rows k[t], v[t] (tokens, heads, dim) to 4 bits at slots[t],
+        as PagedCache.store does (see gba_q4_cache_store)."""
+        self._store(self._at, self._index, k, v, slots, _raw_stream(self._index) if stream is None else stream.cuda_stream)
+
+    def load(self, slots, k=None, v=None, stream=None):
+        """The rows at slots (int32), (tokens, heads, dim) each, into k and v
+        (allocated when None): zeros where the slot is outside the cache."""
+        if stream is not None:
+            with torch.cuda.stream(stream):
+                return self._load(self._at, self._index, slots, k, v, stream.cuda_stream)
+        return self._load(self._at, self._index, slots, k, v, _raw_stream(self._index))
+
+
 # Scratch of calls with workspace="auto", one per (device, stream): calls in a
 # stream's order share one.  A smaller one that was replaced is kept, since a
 # graph captured earlier may hold its address; as sizes at least double, those
@@ -236,8 +296,8 @@ def tree_attention(q, cache, table, lens, offsets, *, max_new, mask=None, window
                    stream=None):
     """Attention of each request's new tokens over the cache.
 
-    q: (tokens, q_heads, dim) of the cache's dtype, q_heads a multiple of the
-    cache's heads; the keys and values of the tokens are in the cache already.
+    cache: a PagedCache or a Q4Cache.  q: (tokens, q_heads, dim) of the cache's
+    dtype, q_heads a multiple of the cache's heads; the keys and values of the tokens are in the cache already.
     table (requests, width), lens (requests,) (cached tokens before the new
     ones), offsets (requests + 1,): int32.  max_new: no request has more new
     tokens.  mask: int64 (tokens, 1) or (tokens,), which of its request's new

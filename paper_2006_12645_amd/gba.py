@@ -74,6 +74,20 @@ class AttentionDesc(ctypes.Structure):
                 ("mask", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
 
 
+class Q4CacheDesc(ctypes.Structure):
+    """Mirror of struct gba_q4_cache."""
+    _fields_ = [("dtype", _int), ("group", _int), ("num_blocks", _i64), ("block_size", _i64), ("heads", _i64), ("dim", _i64),
+                ("k_codes", _vp), ("v_codes", _vp), ("k_scales", _vp), ("v_scales", _vp)]
+
+
+class Q4AttentionDesc(ctypes.Structure):
+    """Mirror of struct gba_q4_attention."""
+    _fields_ = [("cache", Q4CacheDesc), ("requests", _i64), ("width", _i64), ("tokens", _i64), ("max_new", _i64),
+                ("q_heads", _i64), ("window", _i64), ("sinks", _i64), ("scale", ctypes.c_float), ("q", _vp), ("q_token", _i64),
+                ("q_head", _i64), ("out", _vp), ("out_token", _i64), ("out_head", _i64), ("table", _vp), ("lens", _vp),
+                ("offsets", _vp), ("mask", _vp), ("workspace", _vp), ("workspace_bytes", ctypes.c_size_t)]
+
+
 PATHS = ("empty", "tile", "deep", "few_rows", "unaligned", "general")  # enum gba_path
 
 # Every function include/gba.h declares, with its ctypes signature.
@@ -102,6 +116,10 @@ SIGNATURES = {
     "gba_tree_attention_workspace_size": (_int, [ctypes.POINTER(AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "gba_window_attention": (_int, [ctypes.POINTER(AttentionDesc), _i64, _i64, _vp]),
     "gba_window_attention_workspace_size": (_int, [ctypes.POINTER(AttentionDesc), _i64, _i64, ctypes.POINTER(ctypes.c_size_t)]),
+    "gba_q4_cache_store": (_int, [ctypes.POINTER(Q4CacheDesc), _i64, _vp, _i64, _i64, _vp, _i64, _i64, _vp, _vp]),
+    "gba_q4_cache_load": (_int, [ctypes.POINTER(Q4CacheDesc), _i64, _vp, _vp, _i64, _i64, _vp, _i64, _i64, _vp]),
+    "gba_q4_attend": (_int, [ctypes.POINTER(Q4AttentionDesc), _vp]),
+    "gba_q4_attend_workspace_size": (_int, [ctypes.POINTER(Q4AttentionDesc), ctypes.POINTER(ctypes.c_size_t)]),
     "gba_status_string": (_cp, [_int]),
     "gba_version": (_cp, []),
 }
