@@ -22,6 +22,7 @@ struct AttentionArgs {
     int row_tiles;     // of a request and head
     int slots;         // runs of keys there is room for: at least as many as there are
     int target;        // runs to aim at (0: one for each request)
+    int length, each;  // (windows only) if not 0: keys of a run, and how many of them are set aside for each request
     int32_t *arrived;    // [slots][heads][row_tiles], zeros: runs that have ended, at a request's first one; or null
     int32_t *first_run;  // [requests][2]: a request's first run and how many it has
     float *part;       // [slots][heads][row_tiles]: rows x dim sums, then as many maxima and sums of weights
@@ -148,6 +149,23 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
         u.to = u.q.end;
         return u;
     }
+    u.r = -1;
+    if constexpr (WINDOW) {
+        if (p.length != 0) {
+            const int r = x / p.each, i = x - r * p.each;
+            Request q = request_of(p, r);
+            if (q.fresh == 0) return u;
+            bound_keys<TILE>(p, 0, q.fresh - 1, q);
+            u.q = {uniform(q.first), uniform(q.fresh), uniform(q.kept), uniform(q.end), uniform(q.split), uniform(q.gap)};
+            u.n = u.q.end > p.length ? (u.q.end - 1) / p.length + 1 : 1;
+            if (i >= u.n) return u;
+            u.r = r;
+            u.first = x - i;
+            u.from = i * p.length;
+            u.to = u.q.end - u.from > p.length ? u.from + p.length : u.q.end;
+            return u;
+        }
+    }
     float keys = 0.f;
     Request q = {0, 0, 0, 0, 0, 0};
     auto look = [&](int r) {
@@ -162,7 +180,6 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
     int length = mean < (float)(INT_MAX / step * step - step) ? ((int)mean / step + 1) * step : INT_MAX;
     if (length < SHORTEST) length = SHORTEST;
     length = uniform(length);
-    u.r = -1;
     int before = 0;
     for (int base = 0; base < p.requests; base += 64) {
         const int r = base + lane;
@@ -213,6 +230,14 @@ __device__ __forceinline__ unsigned seen_of(bool masked, uint64_t mask, int inde
     return first < 64 ? (unsigned)(mask >> first) : 0u;
 }
 
+// Two 16-bit floats: 0x8000 for each that is infinite or NaN (the exponent's top
+// carries into the sign's place).
+template <class T>
+__device__ __forceinline__ unsigned not_finite(unsigned w)
+{
+    return ((w & T::INFINITE) + T::EXPONENT_ONE) & 0x80008000u;
+}
+
 // Bits of 32 positions: those from number n on (below 0: all of them).
 __device__ __forceinline__ unsigned bits_from(int n) { return n <= 0 ? 0xFFFFFFFFu : n >= 32 ? 0u : 0xFFFFFFFFu << n; }
 
@@ -230,10 +255,39 @@ __device__ __forceinline__ uint64_t bounded_mask(const AttentionArgs &p, int kep
     return out;
 }
 
+// Stores that write through to where every XCD sees them, and loads from there:
+// a workgroup that has written its sums so need not write back its XCD's L2
+// before another one reads them, which costs more than the sums.
+__device__ __forceinline__ void to_other_xcds(float *to, float x) { __hip_atomic_store(to, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void to_other_xcds(float *to, f4 x)
+{
+    typedef uint64_t l2 __attribute__((ext_vector_type(2)));
+    const l2 v = __builtin_bit_cast(l2, x);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(to), v[0], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __hip_atomic_store(reinterpret_cast<uint64_t *>(to) + 1, v[1], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+template <bool OTHERS>
+__device__ __forceinline__ float load_one(const float *at)
+{
+    return OTHERS ? __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : *at;
+}
+template <bool OTHERS>
+__device__ __forceinline__ f4 load_four(const float *at)
+{
+    if constexpr (!OTHERS) {
+        return *reinterpret_cast<const f4 *>(at);
+    } else {
+        typedef uint64_t l2 __attribute__((ext_vector_type(2)));
+        const uint64_t *p = reinterpret_cast<const uint64_t *>(at);
+        return __builtin_bit_cast(f4, l2{__hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT),
+                                         __hip_atomic_load(p + 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT)});
+    }
+}
+
 // Four elements of a row of `n` runs, added in their order.  A run's maximum is
 // -infinity where the row sees none of its keys, and where all of its scores
 // are NaN: its sums, zeros or NaN, are added all the same.
-template <class T>
+template <class T, bool OTHERS = false>
 __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_at, const float *l_at, int64_t stride, int n, typename T::elem *to)
 {
     typedef typename T::elem elem;
@@ -247,11 +301,12 @@ __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_
         for (int u = 0; u < 4; ++u) {
             const bool real = i + u < n;
             const int64_t at = (real ? i + u : i) * stride;
-            const f4 sums = *reinterpret_cast<const f4 *>(sum_at + at);
+            const f4 sums = load_four<OTHERS>(sum_at + at);
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[u][e] = real ? sums[e] : 0.f;
-            t[u] = real ? top_at[at] : -INFINITY;
-            w[u] = real ? l_at[at] : 0.f;
+            const float its_top = load_one<OTHERS>(top_at + at), its_l = load_one<OTHERS>(l_at + at);
+            t[u] = real ? its_top : -INFINITY;
+            w[u] = real ? its_l : 0.f;
         }
 #pragma unroll
         for (int u = 0; u < 4; ++u) next = larger(next, t[u]);
@@ -301,6 +356,35 @@ __device__ __forceinline__ void join_by_last(const AttentionArgs &p, const Run &
         const float *top_at = first_part + ROWS * p.dim + row;
         const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
         join_runs<T>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
+                     static_cast<typename T::elem *>(p.out) + token * p.out_token + h * p.out_head + d);
+    }
+}
+
+// The same where the sums were written with to_other_xcds: every wave waits for
+// its stores, and the count needs no release.
+template <class T, int DP, int ROWS, int THREADS>
+__device__ __forceinline__ void join_written_through(const AttentionArgs &p, const Run &run, const Request &rq, int head, int row_tile, int rows)
+{
+    __shared__ int last;
+    wait_vm_lgkm0<0>();
+    __syncthreads();
+    const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
+    if (threadIdx.x == 0) {
+        last = __hip_atomic_fetch_add(p.arrived + place, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
+        if (last) __hip_atomic_store(p.arrived + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    if (!last) return;
+    const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
+    const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
+    constexpr int FOURS = DP / 4;
+    const int row0 = row_tile * ROWS;
+    for (int j = threadIdx.x; j < ROWS * FOURS; j += THREADS) {
+        const int row = j / FOURS, d = 4 * (j % FOURS);
+        if (row0 + row >= rows || d >= p.dim) continue;
+        const float *top_at = first_part + ROWS * p.dim + row;
+        const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
+        join_runs<T, true>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
                      static_cast<typename T::elem *>(p.out) + token * p.out_token + h * p.out_head + d);
     }
 }
@@ -419,6 +503,26 @@ constexpr int FEW_RUNS = 64;
 constexpr size_t COUNTERS = 65536, COUNTER_BYTES = COUNTERS * sizeof(int32_t);
 
 constexpr int SPLIT_REQUESTS = 1024;           // above that each request is one run
+
+inline int64_t min_of(int64_t a, int64_t b) { return a < b ? a : b; }
+
+// Into how many runs windows of `keys` keys at most are cut, for `pairs` of a
+// request's rows and a head where `room` workgroups run at once: what takes the
+// fewest rounds of them, each as long as a run and, for what a workgroup does
+// beside its keys, `fixed` keys more.
+inline int64_t runs_of_window(int64_t pairs, int64_t keys, int64_t room, int64_t fixed)
+{
+    int64_t best = 1, least = INT64_MAX;
+    for (int64_t n = 1; n <= 256 && n <= div_up(keys, SHORTEST); ++n) {
+        const int64_t length = div_up(div_up(keys, n), SHORTEST) * SHORTEST;
+        const int64_t cost = div_up(pairs * div_up(keys, length), room) * (length + fixed);
+        if (cost < least) {
+            least = cost;
+            best = n;
+        }
+    }
+    return best;
+}
 
 // A thread for four elements from this many rows on (16 trees of 64, 32768 rows:
 // 54.7 us in all, 56.4 with a wave a row), a wave a row below (one request of

@@ -5,8 +5,6 @@
 namespace gba {
 namespace {
 
-int64_t min_of(int64_t a, int64_t b) { return a < b ? a : b; }
-
 // No request has more new tokens than there are rows.
 int64_t most_new(const gba_q4_attention &d) { return min_of(d.max_new, d.tokens); }
 
@@ -43,18 +41,21 @@ gba_status validate(const gba_q4_attention &d)
     return GBA_OK;
 }
 
+// What a workgroup does beside its keys, as keys.
+constexpr int64_t FIXED_KEYS = 512;
+
 struct Shape {
-    int dp, groups, rt, row_tiles, target, slots;
-    bool counts;           // runs are joined by the workgroup that ends last
-    size_t header, bytes;  // of the workspace: what stands before the sums, all
+    int dp, groups, rt, row_tiles, target, slots, length, each;
+    size_t bytes;  // of the workspace: counters, then the sums
 };
 
-// Runs to aim at.
-int64_t runs_to_aim_at(const gba_q4_attention &d, int row_tiles)
-{
-    const int64_t pairs = d.requests * d.cache.heads * row_tiles;
-    return pairs <= 128 ? 512 : pairs < 1024 ? 1024 : 2048;
-}
+// Runs to aim at.  A compute unit has room for two workgroups or more, and each
+// request and head adds half a run on average, its last one: few requests, all
+// runs at once (four of up to 131071 keys, 32 pairs of request and head: 103 us
+// with 512, 129 with 768, where some wait for others); more of them, two rounds,
+// to even out (64 of up to 8192, 512 pairs: 38 us with 256, 34 with 512, 31 with
+// 768).
+int64_t runs_to_aim_at(int64_t pairs) { return pairs <= 128 ? 512 : pairs < 1024 ? 768 : 2048; }
 
 Shape shape_of(const gba_q4_attention &d)
 {
@@ -67,22 +68,30 @@ Shape shape_of(const gba_q4_attention &d)
     s.row_tiles = (int)div_up(rows, 16 * s.rt);
     s.target = 0;
     s.slots = (int)d.requests;
-    s.counts = false;
-    s.header = s.bytes = 0;
+    s.length = s.each = 0;
+    s.bytes = 0;
     int64_t most_keys = d.width * c.block_size;  // of a request
     const int64_t bounded = min_of(d.window, INT_MAX) + min_of(d.sinks, INT_MAX);
-    if (d.window != 0) most_keys = min_of(most_keys, bounded + most_new(d));
+    if (d.window != 0) most_keys = min_of(most_keys, bounded + most_new(d) + 2 * Q4_KEYS);  // (sinks and window in whole tiles)
     // Tiles of rows that fill the chip, or have few keys, are left whole, with the keys that their own rows see.
     const int64_t tokens = div_up(16 * s.rt * c.heads, d.q_heads);
     const bool alone = s.row_tiles > 1 && (d.requests * c.heads * s.row_tiles >= 512 || (d.window != 0 && bounded + tokens <= 1024));
-    if (d.requests <= SPLIT_REQUESTS && most_keys > SHORTEST && !alone) {
-        s.target = (int)div_up(runs_to_aim_at(d, s.row_tiles), c.heads * (int64_t)s.row_tiles);
-        s.slots = (int)d.requests + s.target;
-        s.counts = s.rt * d.requests * c.heads * s.row_tiles * div_up(most_keys, SHORTEST) <= FEW_RUNS &&
-                   (size_t)s.slots * c.heads * s.row_tiles <= COUNTERS;
-        s.header = COUNTER_BYTES + (size_t)div_up(d.requests * 8, 256) * 256;
-        s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt) * (c.dim + 2) * sizeof(float);
+    if (d.requests > SPLIT_REQUESTS || most_keys <= SHORTEST || alone) return s;
+    const int64_t tiles = c.heads * (int64_t)s.row_tiles, pairs = d.requests * tiles;
+    int64_t slots = 0;
+    if (d.window != 0) {
+        const int64_t n = runs_of_window(pairs, most_keys, 256, FIXED_KEYS);
+        s.length = (int)(div_up(div_up(most_keys, n), SHORTEST) * SHORTEST);
+        s.each = (int)div_up(most_keys, s.length);
+        slots = d.requests * s.each;
+    } else {
+        slots = d.requests + div_up(runs_to_aim_at(pairs), tiles);
     }
+    const int64_t counted = slots * tiles;
+    if (s.each == 1 || counted > (int64_t)COUNTERS) return s;  // (more than fill the chip as they are)
+    s.target = (int)div_up(runs_to_aim_at(pairs), tiles);
+    s.slots = (int)slots;
+    s.bytes = COUNTER_BYTES + (size_t)counted * (16 * s.rt) * (c.dim + 2) * sizeof(float);
     return s;
 }
 
@@ -90,11 +99,8 @@ template <class T, int DP, int G, int RT>
 gba_status run_attention(const Q4Args &a, hipStream_t s)
 {
     const int64_t groups = div_up((int64_t)a.slots * a.heads, 8) * 8 * a.row_tiles;
-    const bool joins = a.target != 0 && a.arrived == nullptr, joins_rows = joins && a.tokens * (int64_t)a.q_heads >= JOIN_ROWS;
-    if (groups > (int64_t)UINT_MAX / (64 * Q4_WAVES) || (joins_rows && a.tokens > UINT_MAX / 512)) return GBA_EUNSUPPORTED;
-    const gba_status st = launch(q4_attention_kernel<T, DP, G, RT>, dim3((unsigned)groups), dim3(64 * Q4_WAVES), s, a);
-    if (st != GBA_OK || !joins) return st;
-    return launch_joins<T, DP>(a, 16 * RT, s);
+    if (groups > (int64_t)UINT_MAX / (64 * Q4_WAVES)) return GBA_EUNSUPPORTED;
+    return launch(q4_attention_kernel<T, DP, G, RT>, dim3((unsigned)groups), dim3(64 * Q4_WAVES), s, a);
 }
 
 template <class T, int DP, int G>
@@ -146,7 +152,6 @@ extern "C" gba_status gba_q4_attend(const gba_q4_attention *desc, gba_stream_t s
     if (sh.target != 0 && (d.workspace == nullptr || d.workspace_bytes < sh.bytes)) {
         sh.target = 0;
         sh.slots = (int)d.requests;
-        sh.counts = false;
     }
     Q4Args a = {};
     a.q = d.q;
@@ -181,9 +186,12 @@ extern "C" gba_status gba_q4_attend(const gba_q4_attention *desc, gba_stream_t s
     a.row_tiles = sh.row_tiles;
     a.slots = sh.slots;
     a.target = sh.target;
-    a.arrived = sh.counts ? static_cast<int32_t *>(d.workspace) : nullptr;
-    a.first_run = sh.target != 0 ? reinterpret_cast<int32_t *>(static_cast<char *>(d.workspace) + COUNTER_BYTES) : nullptr;
-    a.part = sh.target != 0 ? reinterpret_cast<float *>(static_cast<char *>(d.workspace) + sh.header) : nullptr;
+    a.length = sh.length;
+    a.each = sh.each;
+    if (sh.target != 0) {
+        a.arrived = static_cast<int32_t *>(d.workspace);
+        a.part = reinterpret_cast<float *>(static_cast<char *>(d.workspace) + COUNTER_BYTES);
+    }
     const hipStream_t s = reinterpret_cast<hipStream_t>(stream);
     return c.dtype == GBA_F16 ? run_attention<F16>(a, sh, s) : run_attention<BF16>(a, sh, s);
 }

@@ -3,7 +3,7 @@
 // A value is scale (code - 8) + offset, with a scale and an offset for a group
 // of dim.  Codes become 16-bit floats 16 + code by a shift, a mask and an or, and
 // nothing else of a value is rounded: with x the query and X its sum over a group
-//     k.x = sum over groups of scale (sum (16 + code) x - 24 X) + offset X
+//     k.x = sum over groups of scale sum (16 + code) x + (offset - 24 scale) X
 //     sum p v = sum (p scale) (16 + code) - 24 sum p scale + sum p offset
 // the first sum of each is a matrix instruction's, the rest fp32.  Weights
 // p scale enter it as two bf16 numbers, the second one what the first's rounding
@@ -32,17 +32,32 @@ struct Q4Args : AttentionArgs {  // k, v: the codes
     const void *k_scales, *v_scales;
 };
 
-// Eight codes as 16 + code, in the order 0 4 1 5 2 6 3 7.
+// Eight codes as 16 + code, in the order 0 4 1 5 2 6 3 7.  The two constants are
+// in a vector and a scalar register, or the and and the or are not one
+// instruction.
 template <class T>
-__device__ __forceinline__ u4 unpacked(unsigned x)
+struct Unpack {
+    unsigned mask = 0x000F000Fu << T::TOP, sixteen = T::SIXTEEN;
+
+    __device__ __forceinline__ Unpack() { asm("" : "+v"(mask), "+s"(sixteen)); }
+    __device__ __forceinline__ u4 operator()(unsigned x) const
+    {
+        u4 v;
+        v[0] = ((x << T::TOP) & mask) | sixteen;
+        v[1] = ((T::TOP >= 4 ? x << (T::TOP >= 4 ? T::TOP - 4 : 0) : x >> (T::TOP < 4 ? 4 - T::TOP : 0)) & mask) | sixteen;
+        v[2] = ((x >> (8 - T::TOP)) & mask) | sixteen;
+        v[3] = ((x >> (12 - T::TOP)) & mask) | sixteen;
+        return v;
+    }
+};
+
+typedef float f2 __attribute__((ext_vector_type(2)));
+
+// Two bf16 numbers in a word, the first one in its low half.
+__device__ __forceinline__ unsigned two_bf16(f2 x)
 {
-    constexpr unsigned MASK = 0x000F000Fu << T::TOP;
-    u4 v;
-    v[0] = ((x << T::TOP) & MASK) | T::SIXTEEN;
-    v[1] = ((T::TOP >= 4 ? x << (T::TOP >= 4 ? T::TOP - 4 : 0) : x >> (T::TOP < 4 ? 4 - T::TOP : 0)) & MASK) | T::SIXTEEN;
-    v[2] = ((x >> (8 - T::TOP)) & MASK) | T::SIXTEEN;
-    v[3] = ((x >> (12 - T::TOP)) & MASK) | T::SIXTEEN;
-    return v;
+    typedef __bf16 b2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(unsigned, __builtin_convertvector(x, b2));
 }
 
 // What lane J of the 16 lanes of a row holds.
@@ -63,11 +78,31 @@ __device__ __forceinline__ int64_t from_lane_uniform(int64_t v, int lane)
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// The sum over the four lanes that hold one row.
+// A value of the even rows of 16 lanes in both rows of their pair, and that of
+// the odd ones; the same of the wave's halves.
+struct Two {
+    unsigned even, odd;
+};
+__device__ __forceinline__ Two rows_of_pairs(unsigned x)
+{
+    const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+    return {r[0], r[1]};
+}
+__device__ __forceinline__ Two halves(unsigned x)
+{
+    const auto r = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+    return {r[0], r[1]};
+}
+__device__ __forceinline__ float as_float(unsigned x) { return __builtin_bit_cast(float, x); }
+__device__ __forceinline__ unsigned as_bits(float x) { return __builtin_bit_cast(unsigned, x); }
+
+// The sum over the four lanes c, c + 16, ...
 __device__ __forceinline__ float across_sum(float x)
 {
-    x += __shfl_xor(x, 32);
-    return x + __shfl_xor(x, 16);
+    const Two t = rows_of_pairs(as_bits(x));
+    x = as_float(t.even) + as_float(t.odd);
+    const Two u = halves(as_bits(x));
+    return as_float(u.even) + as_float(u.odd);
 }
 
 // What is computed from these comes after what is written before: left to
@@ -100,8 +135,9 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     typedef typename T::vec8 vec8;
     typedef elem pair_t __attribute__((ext_vector_type(2)));
     constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = 16 * RT, ROW = DP / 2, TILE = Q4_KEYS * ROW, LOADS = TILE / 1024;
+    constexpr int TERMS = std::is_same_v<T, F16> ? 2 : 1;
     static_assert(TILE <= 16 * RT * 4 * DP, "the sums are no smaller than a tile of V");
-    __shared__ __attribute__((aligned(16))) char smem[q4_lds_bytes<DP, RT>()];
+    __shared__ __attribute__((aligned(128))) char smem[q4_lds_bytes<DP, RT>()];
     __shared__ float tops[Q4_WAVES][ROWS], sums[Q4_WAVES][ROWS];
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
@@ -115,10 +151,6 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     if (run.r < 0) return;
     const Request rq = run.q;
     const int rows = rq.fresh * p.share;
-    if (p.target != 0 && p.arrived == nullptr && run.first == x && head == 0 && row_tile == 0 && threadIdx.x == 0) {
-        p.first_run[2 * run.r] = x;
-        p.first_run[2 * run.r + 1] = run.n;
-    }
     if (row0 >= rows) return;
 
     // ---- tiles: 16 keys are in one block.  A lane looks up a quarter of one of
@@ -153,14 +185,17 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     pair_t ks_next[G], vs_next[G];
     unsigned there_next = 0;  // of keys 16 g .. 16 g + 15, those that exist
     const char *k_codes = static_cast<const char *>(p.k), *v_codes = static_cast<const char *>(p.v);
-    auto fetch = [&](int n) {
-        if (n - looked_up == 16) look_up(n);
-        const int at = 4 * (n - looked_up);
-        const char *k = k_codes + shuffled(first_row, at + (c >> 2)) * ROW + (c & 3) * ROW + g * (ROW / 4);
+    auto fetch_k = [&](int n) {
+        const char *k = k_codes + shuffled(first_row, 4 * (n - looked_up) + (c >> 2)) * ROW + (c & 3) * ROW + g * (ROW / 4);
 #pragma unroll
         for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int i = 0; i < PIECES; ++i) k_next[h][i] = *reinterpret_cast<const words_t *>(k + 4 * h * ROW + 16 * i);
+    };
+    // V, and the scales and offsets of both.
+    auto fetch = [&](int n) {
+        if (n - looked_up == 16) look_up(n);
+        const int at = 4 * (n - looked_up);
         const int64_t pairs = (shuffled(first_row, at + g) + c) * G;
         there_next = (1u << __shfl(keys, at + g)) - 1;
         typedef elem pairs_t __attribute__((ext_vector_type(2 * G)));
@@ -185,10 +220,11 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     if (count > 0) {
         look_up(0);
         fetch(0);
+        fetch_k(0);
     }
 
     // ---- this wave's rows, row c of each block: the second operand, dim
-    // 32 s + 8 g on in the order of `unpacked`
+    // 32 s + 8 g on in the order of Unpack
     vec8 query[RT][STEPS];
     float X[RT][G];
     uint64_t sees[RT];
@@ -226,14 +262,18 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
 
     f4 out[RT][BLOCKS] = {};
     // of the keys of this lane group: sums of weights, of weights times scales and times offsets
-    float total[RT], scales[RT][G], offsets[RT][G], top[RT], limit[RT], base2[RT];
+    float total[RT], offsets[RT][G], top[RT], limit[RT], base2[RT];
+    f4 scales[RT][G] = {};
 #pragma unroll
     for (int i = 0; i < RT; ++i) {
         top[i] = limit[i] = -INFINITY;
         base2[i] = total[i] = 0.f;
 #pragma unroll
-        for (int j = 0; j < G; ++j) scales[i][j] = offsets[i][j] = 0.f;
+        for (int j = 0; j < G; ++j) offsets[i][j] = 0.f;
     }
+    u4 ones_bits = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+    asm("" : "+v"(ones_bits));  // four registers of them, or they are made anew each time
+    const BF16::vec8 ones = __builtin_bit_cast(BF16::vec8, ones_bits);
 
     // 16-byte chunk of a row of V in LDS: chunk ^ swap, over the banks
     constexpr int CHUNKS = DP / 32;
@@ -241,17 +281,17 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     typedef int i2 __attribute__((ext_vector_type(2)));
     typedef __attribute__((address_space(3))) i2 lds_i2;
 
+    const Unpack<T> unpack_k;
+    const Unpack<BF16> unpack_v;
+    // row 16 g + c of V in LDS: the blocks of dim are at this, but for the bits of their chunk
+    const unsigned v_row = (unsigned)(uintptr_t)(lds_void *)mine + lane * ROW + 16 * swap_of(lane);
+
     for (int n = 0; n < count; ++n) {
         float ksc[G], kof[G], vsc[G], vof[G];
-        unsigned k_now[4][STEPS];
-#pragma unroll
-        for (int h = 0; h < 4; ++h)
-#pragma unroll
-            for (int s = 0; s < STEPS; ++s) k_now[h][s] = k_next[h][s / 4][s % 4];
 #pragma unroll
         for (int j = 0; j < G; ++j) {
             ksc[j] = (float)ks_next[j][0];
-            kof[j] = (float)ks_next[j][1];
+            kof[j] = __builtin_fmaf(-24.f, ksc[j], (float)ks_next[j][1]);
             vsc[j] = (float)vs_next[j][0];
             vof[j] = (float)vs_next[j][1];
         }
@@ -274,13 +314,10 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
 #pragma unroll
             for (int i = 0; i < RT; ++i)
 #pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    const float start = -24.f * X[i][j];
-                    part[i][j] = f4{start, start, start, start};
-                }
+                for (int j = 0; j < G; ++j) part[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
-                const vec8 a = __builtin_bit_cast(vec8, unpacked<T>(k_now[H][s]));
+                const vec8 a = __builtin_bit_cast(vec8, unpack_k(k_next[H][s / 4][s % 4]));
 #pragma unroll
                 for (int i = 0; i < RT; ++i) part[i][s / (STEPS / G)] = T::mfma(a, query[i][s], part[i][s / (STEPS / G)]);
             }
@@ -299,6 +336,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
 #pragma unroll
             for (int i = 0; i < RT; ++i) in_order(score[i][H]);
         });
+        if (n + 1 < count) fetch_k(n + 1);
         // ---- which keys a row sees
         const int first = (int)position_of<true>(rq, key0(n));
         const bool edge = __ballot(there != 0xFFFFu) != 0 || first > rq.kept - Q4_KEYS || (first < latest && (unsigned)first + (Q4_KEYS - 1) >= (unsigned)p.sinks);
@@ -377,32 +415,38 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
         each<G>([&](auto group) {
             constexpr int J = decltype(group)::value;
             in_order(vsc[J], vof[J]);
-            BF16::vec8 high[RT][2], low[RT][2];
-            each<16>([&](auto key) {
-                constexpr int E = decltype(key)::value, H = E / 4;
-                const float sc = from_lane<E>(vsc[J]), of = from_lane<E>(vof[J]);
+            u4 weight[TERMS][RT][2];
+            each<8>([&](auto pair) {  // keys 8 half + e and 8 half + 4 + e, next to each other as Unpack has them
+                constexpr int HALF = decltype(pair)::value / 4, E = decltype(pair)::value % 4;
+                const float sc0 = from_lane<8 * HALF + E>(vsc[J]), of0 = from_lane<8 * HALF + E>(vof[J]);
+                const float sc1 = from_lane<8 * HALF + 4 + E>(vsc[J]), of1 = from_lane<8 * HALF + 4 + E>(vof[J]);
 #pragma unroll
                 for (int i = 0; i < RT; ++i) {
-                    const float w = score[i][H][E % 4] * sc;
-                    const __bf16 hi = (__bf16)w;
-                    scales[i][J] += w;
-                    offsets[i][J] = __builtin_fmaf(score[i][H][E % 4], of, offsets[i][J]);
-                    high[i][H / 2][2 * (E % 4) + H % 2] = hi;
-                    low[i][H / 2][2 * (E % 4) + H % 2] = (__bf16)(w - (float)hi);
+                    const float p0 = score[i][2 * HALF][E], p1 = score[i][2 * HALF + 1][E];
+                    const f2 w = {p0 * sc0, p1 * sc1};
+                    const unsigned high = two_bf16(w);
+                    offsets[i][J] = __builtin_fmaf(p1, of1, __builtin_fmaf(p0, of0, offsets[i][J]));
+                    weight[0][i][HALF][E] = high;
+                    if constexpr (TERMS == 2)
+                        weight[1][i][HALF][E] = two_bf16(f2{w[0] - __builtin_bit_cast(float, high << 16), w[1] - __builtin_bit_cast(float, high & 0xFFFF0000u)});
                 }
             });
 #pragma unroll
+            for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+#pragma unroll
+                    for (int i = 0; i < RT; ++i) scales[i][J] = BF16::mfma(ones, __builtin_bit_cast(BF16::vec8, weight[t][i][half]), scales[i][J]);
+#pragma unroll
             for (int b = J * (BLOCKS / G); b < (J + 1) * (BLOCKS / G); ++b) {
-                const int row = lane;  // 16 g + c
-                const i2 words = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2 *)(mine + row * ROW + 16 * ((b >> 1) ^ swap_of(row)) + 8 * (b & 1)));
+                const i2 words = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2 *)(uintptr_t)(v_row ^ (16 * (b >> 1) + 8 * (b & 1))));
 #pragma unroll
                 for (int half = 0; half < 2; ++half) {
-                    const BF16::vec8 v = __builtin_bit_cast(BF16::vec8, unpacked<BF16>((unsigned)words[half]));
+                    const BF16::vec8 v = __builtin_bit_cast(BF16::vec8, unpack_v((unsigned)words[half]));
 #pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        out[i][b] = BF16::mfma(v, high[i][half], out[i][b]);
-                        out[i][b] = BF16::mfma(v, low[i][half], out[i][b]);
-                    }
+                    for (int t = 0; t < TERMS; ++t)
+#pragma unroll
+                        for (int i = 0; i < RT; ++i) out[i][b] = BF16::mfma(v, __builtin_bit_cast(BF16::vec8, weight[t][i][half]), out[i][b]);
                 }
             }
         });
@@ -420,7 +464,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
         }
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-            const float rest_of = across_sum(offsets[i][j]) - 24.f * across_sum(scales[i][j]);
+            const float rest_of = across_sum(offsets[i][j]) - 24.f * scales[i][j][0];
 #pragma unroll
             for (int b = j * (BLOCKS / G); b < (j + 1) * (BLOCKS / G); ++b) {
                 const f4 o = out[i][b] + rest_of;
@@ -455,15 +499,14 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
             for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
             *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r4;
         } else {
-            *reinterpret_cast<f4 *>(part + row * p.dim + d) = o;
+            to_other_xcds(part + row * p.dim + d, o);
             if (four == 0) {
-                part[ROWS * p.dim + row] = m;
-                part[ROWS * (p.dim + 1) + row] = l;
+                to_other_xcds(part + ROWS * p.dim + row, m);
+                to_other_xcds(part + ROWS * (p.dim + 1) + row, l);
             }
         }
     }
-    if (whole_request || p.arrived == nullptr) return;
-    join_by_last<T, DP, ROWS, 64 * Q4_WAVES>(p, run, rq, head, row_tile, rows);
+    if (!whole_request) join_written_through<T, DP, ROWS, 64 * Q4_WAVES>(p, run, rq, head, row_tile, rows);
 }
 
 }  // namespace

@@ -87,14 +87,6 @@ __device__ __forceinline__ void read_transposed(const unsigned *at, u4 (&v)[4])
     for (int i = 0; i < 4; ++i) v[i] = u4{r[2 * i][0], r[2 * i][1], r[2 * i + 1][0], r[2 * i + 1][1]};
 }
 
-// Two 16-bit floats: 0x8000 for each that is infinite or NaN (the exponent's top
-// carries into the sign's place).
-template <class T>
-__device__ __forceinline__ unsigned not_finite(unsigned w)
-{
-    return ((w & T::INFINITE) + T::EXPONENT_ONE) & 0x80008000u;
-}
-
 template <int N>
 struct Const {
     static constexpr int value = N;
@@ -673,6 +665,12 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
 #pragma unroll
             for (int e = 0; e < 4; ++e) r4[e] = (elem)(o[e] * inv);
             *reinterpret_cast<four_t *>(static_cast<elem *>(p.out) + token * p.out_token + h * p.out_head + d) = r4;
+        } else if (WINDOW && RG <= 2) {
+            to_other_xcds(part + row * p.dim + d, o);
+            if (four == 0) {
+                to_other_xcds(part + ROWS * p.dim + row, m);
+                to_other_xcds(part + ROWS * (p.dim + 1) + row, l);
+            }
         } else {
             *reinterpret_cast<f4 *>(part + row * p.dim + d) = o;
             if (four == 0) {
@@ -683,7 +681,8 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     }
     if constexpr (RG <= 2) {
         if (whole_request || p.arrived == nullptr) return;
-        join_by_last<T, DP, ROWS, 64 * WAVES>(p, run, rq, head, row_tile, rows);
+        if constexpr (WINDOW) join_written_through<T, DP, ROWS, 64 * WAVES>(p, run, rq, head, row_tile, rows);
+        else join_by_last<T, DP, ROWS, 64 * WAVES>(p, run, rq, head, row_tile, rows);
     }
 }
 
@@ -723,10 +722,13 @@ gba_status validate(const gba_attention &d)
     return GBA_OK;
 }
 
+// What a workgroup does beside its keys, as keys (windows only).
+constexpr int64_t FIXED_KEYS = 512;
+
 // How a call runs: the kernel, tiles of rows, runs of keys and their room.
 struct Shape {
     bool whole;
-    int dp, rt, rg, row_tiles, target, slots;
+    int dp, rt, rg, row_tiles, target, slots, length, each;
     bool counts;           // runs are joined by the workgroup that ends last
     size_t header, bytes;  // of the workspace: what stands before the sums, all
 };
@@ -745,8 +747,6 @@ int64_t runs_to_aim_at(const gba_attention &d, int rg, int row_tiles)
     if (rg > 2) return pairs < 256 ? 256 - pairs / 2 : 128;
     return pairs <= 128 ? 256 : pairs < 1024 ? 512 : 1024;
 }
-
-int64_t min_of(int64_t a, int64_t b) { return a < b ? a : b; }
 
 // Whether each tile of rows is left whole, with the keys that its own rows see:
 // where the tiles fill the chip, or have few keys.
@@ -777,12 +777,23 @@ Shape shape_of(const gba_attention &d, int64_t window, int64_t sinks)
     s.slots = (int)d.requests;
     s.counts = false;
     s.header = s.bytes = 0;
+    s.length = s.each = 0;
     int64_t most_keys = d.width * c.block_size;  // of a request
-    if (window != 0) most_keys = min_of(most_keys, min_of(window, INT_MAX) + min_of(sinks, INT_MAX) + most_new(d));
+    if (window != 0) most_keys = min_of(most_keys, min_of(window, INT_MAX) + min_of(sinks, INT_MAX) + most_new(d) + 2 * KEYS);  // (in whole tiles)
     if (d.requests <= SPLIT_REQUESTS && most_keys > SHORTEST && !(window != 0 && tiles_alone(d, s, window, sinks))) {
         s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
-        s.counts = s.rg <= 2 && s.rt * s.rg * d.requests * c.heads * s.row_tiles * div_up(most_keys, SHORTEST) <= FEW_RUNS &&
+        if (window != 0) {
+            const int64_t n = runs_of_window(d.requests * c.heads * s.row_tiles, most_keys, s.dp == 64 && s.rg <= 2 ? 512 : 256, FIXED_KEYS);
+            s.length = (int)(div_up(div_up(most_keys, n), SHORTEST) * SHORTEST);
+            s.each = (int)div_up(most_keys, s.length);
+            s.slots = (int)(d.requests * s.each);
+            if (s.each == 1) {
+                s.target = s.length = s.each = 0;
+                return s;
+            }
+        }
+        s.counts = s.rg <= 2 && (window != 0 || s.rt * s.rg * d.requests * c.heads * s.row_tiles * div_up(most_keys, SHORTEST) <= FEW_RUNS) &&
                    (size_t)s.slots * c.heads * s.row_tiles <= COUNTERS;
         s.header = COUNTER_BYTES + (size_t)div_up(d.requests * 8, 256) * 256;
         s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt * s.rg) * (c.dim + 2) * sizeof(float);
@@ -885,6 +896,8 @@ gba_status attend(const gba_attention *desc, int64_t window, int64_t sinks, gba_
     a.row_tiles = sh.row_tiles;
     a.slots = sh.slots;
     a.target = sh.target;
+    a.length = sh.length;
+    a.each = sh.each;
     a.arrived = sh.counts ? static_cast<int32_t *>(d.workspace) : nullptr;
     a.first_run = sh.target != 0 ? reinterpret_cast<int32_t *>(static_cast<char *>(d.workspace) + COUNTER_BYTES) : nullptr;
     a.part = sh.target != 0 ? reinterpret_cast<float *>(static_cast<char *>(d.workspace) + sh.header) : nullptr;

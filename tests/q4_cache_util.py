@@ -94,10 +94,13 @@ class Batch(D.Batch):
         return decode.tree_attention(*self.arguments(), max_new=max(self.counts), mask=None if masks is None else D.signed(masks).cuda(), **kw)
 
     def check(self, got, masks=None, window=None, sinks=0, what="", lens=None):
-        """A score's fp32 sums move its weight by less than 2^-14; the weight
-        enters the second product rounded to 16 bits or more, and that product's
-        fp32 sums are of 16 + code and 24, so that each key's error is at most
-        2^-13 of its weight times |value| + 8 scales; the result is rounded once."""
+        """A score's fp32 sums move its weight by less than 2^-14; the second
+        product's fp32 sums are of 16 + code and 24, so that each key's error is at
+        most 2^-13 of its weight times |value| + 8 scales.  There the weight times
+        the scale is rounded: to 16 bits and more in fp16, within that, and to bf16
+        once in bf16, where it multiplies code - 8 (what is taken from 16 + code is
+        24 times the sum of the rounded ones) and so adds at most 2^-8 of the weight
+        times scale |code - 8|.  The result is rounded once."""
         tokens = sum(self.counts)
         k, v, scale = self.read()
         lens = self.lens if lens is None else lens
@@ -105,6 +108,10 @@ class Batch(D.Batch):
         ref, _ = W.attention(self.q[:tokens], k, v, *args)
         size, _ = W.attention(self.q[:tokens], k, v.abs() + 8 * scale.abs(), *args)
         got = got[:tokens].double().cpu()
+        if self.dtype is torch.bfloat16:
+            c = self.cache
+            steps = scale.abs() * (codes_of(c.v, self.dim, False) - 8).abs().permute(0, 2, 1, 3)
+            size = size + 2.0 ** 5 * W.attention(self.q[:tokens], k, steps, *args)[0]  # (2^-8 over 2^-13)
         finite = ref.isfinite()
         assert torch.equal(got.isnan(), ref.isnan()) and torch.equal(got.isfinite(), finite), (what, "NaN")
         err, bound = (got - ref).abs()[finite], (D.U[self.dtype] * ref.abs() + 2.0 ** -13 * size)[finite]
