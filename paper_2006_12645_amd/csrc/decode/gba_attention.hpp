@@ -506,19 +506,19 @@ constexpr int SPLIT_REQUESTS = 1024;           // above that each request is one
 
 inline int64_t min_of(int64_t a, int64_t b) { return a < b ? a : b; }
 
-// Into how many runs windows of `keys` keys at most are cut, for `pairs` of a
-// request's rows and a head where `room` workgroups run at once: what takes the
-// fewest rounds of them, each as long as a run and, for what a workgroup does
-// beside its keys, `fixed` keys more.
-inline int64_t runs_of_window(int64_t pairs, int64_t keys, int64_t room, int64_t fixed)
+// Length of the runs, a multiple of `step`, that windows of `keys` keys at most
+// are cut into, for `pairs` of a request's rows and a head where `room` workgroups
+// run at once: what takes the fewest rounds of them, each as long as a run and,
+// for what a workgroup does beside its keys, `fixed` keys more.
+inline int64_t run_of_window(int64_t pairs, int64_t keys, int64_t room, int64_t fixed, int64_t step)
 {
-    int64_t best = 1, least = INT64_MAX;
+    int64_t best = keys, least = INT64_MAX;
     for (int64_t n = 1; n <= 256 && n <= div_up(keys, SHORTEST); ++n) {
-        const int64_t length = div_up(div_up(keys, n), SHORTEST) * SHORTEST;
+        const int64_t length = div_up(div_up(keys, n), step) * step;
         const int64_t cost = div_up(pairs * div_up(keys, length), room) * (length + fixed);
         if (cost < least) {
             least = cost;
-            best = n;
+            best = length;
         }
     }
     return best;

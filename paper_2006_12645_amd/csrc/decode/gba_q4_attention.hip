@@ -45,7 +45,7 @@ gba_status validate(const gba_q4_attention &d)
 constexpr int64_t FIXED_KEYS = 512;
 
 struct Shape {
-    int dp, groups, rt, row_tiles, target, slots, length, each;
+    int dp, groups, row_tiles, target, slots, length, each;
     size_t bytes;  // of the workspace: counters, then the sums
 };
 
@@ -64,8 +64,7 @@ Shape shape_of(const gba_q4_attention &d)
     s.dp = q4_width(c.dim);
     s.groups = s.dp > c.group ? s.dp / c.group : 1;
     const int64_t rows = most_new(d) * (d.q_heads / c.heads);
-    s.rt = rows <= 16 || s.dp == 256 ? 1 : rows <= 32 || s.dp == 128 ? 2 : 4;
-    s.row_tiles = (int)div_up(rows, 16 * s.rt);
+    s.row_tiles = (int)div_up(rows, Q4_ROWS);
     s.target = 0;
     s.slots = (int)d.requests;
     s.length = s.each = 0;
@@ -74,14 +73,13 @@ Shape shape_of(const gba_q4_attention &d)
     const int64_t bounded = min_of(d.window, INT_MAX) + min_of(d.sinks, INT_MAX);
     if (d.window != 0) most_keys = min_of(most_keys, bounded + most_new(d) + 2 * Q4_KEYS);  // (sinks and window in whole tiles)
     // Tiles of rows that fill the chip, or have few keys, are left whole, with the keys that their own rows see.
-    const int64_t tokens = div_up(16 * s.rt * c.heads, d.q_heads);
+    const int64_t tokens = div_up(Q4_ROWS * c.heads, d.q_heads);
     const bool alone = s.row_tiles > 1 && (d.requests * c.heads * s.row_tiles >= 512 || (d.window != 0 && bounded + tokens <= 1024));
     if (d.requests > SPLIT_REQUESTS || most_keys <= SHORTEST || alone) return s;
     const int64_t tiles = c.heads * (int64_t)s.row_tiles, pairs = d.requests * tiles;
     int64_t slots = 0;
     if (d.window != 0) {
-        const int64_t n = runs_of_window(pairs, most_keys, 256, FIXED_KEYS);
-        s.length = (int)(div_up(div_up(most_keys, n), SHORTEST) * SHORTEST);
+        s.length = (int)run_of_window(pairs, most_keys, 256, FIXED_KEYS, Q4_KEYS * Q4_WAVES);
         s.each = (int)div_up(most_keys, s.length);
         slots = d.requests * s.each;
     } else {
@@ -91,40 +89,30 @@ Shape shape_of(const gba_q4_attention &d)
     if (s.each == 1 || counted > (int64_t)COUNTERS) return s;  // (more than fill the chip as they are)
     s.target = (int)div_up(runs_to_aim_at(pairs), tiles);
     s.slots = (int)slots;
-    s.bytes = COUNTER_BYTES + (size_t)counted * (16 * s.rt) * (c.dim + 2) * sizeof(float);
+    s.bytes = COUNTER_BYTES + (size_t)counted * Q4_ROWS * (c.dim + 2) * sizeof(float);
     return s;
 }
 
-template <class T, int DP, int G, int RT>
+template <class T, int DP, int G>
 gba_status run_attention(const Q4Args &a, hipStream_t s)
 {
     const int64_t groups = div_up((int64_t)a.slots * a.heads, 8) * 8 * a.row_tiles;
     if (groups > (int64_t)UINT_MAX / (64 * Q4_WAVES)) return GBA_EUNSUPPORTED;
-    return launch(q4_attention_kernel<T, DP, G, RT>, dim3((unsigned)groups), dim3(64 * Q4_WAVES), s, a);
-}
-
-template <class T, int DP, int G>
-gba_status run_attention(const Q4Args &a, const Shape &sh, hipStream_t s)
-{
-    if constexpr (DP == 64)
-        if (sh.rt == 4) return run_attention<T, DP, G, 4>(a, s);
-    if constexpr (DP <= 128)
-        if (sh.rt == 2) return run_attention<T, DP, G, 2>(a, s);
-    return run_attention<T, DP, G, 1>(a, s);
+    return launch(q4_attention_kernel<T, DP, G>, dim3((unsigned)groups), dim3(64 * Q4_WAVES), s, a);
 }
 
 template <class T>
 gba_status run_attention(const Q4Args &a, const Shape &sh, hipStream_t s)
 {
     switch (sh.dp + sh.groups) {
-    case 64 + 1: return run_attention<T, 64, 1>(a, sh, s);
-    case 64 + 2: return run_attention<T, 64, 2>(a, sh, s);
-    case 128 + 1: return run_attention<T, 128, 1>(a, sh, s);
-    case 128 + 2: return run_attention<T, 128, 2>(a, sh, s);
-    case 128 + 4: return run_attention<T, 128, 4>(a, sh, s);
-    case 256 + 2: return run_attention<T, 256, 2>(a, sh, s);
-    case 256 + 4: return run_attention<T, 256, 4>(a, sh, s);
-    default: return run_attention<T, 256, 8>(a, sh, s);
+    case 64 + 1: return run_attention<T, 64, 1>(a, s);
+    case 64 + 2: return run_attention<T, 64, 2>(a, s);
+    case 128 + 1: return run_attention<T, 128, 1>(a, s);
+    case 128 + 2: return run_attention<T, 128, 2>(a, s);
+    case 128 + 4: return run_attention<T, 128, 4>(a, s);
+    case 256 + 2: return run_attention<T, 256, 2>(a, s);
+    case 256 + 4: return run_attention<T, 256, 4>(a, s);
+    default: return run_attention<T, 256, 8>(a, s);
     }
 }
 

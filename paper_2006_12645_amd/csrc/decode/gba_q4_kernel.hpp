@@ -6,8 +6,8 @@
 //     k.x = sum over groups of scale sum (16 + code) x + (offset - 24 scale) X
 //     sum p v = sum (p scale) (16 + code) - 24 sum p scale + sum p offset
 // the first sum of each is a matrix instruction's, the rest fp32.  Weights
-// p scale enter it as two bf16 numbers, the second one what the first's rounding
-// left: bf16 has the range that scales need, and two of them 16 bits.
+// p scale enter it in bf16, which has the range that scales need, and for fp16
+// results as two numbers, the second one what the first's rounding left.
 //
 // Tiles of 64 keys.  Key 16 g + 4 h + e of a tile is row 4 g + e of the h-th
 // 16-key product, so that lane group g has the scores of keys 16 g .. 16 g + 15:
@@ -27,6 +27,7 @@ namespace {
 
 constexpr int Q4_KEYS = 64;   // of a tile
 constexpr int Q4_WAVES = 4;   // take the tiles of a run in turn
+constexpr int Q4_ROWS = 16;   // of a workgroup
 
 struct Q4Args : AttentionArgs {  // k, v: the codes
     const void *k_scales, *v_scales;
@@ -120,24 +121,31 @@ __device__ __forceinline__ void each(F f)
     }
 }
 
-// Bytes of a workgroup's LDS: V's tiles, then the waves' sums.
-template <int DP, int RT>
-constexpr int q4_lds_bytes()
-{
-    return Q4_WAVES * 16 * RT * 4 * DP;  // (V's tiles take 64 DP / 2 bytes a wave)
-}
-
-// DP: dim, padded.  G: groups of dim.  RT: blocks of 16 rows of a wave.
-template <class T, int DP, int G, int RT>
-__global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q4_attention_kernel(Q4Args p)
+// DP: dim, padded.  G: groups of dim.  A workgroup has 16 rows of a request and
+// key head, and its waves the tiles of a run in turn.
+//
+// Bound by HBM where tiles are many: four requests of 60000 to 131071 keys, 8 key
+// heads of 128 in groups of 128, 506 MB, in 101.5 us  Else by vector
+// instructions, about 750 a tile of dim 128 in two groups, of which 260 unpack
+// codes: 64 requests of up to 8192 keys 31 us.  16 rows, not 32: those would
+// share what is unpacked, but leave one wave a SIMD (16 trees of 64 tokens, four
+// heads a key head: 102 us, 124 with 32).  Unsplit codes of K or V in LDS for all
+// waves, with rows and keys of the products exchanged so that scales need no
+// broadcasts but weights pass through LDS, were slower for 16 rows (51 us to 46 for
+// 128 windows of 4096 keys and four tokens).
+template <class T, int DP, int G>
+__global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention_kernel(Q4Args p)
 {
     typedef typename T::elem elem;
     typedef typename T::vec8 vec8;
     typedef elem pair_t __attribute__((ext_vector_type(2)));
-    constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = 16 * RT, ROW = DP / 2, TILE = Q4_KEYS * ROW, LOADS = TILE / 1024;
+    constexpr int STEPS = DP / 32, BLOCKS = DP / 16, ROWS = Q4_ROWS, ROW = DP / 2, TILE = Q4_KEYS * ROW, LOADS = TILE / 1024;
+    constexpr int SUMS = ROWS * 4 * DP;  // bytes of LDS of a wave: first a tile of V, then the sums of its rows
+    static_assert(TILE <= SUMS, "a tile of V is no larger than the sums");
+    // Weights as two bf16 numbers in fp16; one in bf16, whose results are rounded as
+    // it is (38.5 us with two in place of 36 for 64 requests of up to 8192 keys).
     constexpr int TERMS = std::is_same_v<T, F16> ? 2 : 1;
-    static_assert(TILE <= 16 * RT * 4 * DP, "the sums are no smaller than a tile of V");
-    __shared__ __attribute__((aligned(128))) char smem[q4_lds_bytes<DP, RT>()];
+    __shared__ __attribute__((aligned(128))) char smem[Q4_WAVES * SUMS];
     __shared__ float tops[Q4_WAVES][ROWS], sums[Q4_WAVES][ROWS];
 
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), c = lane & 15, g = lane >> 4;
@@ -156,7 +164,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     // ---- tiles: 16 keys are in one block.  A lane looks up a quarter of one of
     // the next 16 tiles: the row of its first key in the cache (row 0 where there
     // is none: codes are finite whatever they are) and how many keys exist.
-    char *mine = smem + wave * (16 * RT * 4 * DP);
+    char *mine = smem + wave * SUMS;
     const int tiles = (int)(((unsigned)(run.to - run.from) + Q4_KEYS - 1) / Q4_KEYS);
     const int count = tiles > wave ? (tiles - wave + Q4_WAVES - 1) / Q4_WAVES : 0;
     const int32_t *entries = p.table + (int64_t)run.r * p.width;
@@ -223,54 +231,42 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
         fetch_k(0);
     }
 
-    // ---- this wave's rows, row c of each block: the second operand, dim
-    // 32 s + 8 g on in the order of Unpack
-    vec8 query[RT][STEPS];
-    float X[RT][G];
-    uint64_t sees[RT];
-    int index[RT], begin[RT];
+    // ---- this wave's rows, row c: the second operand, dim 32 s + 8 g on in the
+    // order of Unpack
+    vec8 query[STEPS];
+    float X[G];
+    const int my_row = row0 + c;
+    const bool real = my_row < rows;
+    const int index = real ? my_row / p.share : 0, token = rq.first + index;  // its token among the new ones, among all
+    const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? my_row % p.share : 0)) * p.q_head;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        const int row = row0 + 16 * i + c;
-        const bool real = row < rows;
-        index[i] = real ? row / p.share : 0;
-        const int token = rq.first + index[i];
-        const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? row % p.share : 0)) * p.q_head;
+    for (int j = 0; j < G; ++j) X[j] = 0.f;
 #pragma unroll
-        for (int j = 0; j < G; ++j) X[i][j] = 0.f;
+    for (int s = 0; s < STEPS; ++s) {
+        const int d = 32 * s + 8 * g;
+        vec8 y = {};
+        if (real && d < p.dim) y = *reinterpret_cast<const vec8 *>(q + d);
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            const int d = 32 * s + 8 * g;
-            vec8 y = {};
-            if (real && d < p.dim) y = *reinterpret_cast<const vec8 *>(q + d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const elem signed_y = p.sign != 1.f ? (elem)((float)y[e] * p.sign) : y[e];
-                query[i][s][2 * (e % 4) + e / 4] = signed_y;
-                X[i][s / (STEPS / G)] += (float)signed_y;
-            }
+        for (int e = 0; e < 8; ++e) {
+            const elem signed_y = p.sign != 1.f ? (elem)((float)y[e] * p.sign) : y[e];
+            query[s][2 * (e % 4) + e / 4] = signed_y;
+            X[s / (STEPS / G)] += (float)signed_y;
         }
-#pragma unroll
-        for (int j = 0; j < G; ++j) X[i][j] = across_sum(X[i][j]);
-        sees[i] = p.mask != nullptr ? p.mask[token] : 0;
-        if (p.mask != nullptr && rq.fresh < 64) sees[i] &= ((uint64_t)1 << rq.fresh) - 1;
-        begin[i] = begin_of(p, rq.kept, p.mask != nullptr ? __popcll(sees[i]) : index[i] + 1);
-        if (p.mask != nullptr) sees[i] = bounded_mask(p, rq.kept, sees[i]);
     }
+#pragma unroll
+    for (int j = 0; j < G; ++j) X[j] = across_sum(X[j]);
     const bool masked = p.mask != nullptr;
-    const int latest = begin_of(p, rq.kept, rq.fresh);
+    uint64_t sees = masked ? p.mask[token] : 0;  // bits of the new tokens that the row sees
+    if (masked && rq.fresh < 64) sees &= ((uint64_t)1 << rq.fresh) - 1;
+    const int begin = begin_of(p, rq.kept, masked ? __popcll(sees) : index + 1);
+    if (masked) sees = bounded_mask(p, rq.kept, sees);
+    const int latest = begin_of(p, rq.kept, rq.fresh);  // no row's window begins later
 
-    f4 out[RT][BLOCKS] = {};
-    // of the keys of this lane group: sums of weights, of weights times scales and times offsets
-    float total[RT], offsets[RT][G], top[RT], limit[RT], base2[RT];
-    f4 scales[RT][G] = {};
+    f4 out[BLOCKS] = {}, scales[G] = {};  // sums of weights times scales times 16 + code, and of weights times scales
+    // of the keys of this lane group: sums of weights and of weights times offsets
+    float total = 0.f, offsets[G], top = -INFINITY, limit = -INFINITY, base2 = 0.f;
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        top[i] = limit[i] = -INFINITY;
-        base2[i] = total[i] = 0.f;
-#pragma unroll
-        for (int j = 0; j < G; ++j) offsets[i][j] = 0.f;
-    }
+    for (int j = 0; j < G; ++j) offsets[j] = 0.f;
     u4 ones_bits = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
     asm("" : "+v"(ones_bits));  // four registers of them, or they are made anew each time
     const BF16::vec8 ones = __builtin_bit_cast(BF16::vec8, ones_bits);
@@ -280,20 +276,20 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     auto swap_of = [](int row) { return DP == 64 ? (row >> 2) & 1 : DP == 128 ? (row >> 1) & 3 : row & 7; };
     typedef int i2 __attribute__((ext_vector_type(2)));
     typedef __attribute__((address_space(3))) i2 lds_i2;
-
     const Unpack<T> unpack_k;
     const Unpack<BF16> unpack_v;
     // row 16 g + c of V in LDS: the blocks of dim are at this, but for the bits of their chunk
     const unsigned v_row = (unsigned)(uintptr_t)(lds_void *)mine + lane * ROW + 16 * swap_of(lane);
 
     for (int n = 0; n < count; ++n) {
-        float ksc[G], kof[G], vsc[G], vof[G];
+        float ksc[G], kof[G], vsc[G], vof[G];  // scales and offsets of key `lane`; of K, offset - 24 scale
 #pragma unroll
         for (int j = 0; j < G; ++j) {
-            ksc[j] = (float)ks_next[j][0];
-            kof[j] = __builtin_fmaf(-24.f, ksc[j], (float)ks_next[j][1]);
-            vsc[j] = (float)vs_next[j][0];
-            vof[j] = (float)vs_next[j][1];
+            const bool used = j * (DP / G) < p.dim;  // (what stands past dim is not)
+            ksc[j] = used ? (float)ks_next[j][0] : 0.f;
+            kof[j] = used ? __builtin_fmaf(-24.f, ksc[j], (float)ks_next[j][1]) : 0.f;
+            vsc[j] = used ? (float)vs_next[j][0] : 0.f;
+            vof[j] = used ? (float)vs_next[j][1] : 0.f;
         }
         const unsigned there = there_next;
         lanes_meet();  // the last tile's V has been read
@@ -305,56 +301,45 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
         if (n + 1 < count) fetch(n + 1);
         lanes_meet();
 
-        // ---- scores: keys 16 g + 4 h + e, row c of each block
-        f4 score[RT][4];
+        // ---- scores: keys 16 g + 4 h + e, row c
+        f4 score[4];
         each<4>([&](auto half) {
             constexpr int H = decltype(half)::value;
+#pragma unroll
             for (int j = 0; j < G; ++j) in_order(ksc[j], kof[j]);
-            f4 part[RT][G];
+            f4 part[G];
 #pragma unroll
-            for (int i = 0; i < RT; ++i)
-#pragma unroll
-                for (int j = 0; j < G; ++j) part[i][j] = f4{0.f, 0.f, 0.f, 0.f};
+            for (int j = 0; j < G; ++j) part[j] = f4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
             for (int s = 0; s < STEPS; ++s) {
                 const vec8 a = __builtin_bit_cast(vec8, unpack_k(k_next[H][s / 4][s % 4]));
-#pragma unroll
-                for (int i = 0; i < RT; ++i) part[i][s / (STEPS / G)] = T::mfma(a, query[i][s], part[i][s / (STEPS / G)]);
+                part[s / (STEPS / G)] = T::mfma(a, query[s], part[s / (STEPS / G)]);
             }
             each<4>([&](auto element) {
                 constexpr int E = decltype(element)::value;
 #pragma unroll
                 for (int j = 0; j < G; ++j) {
                     const float sc = from_lane<4 * H + E>(ksc[j]), of = from_lane<4 * H + E>(kof[j]);
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) {
-                        const float scaled = j == 0 ? sc * part[i][j][E] : __builtin_fmaf(sc, part[i][j][E], score[i][H][E]);
-                        score[i][H][E] = __builtin_fmaf(of, X[i][j], scaled);
-                    }
+                    const float scaled = j == 0 ? sc * part[j][E] : __builtin_fmaf(sc, part[j][E], score[H][E]);
+                    score[H][E] = __builtin_fmaf(of, X[j], scaled);
                 }
             });
-#pragma unroll
-            for (int i = 0; i < RT; ++i) in_order(score[i][H]);
+            in_order(score[H]);
         });
         if (n + 1 < count) fetch_k(n + 1);
-        // ---- which keys a row sees
+        // ---- which keys the row sees
         const int first = (int)position_of<true>(rq, key0(n));
         const bool edge = __ballot(there != 0xFFFFu) != 0 || first > rq.kept - Q4_KEYS || (first < latest && (unsigned)first + (Q4_KEYS - 1) >= (unsigned)p.sinks);
-        unsigned seen[RT];
-#pragma unroll
-        for (int i = 0; i < RT; ++i) seen[i] = 0xFFFFu;
+        unsigned seen = 0xFFFFu;
         if (edge) {
             const int mine_first = first + 16 * g;
+            seen = there & seen_of(masked, sees, index, mine_first - rq.kept) &
+                   (bits_from(begin - mine_first) | ~bits_from(p.sinks - mine_first) | (masked ? bits_from(rq.kept - mine_first) : 0u));
 #pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                seen[i] = there & seen_of(masked, sees[i], index[i], mine_first - rq.kept) &
-                          (bits_from(begin[i] - mine_first) | ~bits_from(p.sinks - mine_first) | (masked ? bits_from(rq.kept - mine_first) : 0u));
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {  // (as bits: a score that is left out may be NaN)
-                    const float is = score[i][e / 4][e % 4];
-                    const unsigned bits = (seen[i] >> e) & 1 ? __builtin_bit_cast(unsigned, is) : 0xFF800000u;
-                    score[i][e / 4][e % 4] = __builtin_bit_cast(float, bits);
-                }
+            for (int e = 0; e < 16; ++e) {  // (as bits: a score that is left out may be NaN)
+                const float is = score[e / 4][e % 4];
+                const unsigned bits = (seen >> e) & 1 ? __builtin_bit_cast(unsigned, is) : 0xFF800000u;
+                score[e / 4][e % 4] = __builtin_bit_cast(float, bits);
             }
         }
         // What a value stands for whose scale or offset is not finite is NaN, and
@@ -369,74 +354,56 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
                 const bool is = 0.f * vsc[j] + 0.f * vof[j] != 0.f;
                 const unsigned which = (unsigned)(__ballot(is) >> (16 * g)) & 0xFFFFu;
                 if (is) vsc[j] = vof[j] = 0.f;
-#pragma unroll
-                for (int i = 0; i < RT; ++i)
-                    if (which & seen[i]) offsets[i][j] = NAN;
+                if (which & seen) offsets[j] = NAN;
             }
         }
         // ---- softmax: the maximum moves when a score passes it by 2^8
-        float most[RT];
-        bool past = false;
+        float most = score[0][0];
 #pragma unroll
-        for (int i = 0; i < RT; ++i) {
-            most[i] = score[i][0][0];
+        for (int e = 1; e < 16; ++e) most = larger(most, score[e / 4][e % 4]);
+        most *= p.scale2;
+        if (__ballot(most > limit)) {
+            const float now = larger(across_max(most), top);
+            const float next = now == -INFINITY ? 0.f : now;
+            const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2 - next);
+            top = now;
+            limit = now + 8.f;
+            base2 = next;
+            total *= keep;
 #pragma unroll
-            for (int e = 1; e < 16; ++e) most[i] = larger(most[i], score[i][e / 4][e % 4]);
-            most[i] *= p.scale2;
-            past |= most[i] > limit[i];
-        }
-        if (__ballot(past)) {
-#pragma unroll
-            for (int i = 0; i < RT; ++i) {
-                const float now = larger(across_max(most[i]), top[i]);
-                const float next = now == -INFINITY ? 0.f : now;
-                const float keep = top[i] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2[i] - next);
-                top[i] = now;
-                limit[i] = now + 8.f;
-                base2[i] = next;
-                total[i] *= keep;
-#pragma unroll
-                for (int j = 0; j < G; ++j) {
-                    scales[i][j] *= keep;
-                    offsets[i][j] *= keep;
-                }
-#pragma unroll
-                for (int b = 0; b < BLOCKS; ++b) out[i][b] *= keep;
+            for (int j = 0; j < G; ++j) {
+                scales[j] *= keep;
+                offsets[j] *= keep;
             }
+#pragma unroll
+            for (int b = 0; b < BLOCKS; ++b) out[b] *= keep;
         }
 #pragma unroll
-        for (int i = 0; i < RT; ++i)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) {
-                score[i][e / 4][e % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[i][e / 4][e % 4], p.scale2, -base2[i]));
-                total[i] += score[i][e / 4][e % 4];
-            }
+        for (int e = 0; e < 16; ++e) {
+            score[e / 4][e % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[e / 4][e % 4], p.scale2, -base2));
+            total += score[e / 4][e % 4];
+        }
         // ---- weights of each group and its blocks of dim
         each<G>([&](auto group) {
             constexpr int J = decltype(group)::value;
             in_order(vsc[J], vof[J]);
-            u4 weight[TERMS][RT][2];
+            u4 weight[TERMS][2];
             each<8>([&](auto pair) {  // keys 8 half + e and 8 half + 4 + e, next to each other as Unpack has them
                 constexpr int HALF = decltype(pair)::value / 4, E = decltype(pair)::value % 4;
                 const float sc0 = from_lane<8 * HALF + E>(vsc[J]), of0 = from_lane<8 * HALF + E>(vof[J]);
                 const float sc1 = from_lane<8 * HALF + 4 + E>(vsc[J]), of1 = from_lane<8 * HALF + 4 + E>(vof[J]);
-#pragma unroll
-                for (int i = 0; i < RT; ++i) {
-                    const float p0 = score[i][2 * HALF][E], p1 = score[i][2 * HALF + 1][E];
-                    const f2 w = {p0 * sc0, p1 * sc1};
-                    const unsigned high = two_bf16(w);
-                    offsets[i][J] = __builtin_fmaf(p1, of1, __builtin_fmaf(p0, of0, offsets[i][J]));
-                    weight[0][i][HALF][E] = high;
-                    if constexpr (TERMS == 2)
-                        weight[1][i][HALF][E] = two_bf16(f2{w[0] - __builtin_bit_cast(float, high << 16), w[1] - __builtin_bit_cast(float, high & 0xFFFF0000u)});
-                }
+                const float p0 = score[2 * HALF][E], p1 = score[2 * HALF + 1][E];
+                const f2 w = {p0 * sc0, p1 * sc1};
+                const unsigned high = two_bf16(w);
+                offsets[J] = __builtin_fmaf(p1, of1, __builtin_fmaf(p0, of0, offsets[J]));
+                weight[0][HALF][E] = high;
+                if constexpr (TERMS == 2)
+                    weight[1][HALF][E] = two_bf16(f2{w[0] - __builtin_bit_cast(float, high << 16), w[1] - __builtin_bit_cast(float, high & 0xFFFF0000u)});
             });
 #pragma unroll
             for (int t = 0; t < TERMS; ++t)
 #pragma unroll
-                for (int half = 0; half < 2; ++half)
-#pragma unroll
-                    for (int i = 0; i < RT; ++i) scales[i][J] = BF16::mfma(ones, __builtin_bit_cast(BF16::vec8, weight[t][i][half]), scales[i][J]);
+                for (int half = 0; half < 2; ++half) scales[J] = BF16::mfma(ones, __builtin_bit_cast(BF16::vec8, weight[t][half]), scales[J]);
 #pragma unroll
             for (int b = J * (BLOCKS / G); b < (J + 1) * (BLOCKS / G); ++b) {
                 const i2 words = __builtin_amdgcn_ds_read_tr4_b64_v2i32((lds_i2 *)(uintptr_t)(v_row ^ (16 * (b >> 1) + 8 * (b & 1))));
@@ -444,9 +411,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
                 for (int half = 0; half < 2; ++half) {
                     const BF16::vec8 v = __builtin_bit_cast(BF16::vec8, unpack_v((unsigned)words[half]));
 #pragma unroll
-                    for (int t = 0; t < TERMS; ++t)
-#pragma unroll
-                        for (int i = 0; i < RT; ++i) out[i][b] = BF16::mfma(v, __builtin_bit_cast(BF16::vec8, weight[t][i][half]), out[i][b]);
+                    for (int t = 0; t < TERMS; ++t) out[b] = BF16::mfma(v, __builtin_bit_cast(BF16::vec8, weight[t][half]), out[b]);
                 }
             }
         });
@@ -455,22 +420,17 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
     // ---- this wave's sums, joined with the others' through LDS: row c, chunks of
     // four of dim, chunk j of a row at j ^ c
     lanes_meet();
+    total = across_sum(total);
+    if (g == 0) {
+        tops[wave][c] = top;
+        sums[wave][c] = total;
+    }
 #pragma unroll
-    for (int i = 0; i < RT; ++i) {
-        total[i] = across_sum(total[i]);
-        if (g == 0) {
-            tops[wave][16 * i + c] = top[i];
-            sums[wave][16 * i + c] = total[i];
-        }
+    for (int j = 0; j < G; ++j) {
+        const float rest_of = across_sum(offsets[j]) - 24.f * scales[j][0];
 #pragma unroll
-        for (int j = 0; j < G; ++j) {
-            const float rest_of = across_sum(offsets[i][j]) - 24.f * scales[i][j][0];
-#pragma unroll
-            for (int b = j * (BLOCKS / G); b < (j + 1) * (BLOCKS / G); ++b) {
-                const f4 o = out[i][b] + rest_of;
-                *reinterpret_cast<f4 *>(mine + (16 * i + c) * (4 * DP) + 16 * ((4 * b + g) ^ c)) = o;
-            }
-        }
+        for (int b = j * (BLOCKS / G); b < (j + 1) * (BLOCKS / G); ++b)
+            *reinterpret_cast<f4 *>(mine + c * (4 * DP) + 16 * ((4 * b + g) ^ c)) = out[b] + rest_of;
     }
     __syncthreads();
     const bool whole_request = run.n == 1;
@@ -489,7 +449,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, RT == 1 && DP <= 128 ? 2 : 1) q
         for (int w = 0; w < Q4_WAVES; ++w) {
             const float share = tops[w][row] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(tops[w][row] - m);
             l += share * sums[w][row];
-            o += share * *reinterpret_cast<const f4 *>(smem + w * (16 * RT * 4 * DP) + row * (4 * DP) + 16 * (four ^ (row & 15)));
+            o += share * *reinterpret_cast<const f4 *>(smem + w * SUMS + row * (4 * DP) + 16 * (four ^ (row & 15)));
         }
         if (whole_request) {
             const float inv = l > 0.f ? 1.f / l : 0.f;

@@ -784,8 +784,7 @@ Shape shape_of(const gba_attention &d, int64_t window, int64_t sinks)
         s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
         s.slots = (int)d.requests + s.target;
         if (window != 0) {
-            const int64_t n = runs_of_window(d.requests * c.heads * s.row_tiles, most_keys, s.dp == 64 && s.rg <= 2 ? 512 : 256, FIXED_KEYS);
-            s.length = (int)(div_up(div_up(most_keys, n), SHORTEST) * SHORTEST);
+            s.length = (int)run_of_window(d.requests * c.heads * s.row_tiles, most_keys, s.dp == 64 && s.rg <= 2 ? 512 : 256, FIXED_KEYS, 4 * KEYS);
             s.each = (int)div_up(most_keys, s.length);
             s.slots = (int)(d.requests * s.each);
             if (s.each == 1) {
