@@ -53,6 +53,18 @@ __device__ __forceinline__ int begin_of(const AttentionArgs &p, int kept, int se
     return (int)(begin < 0 ? 0 : begin < INT_MAX ? begin : INT_MAX);
 }
 
+// Of new tokens `from` to `to`: every one sees the positions from `latest` on
+// that are before `sure`.
+struct Edges {
+    int latest, sure;
+};
+__device__ __forceinline__ Edges edges_of(const AttentionArgs &p, const Request &q, int from, int to)
+{
+    if (p.mask != nullptr) return {begin_of(p, q.kept, q.fresh), q.kept};
+    const int64_t past = (int64_t)q.kept + from + 1;
+    return {begin_of(p, q.kept, to + 1), (int)(past < INT_MAX ? past : INT_MAX)};
+}
+
 // The keys of new tokens `from` to `to` of a request (of all of them with a
 // mask: the shortest text is the cached one), sinks and window in whole tiles
 // of TILE.

@@ -261,7 +261,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
     if (masked && rq.fresh < 64) sees &= ((uint64_t)1 << rq.fresh) - 1;
     const int begin = begin_of(p, rq.kept, masked ? __popcll(sees) : index + 1);
     if (masked) sees = bounded_mask(p, rq.kept, sees);
-    const int latest = begin_of(p, rq.kept, rq.fresh);  // no row's window begins later
+    const Edges edges = edges_of(p, rq, row0 / p.share, (int)(min((int64_t)row0 + ROWS, (int64_t)rows) - 1) / p.share);
 
     f4 out[BLOCKS] = {}, scales[G] = {};  // sums of weights times scales times 16 + code, and of weights times scales
     // of the keys of this lane group: sums of weights and of weights times offsets
@@ -330,7 +330,8 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         if (n + 1 < count) fetch_k(n + 1);
         // ---- which keys the row sees
         const int first = (int)position_of<true>(rq, key0(n));
-        const bool edge = __ballot(there != 0xFFFFu) != 0 || first > rq.kept - Q4_KEYS || (first < latest && (unsigned)first + (Q4_KEYS - 1) >= (unsigned)p.sinks);
+        const bool edge = __ballot(there != 0xFFFFu) != 0 || first > edges.sure - Q4_KEYS ||
+                          (first < edges.latest && (unsigned)first + (Q4_KEYS - 1) >= (unsigned)p.sinks);
         unsigned seen = 0xFFFFu;
         if (edge) {
             const int mine_first = first + 16 * g;

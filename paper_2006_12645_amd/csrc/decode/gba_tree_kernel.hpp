@@ -314,7 +314,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
         }
     }
     const bool masked = p.mask != nullptr;
-    const int latest = WINDOW ? begin_of(p, rq.kept, rq.fresh) : 0;  // no row's window begins later
+    const Edges edges = WINDOW ? edges_of(p, rq, row0 / p.share, (int)(min((int64_t)row0 + ROWS, (int64_t)rows) - 1) / p.share) : Edges{0, rq.kept};
 
     f4 out[RT][BLOCKS] = {}, weights[RT] = {};
     // running maximum; what a score may be before it moves; what is subtracted
@@ -372,7 +372,8 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     auto soften = [&](int n, unsigned there) -> bool {
         bool unseen = false;
         const int first = (int)position_of<WINDOW>(rq, key0(n)), first_draft = first - rq.kept;  // of the new tokens, or below 0
-        if (there != 0xFFFFFFFFu || first_draft + KEYS > 0 || (WINDOW && first < latest && (unsigned)first + (KEYS - 1) >= (unsigned)p.sinks)) {
+        if (there != 0xFFFFFFFFu || (WINDOW ? first > edges.sure - KEYS : first_draft + KEYS > 0) ||
+            (WINDOW && first < edges.latest && (unsigned)first + (KEYS - 1) >= (unsigned)p.sinks)) {
 #pragma unroll
             for (int i = 0; i < RT; ++i) {
                 unsigned all = there & seen_of(masked, sees[i], index[i], first_draft);
@@ -506,8 +507,8 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
             __builtin_amdgcn_s_barrier();  // every wave's share is there, and the other stage has been read
             const unsigned slot = (round & 1) * (SUB * S::PAIR);
             const int64_t stage_end = run.from + (int64_t)(KEYS * KG * SUB) * (round + 1);
-            bool hides = stage_end + (WINDOW ? rq.gap : 0) > rq.kept;  // whether a row may not see a key of this stage
-            if constexpr (WINDOW) hides |= (int64_t)position_of<true>(rq, (unsigned)(stage_end - KEYS * KG * SUB)) < latest;
+            bool hides = stage_end + (WINDOW ? rq.gap : 0) > edges.sure;  // whether a row may not see a key of this stage
+            if constexpr (WINDOW) hides |= (int64_t)position_of<true>(rq, (unsigned)(stage_end - KEYS * KG * SUB)) < edges.latest;
             if (hides) {
                 clean(round * SUB, slot, SUB * COPIES / RG * rg, SUB * COPIES / RG);
                 wait_vm_lgkm0<0>();
