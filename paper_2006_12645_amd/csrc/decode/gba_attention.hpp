@@ -18,7 +18,8 @@ struct AttentionArgs {
     int requests, width, tokens, max_new, q_heads, heads, share, num_blocks, block_size, dim;
     float scale2;      // |scale| * log2(e); its sign, or 0, goes to the queries
     float sign;
-    int window, sinks; // (windows only) what a token sees of its text: the last ones and the first
+    int64_t window;    // (windows only) what a token sees of its text: the last ones
+    int sinks;         // and the first
     int row_tiles;     // of a request and head
     int slots;         // runs of keys there is room for: at least as many as there are
     int target;        // runs to aim at (0: one for each request)
@@ -259,7 +260,7 @@ __device__ __forceinline__ uint64_t bounded_mask(const AttentionArgs &p, int kep
 {
     const int64_t firsts = (int64_t)p.sinks - kept;
     uint64_t out = mask;
-    for (int i = 0, drop = __popcll(mask) - p.window; i < drop; ++i) {
+    for (int i = 0, drop = p.window < 64 ? __popcll(mask) - (int)p.window : 0; i < drop; ++i) {
         const uint64_t lowest = mask & (0 - mask);
         mask ^= lowest;
         if (i >= firsts) out ^= lowest;
@@ -524,9 +525,10 @@ inline int64_t min_of(int64_t a, int64_t b) { return a < b ? a : b; }
 // for what a workgroup does beside its keys, `fixed` keys more.
 inline int64_t run_of_window(int64_t pairs, int64_t keys, int64_t room, int64_t fixed, int64_t step)
 {
-    int64_t best = keys, least = INT64_MAX;
+    int64_t best = step, least = INT64_MAX;
     for (int64_t n = 1; n <= 256 && n <= div_up(keys, SHORTEST); ++n) {
         const int64_t length = div_up(div_up(keys, n), step) * step;
+        if (length > INT_MAX) continue;
         const int64_t cost = div_up(pairs * div_up(keys, length), room) * (length + fixed);
         if (cost < least) {
             least = cost;

@@ -169,7 +169,7 @@ extern "C" gba_status gba_q4_attend(const gba_q4_attention *desc, gba_stream_t s
     const float scale2 = d.scale * LOG2_E;
     a.sign = scale2 > 0.f ? 1.f : scale2 < 0.f ? -1.f : 0.f;
     a.scale2 = scale2 > 0.f ? scale2 : scale2 < 0.f ? -scale2 : 1.f;
-    a.window = d.window != 0 ? (int)min_of(d.window, INT_MAX) : INT_MAX;
+    a.window = d.window != 0 ? d.window : INT64_MAX;
     a.sinks = d.window != 0 ? (int)min_of(d.sinks, INT_MAX) : 0;
     a.row_tiles = sh.row_tiles;
     a.slots = sh.slots;

@@ -255,7 +255,10 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         }
     }
 #pragma unroll
-    for (int j = 0; j < G; ++j) X[j] = across_sum(X[j]);
+    for (int j = 0; j < G; ++j) {
+        X[j] = across_sum(X[j]);
+        X[j] += X[j] - X[j];  // (NaN where the query is not finite)
+    }
     const bool masked = p.mask != nullptr;
     uint64_t sees = masked ? p.mask[token] : 0;  // bits of the new tokens that the row sees
     if (masked && rq.fresh < 64) sees &= ((uint64_t)1 << rq.fresh) - 1;

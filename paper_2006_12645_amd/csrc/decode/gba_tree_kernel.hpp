@@ -891,7 +891,7 @@ gba_status attend(const gba_attention *desc, int64_t window, int64_t sinks, gba_
     const float scale2 = d.scale * LOG2_E;
     a.sign = scale2 > 0.f ? 1.f : scale2 < 0.f ? -1.f : 0.f;
     a.scale2 = scale2 > 0.f ? scale2 : scale2 < 0.f ? -scale2 : 1.f;
-    a.window = (int)min_of(window, INT_MAX);
+    a.window = window;
     a.sinks = (int)min_of(sinks, INT_MAX);
     a.row_tiles = sh.row_tiles;
     a.slots = sh.slots;
