@@ -671,7 +671,8 @@ typedef struct gba_q4_cache {
  * Errors: GBA_EINVAL for cache == NULL, a bad enum or group, negative sizes,
  * block_size < 1, a NULL pointer that is read or written; GBA_EUNSUPPORTED for
  * other dims, block sizes or alignments, num_blocks * block_size or tokens above
- * 2^31-1, or more than 65535 heads; GBA_EHIP if the launch fails.
+ * 2^31-1, more than 65535 heads, or a launch of 2^32 threads or more (from 2^24
+ * tokens on); GBA_EHIP if the launch fails.
  */
 gba_status gba_q4_cache_store(const gba_q4_cache *cache, int64_t tokens, const void *k, int64_t k_token,
                               int64_t k_head, const void *v, int64_t v_token, int64_t v_head,

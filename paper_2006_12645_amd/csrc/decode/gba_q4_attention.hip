@@ -41,7 +41,8 @@ gba_status validate(const gba_q4_attention &d)
     return GBA_OK;
 }
 
-// What a workgroup does beside its keys, as keys.
+// What a workgroup does beside its keys, as keys: a window of 128 requests and 4
+// heads (4236 keys, 512 pairs) is one run, 43 us; as three, 47.
 constexpr int64_t FIXED_KEYS = 512;
 
 struct Shape {

@@ -124,16 +124,15 @@ __device__ __forceinline__ void each(F f)
 // DP: dim, padded.  G: groups of dim.  A workgroup has 16 rows of a request and
 // key head, and its waves the tiles of a run in turn.
 //
-// Bound by HBM where tiles are many: four requests of 60000 to 131071 keys, 8 key
-// heads of 128 in groups of 128, 506 MB, in 101.5 us
-// (5.0 TB/s).  Else by vector
-// instructions, about 750 a tile of dim 128 in two groups, of which 260 unpack
-// codes: 64 requests of up to 8192 keys 31 us.  16 rows, not 32: those would
-// share what is unpacked, but leave one wave a SIMD (16 trees of 64 tokens, four
-// heads a key head: 102 us, 124 with 32).  Unsplit codes of K or V in LDS for all
-// waves, with rows and keys of the products exchanged so that scales need no
-// broadcasts but weights pass through LDS, were slower for 16 rows (51 us to 46 for
-// 128 windows of 4096 keys and four tokens).
+// Bound by HBM where tiles are many and groups few: four requests of 60000 to
+// 131071 keys, 8 key heads of 128 in groups of 128, 506 MB, in 102 to 105 us (4.9
+// TB/s).  Else by vector instructions, about 740 a tile of dim 128 in two groups,
+// of which 224 unpack codes: 64 requests of up to 8192 keys, 79 MB, 31 us; 16 trees
+// of 64 tokens, four heads a key head, 103 us.  Two blocks of 16 rows a wave would
+// share what is unpacked, but leave one wave a SIMD: 124 us.  With rows and keys
+// exchanged in the first product a lane has one key, and scales need no
+// broadcasts, but weights go through LDS to the second: 33 us and, of 128 windows
+// of 4096 keys for 16 rows, 51 in place of 43.
 template <class T, int DP, int G>
 __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention_kernel(Q4Args p)
 {

@@ -1,6 +1,7 @@
 """A decoding step: few-row products with 4-bit weights, the block tables and
-slot maps of a paged key/value cache, the cache itself, and the attention of
-each request's new tokens over it (one token, a chain or a tree of drafts).
+slot maps of a paged key/value cache, the cache itself, in 16 bits or in 4, and
+the attention of each request's new tokens over it (one token, a chain or a tree
+of drafts), of all that is cached or of a window.
 
 Argument marshalling over libgba.so, like :mod:`paper_2006_12645_amd.gba`:
 every step of the computation is a HIP kernel, launched on `stream` or torch's
