@@ -290,7 +290,9 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         for (int j = 0; j < G; ++j) {
             const bool used = j * (DP / G) < p.dim;  // (what stands past dim is not)
             ksc[j] = used ? (float)ks_next[j][0] : 0.f;
-            kof[j] = used ? __builtin_fmaf(-24.f, ksc[j], (float)ks_next[j][1]) : 0.f;
+            const float of = used ? (float)ks_next[j][1] : 0.f;
+            kof[j] = __builtin_fmaf(-24.f, ksc[j], of);
+            ksc[j] += 0.f * ksc[j] + 0.f * of;  // (NaN where one is not finite: a score of -infinity would be no key)
             vsc[j] = used ? (float)vs_next[j][0] : 0.f;
             vof[j] = used ? (float)vs_next[j][1] : 0.f;
         }

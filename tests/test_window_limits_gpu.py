@@ -114,3 +114,20 @@ def test_a_query_that_is_not_finite_is_nan():
             rows = torch.zeros((count, 4), dtype=torch.bool)
             rows[count - 1, 1] = True
             assert torch.equal(got.isnan().all(2).cpu(), rows) and torch.equal(got.isfinite().all(2).cpu(), ~rows)
+
+
+@pytest.mark.parametrize("workspace", ["auto", None], ids=["runs", "one"])
+@pytest.mark.parametrize("count", [1, 20, 64])
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+def test_a_query_or_a_key_that_is_not_finite_in_one_of_many_runs(bad, count, workspace):
+    b = Q.Batch(13, [9000, 12000], [count, count], heads=4, share=2, dim=128, block=16, dtype=BF16, group=64)
+    b.q[2 * count - 1, 3, 40] = bad
+    page = int(b.table[0, 400])
+    b.cache.k_scales[page, 2, 5, 1, 0] = bad
+    print("CASE q4 not finite in a run", bad, count, workspace, flush=True)
+    for window, sinks in [(None, 0), (8000, 5)]:
+        got = b.attend(workspace=workspace, window=window, sinks=sinks)
+        rows = torch.zeros(got.shape[:2], dtype=torch.bool)
+        rows[2 * count - 1, 3] = True
+        rows[:count, 4:6] = True
+        assert torch.equal(got.isnan().all(2).cpu(), rows) and torch.equal(got.isfinite().all(2).cpu(), ~rows)
