@@ -127,7 +127,7 @@ __device__ __forceinline__ void each(F f)
 // Bound by HBM where tiles are many and groups few: four requests of 60000 to
 // 131071 keys, 8 key heads of 128 in groups of 128, 506 MB, in 102 to 105 us (4.9
 // TB/s).  Else by vector instructions, about 740 a tile of dim 128 in two groups,
-// of which 224 unpack codes: 64 requests of up to 8192 keys, 79 MB, 31 us; 16 trees
+// of which 224 unpack codes: 64 requests of up to 8192 keys, 79 MB, 32 us; 16 trees
 // of 64 tokens, four heads a key head, 103 us.  Two blocks of 16 rows a wave would
 // share what is unpacked, but leave one wave a SIMD: 124 us.  With rows and keys
 // exchanged in the first product a lane has one key, and scales need no

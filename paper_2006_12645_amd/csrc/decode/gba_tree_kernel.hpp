@@ -32,7 +32,7 @@
 // its others are counted without the gap, in whole tiles, and a tile at the edge
 // of a row's window or sinks is masked as one with new tokens is.  64 requests in a
 // window of 4096, 8 key heads of 128, 858 MB: 163 us (5.3 TB/s); 8192 tokens of a
-// prompt in one of 1024, four heads a key head: 195 us (706 TFLOP/s).
+// prompt in one of 1024, four heads a key head: 197 us (700 TFLOP/s).
 #pragma once
 
 #include "gba_attention.hpp"
