@@ -121,6 +121,26 @@ __device__ __forceinline__ void each(F f)
     }
 }
 
+// Where there are a few times as many workgroups as the chip holds, and requests
+// may have many keys, those of long requests go first, so that no long one is left
+// for the end: 16 trees of 64 tokens over 500 to 4096 keys, 2048 workgroups, 103 us
+// as they come and 83, of 36 tokens over 100 to 8000 keys 96 and 65; over 4000 keys
+// each 179 and 181; 64 trees of 64 over 100 to 4000 keys, 8192 workgroups, 271 and 285.
+constexpr int64_t Q4_SORTED_FROM = 1024, Q4_SORTED_TO = 4096, Q4_SORTED_KEYS = 2048;
+
+// The x-th longest of up to 64 requests, in steps of 64 keys; of equal ones, the
+// first first.
+__device__ __forceinline__ int nth_longest(const Q4Args &p, int x, int lane)
+{
+    const int key = lane < p.requests ? (max(p.lens[lane], 0) & ~63) | (63 - lane) : -1;
+    int before = 0;
+#pragma unroll 1
+    for (int r = 0; r < p.requests; r += 16)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) before += __builtin_amdgcn_readlane(key, r + i) > key;
+    return __builtin_ctzll(__ballot(lane < p.requests && before == x));
+}
+
 // DP: dim, padded.  G: groups of dim.  A workgroup has 16 rows of a request and
 // key head, and its waves the tiles of a run in turn.
 //
@@ -128,7 +148,7 @@ __device__ __forceinline__ void each(F f)
 // 131071 keys, 8 key heads of 128 in groups of 128, 506 MB, in 102 to 105 us (4.9
 // TB/s).  Else by vector instructions, about 740 a tile of dim 128 in two groups,
 // of which 224 unpack codes: 64 requests of up to 8192 keys, 79 MB, 32 us; 16 trees
-// of 64 tokens, four heads a key head, 103 us.  Two blocks of 16 rows a wave would
+// of 64 tokens, four heads a key head, 83 us.  Two blocks of 16 rows a wave would
 // share what is unpacked, but leave one wave a SIMD: 124 us.  With rows and keys
 // exchanged in the first product a lane has one key, and scales need no
 // broadcasts, but weights go through LDS to the second: 33 us and, of 128 windows
@@ -152,8 +172,13 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
     // The row tiles of one run and head have ids 8 apart: the same XCD's L2.
     const int xcd = blockIdx.x & 7, rest = blockIdx.x >> 3;
     const int row_tile = rest % p.row_tiles, item = rest / p.row_tiles * 8 + xcd;
-    const int head = item % p.heads, x = item / p.heads;
+    const int head = item % p.heads;
+    int x = item / p.heads;
     if (x >= p.slots) return;
+    const int64_t workgroups = (int64_t)p.slots * p.heads * p.row_tiles;
+    if (p.target == 0 && p.requests <= 64 && workgroups >= Q4_SORTED_FROM && workgroups <= Q4_SORTED_TO &&
+        min((int64_t)p.width * p.block_size, p.window) >= Q4_SORTED_KEYS)
+        x = nth_longest(p, x, lane);
     const int row0 = row_tile * ROWS;
     const Run run = run_of<true, Q4_KEYS>(p, x, lane, Q4_KEYS * Q4_WAVES, row0, ROWS);
     if (run.r < 0) return;

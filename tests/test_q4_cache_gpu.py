@@ -286,6 +286,19 @@ def test_an_empty_cache():
     assert not got.any()
 
 
+@pytest.mark.parametrize("heads,share,dim,lens,counts", [
+    (16, 4, 64, [500, 3000, 0, 2100], [64, 64, 60, 64]), (16, 4, 128, [2000, 2010, 2000, 1984], [64, 1, 64, 33]),
+    (8, 8, 64, [2100 - 64 * i for i in range(10)] + [17 * i for i in range(10)], [i % 41 for i in range(20)]),
+    (4, 4, 64, [(997 * i) % 2100 for i in range(64)], [16] * 64)])
+def test_many_rows_of_requests_of_different_lengths(heads, share, dim, lens, counts):
+    b = Q.Batch(61, lens, counts, heads=heads, share=share, dim=dim, block=32, dtype=BF16, group=64)
+    assert 1024 <= len(lens) * heads * -(-max(counts) * share // 16) <= 4096 and b.table.shape[1] * 32 >= 2048
+    masks = tree_masks(random.Random(len(lens)), counts)
+    for words, window in [(None, None), (masks, None), (masks, 2050)]:
+        print("CASE q4 lengths", heads, share, dim, words is not None, window, flush=True)
+        b.check(b.attend(words, window=window, sinks=3 if window else 0), words, window, 3 if window else 0)
+
+
 def test_on_another_stream_and_in_a_graph():
     b = Q.Batch(91, [3000, 500, 9], [4, 4, 4], heads=2, share=4, dim=128, block=16, dtype=BF16, group=64)
     q, cache, table, lens, offsets = b.arguments()
