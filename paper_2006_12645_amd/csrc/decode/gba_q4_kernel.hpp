@@ -79,6 +79,16 @@ __device__ __forceinline__ int64_t from_lane_uniform(int64_t v, int lane)
     return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
+// From this on a scale or an offset is a large one, if there are such numbers.
+// Below it no sum overflows: of less than 2^31 keys, weights of up to 2^8 and
+// numbers of up to 31 scales, or of an offset, it is below 2^(31 + 8 + 5 + 80).  A row
+// that sees a large one has weights that are 2^LOWER smaller, its sum of weights
+// among them, and so room for any value of the type; scales times weights then lose
+// bits below 2^-78, more than 150 powers of two below that value.
+template <class T>
+constexpr float LARGE = std::is_same_v<T, BF16> ? 0x1p80f : INFINITY;
+constexpr float LOWER = 48.f;
+
 // A value of the even rows of 16 lanes in both rows of their pair, and that of
 // the odd ones; the same of the wave's halves.
 struct Two {
@@ -293,6 +303,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
     f4 out[BLOCKS] = {}, scales[G] = {};  // sums of weights times scales times 16 + code, and of weights times scales
     // of the keys of this lane group: sums of weights and of weights times offsets
     float total = 0.f, offsets[G], top = -INFINITY, limit = -INFINITY, base2 = 0.f;
+    unsigned lower = 0;  // bits of the rows that have seen a large value
 #pragma unroll
     for (int j = 0; j < G; ++j) offsets[j] = 0.f;
     u4 ones_bits = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
@@ -311,6 +322,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
 
     for (int n = 0; n < count; ++n) {
         float ksc[G], kof[G], vsc[G], vof[G];  // scales and offsets of key `lane`; of K, offset - 24 scale
+        float largest = 0.f;  // of V's (NaN if one is)
 #pragma unroll
         for (int j = 0; j < G; ++j) {
             const bool used = j * (DP / G) < p.dim;  // (what stands past dim is not)
@@ -320,6 +332,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
             ksc[j] += 0.f * ksc[j] + 0.f * of;  // (NaN where one is not finite: a score of -infinity would be no key)
             vsc[j] = used ? (float)vs_next[j][0] : 0.f;
             vof[j] = used ? (float)vs_next[j][1] : 0.f;
+            largest = larger(larger(largest, __builtin_fabsf(vsc[j])), __builtin_fabsf(vof[j]));
         }
         const unsigned there = there_next;
         lanes_meet();  // the last tile's V has been read
@@ -376,10 +389,9 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         // What a value stands for whose scale or offset is not finite is NaN, and
         // 0 times it has to be 0 where it is not seen: it is taken out, and the
         // offsets of the rows that see it are NaN.
-        float odd = 0.f;
-#pragma unroll
-        for (int j = 0; j < G; ++j) odd += 0.f * vsc[j] + 0.f * vof[j];
-        if (__ballot(odd != 0.f)) {
+        bool lowered = false;
+        const uint64_t large_keys = __ballot(!(largest < LARGE<T>));
+        if (large_keys != 0) {
 #pragma unroll
             for (int j = 0; j < G; ++j) {
                 const bool is = 0.f * vsc[j] + 0.f * vof[j] != 0.f;
@@ -387,15 +399,23 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
                 if (is) vsc[j] = vof[j] = 0.f;
                 if (which & seen) offsets[j] = NAN;
             }
+            if constexpr (LARGE<T> < INFINITY) {
+                uint64_t row = __ballot(((unsigned)(large_keys >> (16 * g)) & seen) != 0);  // (seen: 16 bits)
+                row |= row >> 32;
+                row |= row >> 16;
+                const unsigned now = (unsigned)row & 0xFFFFu;
+                lowered = (now & ~lower) != 0;
+                lower |= now;
+            }
         }
         // ---- softmax: the maximum moves when a score passes it by 2^8
         float most = score[0][0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) most = larger(most, score[e / 4][e % 4]);
         most *= p.scale2;
-        if (__ballot(most > limit)) {
+        if (__ballot(most > limit) != 0 || lowered) {
             const float now = larger(across_max(most), top);
-            const float next = now == -INFINITY ? 0.f : now;
+            const float next = now == -INFINITY ? 0.f : LARGE<T> < INFINITY && (lower >> c & 1) ? now + LOWER : now;
             const float keep = top == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(base2 - next);
             top = now;
             limit = now + 8.f;
@@ -453,7 +473,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
     lanes_meet();
     total = across_sum(total);
     if (g == 0) {
-        tops[wave][c] = top;
+        tops[wave][c] = top == -INFINITY ? top : base2;  // (what the sums are relative to)
         sums[wave][c] = total;
     }
 #pragma unroll
