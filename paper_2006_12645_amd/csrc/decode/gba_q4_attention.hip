@@ -170,6 +170,10 @@ extern "C" gba_status gba_q4_attend(const gba_q4_attention *desc, gba_stream_t s
     const float scale2 = d.scale * LOG2_E;
     a.sign = scale2 > 0.f ? 1.f : scale2 < 0.f ? -1.f : 0.f;
     a.scale2 = scale2 > 0.f ? scale2 : scale2 < 0.f ? -scale2 : 1.f;
+    if (c.dtype == GBA_BF16) {  // what keys were divided by, or with a scale that has no room for it the queries
+        if (a.scale2 < 0x1p119f) a.scale2 *= 1.f / KEYS_DOWN<BF16>;
+        else a.sign *= 1.f / KEYS_DOWN<BF16>;
+    }
     a.window = d.window != 0 ? d.window : INT64_MAX;
     a.sinks = d.window != 0 ? (int)min_of(d.sinks, INT_MAX) : 0;
     a.row_tiles = sh.row_tiles;

@@ -89,6 +89,13 @@ template <class T>
 constexpr float LARGE = std::is_same_v<T, BF16> ? 0x1p80f : INFINITY;
 constexpr float LOWER = 48.f;
 
+// Keys are taken 2^-8 times in bf16, where 24 scales, and scores of (16 + code)
+// scales, may have no place in fp32 otherwise; scores are multiplied by 2^8 again
+// with the scale of the softmax.  Exact: what that leaves of the smallest
+// numbers fp32 holds as they are.
+template <class T>
+constexpr float KEYS_DOWN = std::is_same_v<T, BF16> ? 0x1p-8f : 1.f;
+
 // A value of the even rows of 16 lanes in both rows of their pair, and that of
 // the odd ones; the same of the wave's halves.
 struct Two {
@@ -326,8 +333,8 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
 #pragma unroll
         for (int j = 0; j < G; ++j) {
             const bool used = j * (DP / G) < p.dim;  // (what stands past dim is not)
-            ksc[j] = used ? (float)ks_next[j][0] : 0.f;
-            const float of = used ? (float)ks_next[j][1] : 0.f;
+            ksc[j] = used ? (float)ks_next[j][0] * KEYS_DOWN<T> : 0.f;
+            const float of = used ? (float)ks_next[j][1] * KEYS_DOWN<T> : 0.f;
             kof[j] = __builtin_fmaf(-24.f, ksc[j], of);
             ksc[j] += 0.f * ksc[j] + 0.f * of;  // (NaN where one is not finite: a score of -infinity would be no key)
             vsc[j] = used ? (float)vs_next[j][0] : 0.f;

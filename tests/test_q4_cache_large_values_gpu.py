@@ -1,6 +1,6 @@
-"""Attention over a cache in 4 bits whose values are next to bf16's largest,
-where a sum of (16 + code) scales, or of 24 scales, is no fp32 number although
-the result is one.
+"""Attention over a cache in 4 bits whose values or keys are next to bf16's
+largest, where a sum of (16 + code) scales, or of 24 scales, is no fp32
+number although the result is one.
 
 Scales and offsets are multiplied by powers of two, so the references and bounds
 are those of ordinary values, multiplied likewise."""
@@ -78,3 +78,29 @@ def test_values_that_no_row_sees(name, ws, window):
             b.cache.v_scales[page, :, at] = 3e38 if pos % 3 else float("nan")
     print("CASE q4 large unseen", name, ws, flush=True)
     assert torch.equal(b.attend(masks, **args), want)
+
+
+@pytest.mark.parametrize("name,ws,window", CALLS)
+def test_keys(name, ws, window):
+    """Keys whose group spans more than fp32 holds of 24 scales, and small queries."""
+    b, masks = batch(name, 6)
+    multiply(b.cache.k_scales, 126)
+    b.q, scale = b.q * 2.0 ** -100, b.scale * 2.0 ** -26
+    assert 24 * largest(b.cache.k_scales[..., 0]) > 2.0 ** 128
+    print("CASE q4 large keys", name, ws, window, flush=True)
+    got = b.attend(masks, window=window, sinks=3 if window else 0, workspace=ws, scale=scale)
+    b.scale = scale
+    b.check(got, masks, window, 3 if window else 0)
+
+
+@pytest.mark.parametrize("half", [60, 63])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_a_large_softmax_scale(sign, half):
+    """Scores of ordinary size by a scale near the largest and small keys and queries."""
+    b, masks = batch("whole", 8)
+    multiply(b.cache.k_scales, -half)
+    b.q, scale = b.q * 2.0 ** -half, sign * b.scale * 2.0 ** (2 * half)
+    print("CASE q4 large scale", sign, half, flush=True)
+    got = b.attend(masks, scale=scale)
+    b.scale = scale
+    b.check(got, masks)
