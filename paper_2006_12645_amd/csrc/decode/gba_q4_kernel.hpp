@@ -96,6 +96,12 @@ constexpr float LOWER = 48.f;
 template <class T>
 constexpr float KEYS_DOWN = std::is_same_v<T, BF16> ? 0x1p-8f : 1.f;
 
+// The query of a row that has an element of 2^65 or more is taken 2^-16 times in
+// bf16, where a sum of (16 + code) of them may have no place in fp32 otherwise.
+// (Not with a scale of the softmax that has no room for it: scores of such queries
+// have none either.)
+constexpr float QUERY_DOWN = 0x1p-16f, NO_ROOM = 0x1p100f;
+
 // A value of the even rows of 16 lanes in both rows of their pair, and that of
 // the odd ones; the same of the wave's halves.
 struct Two {
@@ -281,24 +287,39 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
     const bool real = my_row < rows;
     const int index = real ? my_row / p.share : 0, token = rq.first + index;  // its token among the new ones, among all
     const elem *q = static_cast<const elem *>(p.q) + token * p.q_token + (head * p.share + (real ? my_row % p.share : 0)) * p.q_head;
-#pragma unroll
-    for (int j = 0; j < G; ++j) X[j] = 0.f;
+    float scale2 = p.scale2;
+    unsigned large = 0;  // at the top of an element's exponent: two ones, which it has from 2^65 on
 #pragma unroll
     for (int s = 0; s < STEPS; ++s) {
         const int d = 32 * s + 8 * g;
-        vec8 y = {};
-        if (real && d < p.dim) y = *reinterpret_cast<const vec8 *>(q + d);
+        u4 y = {};
+        if (real && d < p.dim) y = *reinterpret_cast<const u4 *>(q + d);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const elem signed_y = p.sign != 1.f ? (elem)((float)y[e] * p.sign) : y[e];
-            query[s][2 * (e % 4) + e / 4] = signed_y;
-            X[s / (STEPS / G)] += (float)signed_y;
+        for (int e = 0; e < 4; ++e) large |= y[e] & (y[e] << 1);
+        const vec8 values = __builtin_bit_cast(vec8, y);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) query[s][2 * (e % 4) + e / 4] = p.sign != 1.f ? (elem)((float)values[e] * p.sign) : values[e];
+    }
+    if constexpr (std::is_same_v<T, BF16>) {
+        uint64_t row = __ballot((large & 0x40004000u) != 0 && p.scale2 < NO_ROOM);
+        if (row != 0) {
+            row |= row >> 32;
+            row |= row >> 16;
+            if (row >> c & 1) {
+                scale2 *= 1.f / QUERY_DOWN;
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) query[s][e] = (elem)((float)query[s][e] * QUERY_DOWN);
+            }
         }
     }
 #pragma unroll
     for (int j = 0; j < G; ++j) {
-        X[j] = across_sum(X[j]);
-        X[j] += X[j] - X[j];  // (NaN where the query is not finite)
+        f4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int s = j * (STEPS / G); s < (j + 1) * (STEPS / G); ++s) sum = T::mfma(vec8{1, 1, 1, 1, 1, 1, 1, 1}, query[s], sum);
+        X[j] = sum[0] + (sum[0] - sum[0]);  // (NaN where the query is not finite)
     }
     const bool masked = p.mask != nullptr;
     uint64_t sees = masked ? p.mask[token] : 0;  // bits of the new tokens that the row sees
@@ -419,7 +440,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         float most = score[0][0];
 #pragma unroll
         for (int e = 1; e < 16; ++e) most = larger(most, score[e / 4][e % 4]);
-        most *= p.scale2;
+        most *= scale2;
         if (__ballot(most > limit) != 0 || lowered) {
             const float now = larger(across_max(most), top);
             const float next = now == -INFINITY ? 0.f : LARGE<T> < INFINITY && (lower >> c & 1) ? now + LOWER : now;
@@ -438,7 +459,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
-            score[e / 4][e % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[e / 4][e % 4], p.scale2, -base2));
+            score[e / 4][e % 4] = __builtin_amdgcn_exp2f(__builtin_fmaf(score[e / 4][e % 4], scale2, -base2));
             total += score[e / 4][e % 4];
         }
         // ---- weights of each group and its blocks of dim

@@ -1,5 +1,5 @@
-"""Attention over a cache in 4 bits whose values or keys are next to bf16's
-largest, where a sum of (16 + code) scales, or of 24 scales, is no fp32
+"""Attention over a cache in 4 bits whose values, keys or queries are next to
+bf16's largest, where a sum of (16 + code) scales, or of 24 scales, is no fp32
 number although the result is one.
 
 Scales and offsets are multiplied by powers of two, so the references and bounds
@@ -88,6 +88,21 @@ def test_keys(name, ws, window):
     b.q, scale = b.q * 2.0 ** -100, b.scale * 2.0 ** -26
     assert 24 * largest(b.cache.k_scales[..., 0]) > 2.0 ** 128
     print("CASE q4 large keys", name, ws, window, flush=True)
+    got = b.attend(masks, window=window, sinks=3 if window else 0, workspace=ws, scale=scale)
+    b.scale = scale
+    b.check(got, masks, window, 3 if window else 0)
+
+
+@pytest.mark.parametrize("name,ws,window", CALLS)
+def test_queries(name, ws, window):
+    """Queries next to the largest and small keys; of two rows of a tile, one has
+    ordinary queries and scores near 0."""
+    b, masks = batch(name, 7)
+    multiply(b.cache.k_scales, -90)
+    b.q, scale = b.q * 2.0 ** 120, b.scale * 2.0 ** -30
+    b.q[0, 0] *= 2.0 ** -120
+    assert largest(b.q) > 2.0 ** 121
+    print("CASE q4 large queries", name, ws, window, flush=True)
     got = b.attend(masks, window=window, sinks=3 if window else 0, workspace=ws, scale=scale)
     b.scale = scale
     b.check(got, masks, window, 3 if window else 0)
