@@ -79,7 +79,7 @@ __device__ __forceinline__ int key_word(int w)
 // ends: scale = (high - low) / 15 and offset = low + 8 scale, each rounded to
 // the cache's type; the codes are those nearest to the values, given these two.
 // The steps are those of include/gba.h, in fp32, and nothing is contracted that
-// would round differently: 0.5 high, 0.5 low and 8 scale are exact.
+// would round differently: 0.5 high and 0.5 low are exact.
 template <class T, int WORDS, bool WIDE, int AT_ONCE>
 __global__ void __launch_bounds__(256) q4_store_kernel(Q4StoreArgs p)
 {
@@ -131,7 +131,7 @@ __global__ void __launch_bounds__(256) q4_store_kernel(Q4StoreArgs p)
         const bool finite = high - high == 0.f && low - low == 0.f;
         float scale = finite ? (float)(elem)((0.5f * high - 0.5f * low) * (2.f / 15.f)) : 0.f;
         if (scale < SMALLEST_SCALE) scale = 0.f;
-        const float offset = finite ? (float)(elem)(low + 8.f * scale) : high < low ? 0.f : NAN;  // (padding: no value)
+        const float offset = finite ? (float)(elem)q4_offset(low, scale) : high < low ? 0.f : NAN;  // (padding: no value)
         const float inverse = scale > 0.f ? 1.f / scale : 0.f;
         // 1.5 2^23 + 8 + steps, rounded to a whole number by that sum, has the code
         // in its low bits; what else these numbers hold adds up to a constant.

@@ -9,6 +9,11 @@ namespace gba {
 // its lowest value.
 constexpr float SMALLEST_SCALE = 0x1p-100f;
 
+// The offset of a group before its rounding: low + 8 scale, rounded once.  8 scale
+// has no place in fp32 where a group spans nearly all of bf16, so the product is
+// part of the sum whatever the compiler contracts.
+__host__ __device__ __forceinline__ float q4_offset(float low, float scale) { return __builtin_fmaf(8.f, scale, low); }
+
 // Elements of a stored row: dim, padded.
 inline int q4_width(int64_t dim) { return dim <= 64 ? 64 : dim <= 128 ? 128 : 256; }
 
