@@ -297,6 +297,10 @@ __device__ __forceinline__ f4 load_four(const float *at)
     }
 }
 
+// Until this wave's stores have arrived: those before this in the source, which the
+// compiler moves past no assembly that may touch memory.
+__device__ __forceinline__ void stores_arrive() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
 // Four elements of a row of `n` runs, added in their order.  A run's maximum is
 // -infinity where the row sees none of its keys, and where all of its scores
 // are NaN: its sums, zeros or NaN, are added all the same.
@@ -373,13 +377,18 @@ __device__ __forceinline__ void join_by_last(const AttentionArgs &p, const Run &
     }
 }
 
-// The same where the sums were written with to_other_xcds: every wave waits for
-// its stores, and the count needs no release.
+// The same where the sums were written with to_other_xcds.  The language orders
+// nothing here, since the count is relaxed: a release would write back the XCD's
+// L2.  What is relied upon is this hardware's: a store that writes through has
+// arrived where every XCD reads it when the wave's vmcnt no longer counts it, each
+// wave waits for that before the barrier, and so before the count; loads of agent
+// scope are not served from an L2 that may be out of date.  To the compiler the
+// assembly before the count and after it is an order of memory.
 template <class T, int DP, int ROWS, int THREADS>
 __device__ __forceinline__ void join_written_through(const AttentionArgs &p, const Run &run, const Request &rq, int head, int row_tile, int rows)
 {
     __shared__ int last;
-    wait_vm_lgkm0<0>();
+    stores_arrive();
     __syncthreads();
     const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
     if (threadIdx.x == 0) {
@@ -388,6 +397,7 @@ __device__ __forceinline__ void join_written_through(const AttentionArgs &p, con
     }
     __syncthreads();
     if (!last) return;
+    asm volatile("" ::: "memory");
     const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
     const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
     constexpr int FOURS = DP / 4;
