@@ -79,18 +79,21 @@ Shape shape_of(const gba_q4_attention &d)
     if (d.requests > SPLIT_REQUESTS || most_keys <= SHORTEST || alone) return s;
     const int64_t tiles = c.heads * (int64_t)s.row_tiles, pairs = d.requests * tiles;
     int64_t slots = 0;
+    const int64_t sums = Q4_ROWS * (c.dim + 2) * (int64_t)sizeof(float);
     if (d.window != 0) {
-        s.length = (int)run_of_window(pairs, most_keys, 256, FIXED_KEYS, Q4_KEYS * Q4_WAVES);
-        s.each = (int)div_up(most_keys, s.length);
-        slots = d.requests * s.each;
+        const int64_t length = run_of_window(pairs, sums, most_keys, 256, FIXED_KEYS, Q4_KEYS * Q4_WAVES);
+        const int64_t each = div_up(most_keys, length);
+        if (each == 1) return s;
+        s.length = (int)length;
+        s.each = (int)each;
+        slots = d.requests * each;
     } else {
         slots = d.requests + div_up(runs_to_aim_at(pairs), tiles);
+        if (slots * tiles > (int64_t)COUNTERS) return s;  // (more than fill the chip as they are)
     }
-    const int64_t counted = slots * tiles;
-    if (s.each == 1 || counted > (int64_t)COUNTERS) return s;  // (more than fill the chip as they are)
     s.target = (int)div_up(runs_to_aim_at(pairs), tiles);
     s.slots = (int)slots;
-    s.bytes = COUNTER_BYTES + (size_t)counted * Q4_ROWS * (c.dim + 2) * sizeof(float);
+    s.bytes = COUNTER_BYTES + (size_t)(slots * tiles * sums);
     return s;
 }
 

@@ -786,21 +786,22 @@ Shape shape_of(const gba_attention &d, int64_t window, int64_t sinks)
     int64_t most_keys = d.width * c.block_size;  // of a request
     if (window != 0) most_keys = min_of(most_keys, min_of(window, INT_MAX) + min_of(sinks, INT_MAX) + most_new(d) + 2 * KEYS);  // (in whole tiles)
     if (d.requests <= SPLIT_REQUESTS && most_keys > SHORTEST && !(window != 0 && tiles_alone(d, s, window, sinks))) {
-        s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
-        s.slots = (int)d.requests + s.target;
+        const int64_t pairs = d.requests * c.heads * s.row_tiles, sums = 16 * s.rt * s.rg * (c.dim + 2) * (int64_t)sizeof(float);
+        int64_t slots = d.requests;
         if (window != 0) {
-            s.length = (int)run_of_window(d.requests * c.heads * s.row_tiles, most_keys, s.dp == 64 && s.rg <= 2 ? 512 : 256, FIXED_KEYS, 4 * KEYS);
-            s.each = (int)div_up(most_keys, s.length);
-            s.slots = (int)(d.requests * s.each);
-            if (s.each == 1) {
-                s.target = s.length = s.each = 0;
-                return s;
-            }
+            const int64_t length = run_of_window(pairs, sums, most_keys, s.dp == 64 && s.rg <= 2 ? 512 : 256, FIXED_KEYS, 4 * KEYS);
+            const int64_t each = div_up(most_keys, length);
+            if (each == 1) return s;
+            s.length = (int)length;
+            s.each = (int)each;
+            slots *= each;
         }
-        s.counts = s.rg <= 2 && (window != 0 || s.rt * s.rg * d.requests * c.heads * s.row_tiles * div_up(most_keys, SHORTEST) <= FEW_RUNS) &&
+        s.target = (int)div_up(runs_to_aim_at(d, s.rg, s.row_tiles), c.heads * (int64_t)s.row_tiles);
+        s.slots = (int)(window != 0 ? slots : slots + s.target);
+        s.counts = s.rg <= 2 && (window != 0 || s.rt * s.rg * pairs * div_up(most_keys, SHORTEST) <= FEW_RUNS) &&
                    (size_t)s.slots * c.heads * s.row_tiles <= COUNTERS;
         s.header = COUNTER_BYTES + (size_t)div_up(d.requests * 8, 256) * 256;
-        s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * (16 * s.rt * s.rg) * (c.dim + 2) * sizeof(float);
+        s.bytes = s.header + (size_t)s.slots * c.heads * s.row_tiles * sums;
     }
     return s;
 }
