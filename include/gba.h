@@ -573,7 +573,9 @@ typedef struct gba_attention {
  *     out = sum_p exp(s_p - m) V_p / sum_p exp(s_p - m),   m = max_p s_p
  * and zeros where it sees none.  The weights exp(s_p - m) are rounded to the
  * cache's dtype for the second product, as its matrix instructions take them,
- * and their sum is that of the rounded ones.
+ * and their sum is that of the rounded ones.  Sums are of fp32, and in bf16 of
+ * weights of up to 2^8: where a row sees P positions they have room for every V
+ * below 2^119 / P, and larger ones may overflow.
  * What the cache holds at positions that a token does not see has no effect
  * on its rows, infinities and NaN included (a position whose block is outside
  * the cache counts as not seen, and so does one with a score of -infinity).  A
@@ -709,10 +711,12 @@ typedef struct gba_q4_attention {
  * gba_q4_attend -- attention of each request's new tokens over a cache in 4
  * bits: the formula of gba_tree_attention, or with a window that of
  * gba_window_attention, for the values that the codes stand for.  Those are not
- * rounded; the softmax weights enter the second product with 16 bits, and their
- * sum is in fp32.  What is said there of positions that a token does not see, of
- * missing blocks, rows of no request, offsets and the workspace holds here too.
- * A row whose query is not finite is NaN.
+ * rounded.  The softmax weights, times the scales of V, are for the second
+ * product: with fp16 as two bf16 numbers, 16 bits, and with bf16 as one, 8 bits.
+ * Their own sum is of weights that are not rounded, in fp32.  What is said there
+ * of positions that a token does not see, of missing blocks, rows of no request,
+ * offsets and the workspace holds here too.  A row whose query is not finite is
+ * NaN, and zeros if it sees no position.
  *
  * q and out 16-byte aligned with strides that are multiples of 8 (out: 4), but in
  * dimensions of one element.

@@ -27,7 +27,7 @@ gba_status validate(const gba_q4_attention &d)
     if (d.mask != nullptr && d.max_new > 64) return GBA_EUNSUPPORTED;
     if (nothing_to_do(d)) return GBA_OK;
     if (c.heads == 0 || d.q_heads % c.heads != 0) return GBA_EINVAL;
-    if (most_new(d) * (d.q_heads / c.heads) > INT_MAX - 255) return GBA_EUNSUPPORTED;  // rows of a request and head, in tiles of up to 64
+    if (most_new(d) * (d.q_heads / c.heads) > INT_MAX - 255) return GBA_EUNSUPPORTED;  // rows of a request and head, in tiles of 16
     if (d.q == nullptr || d.out == nullptr || d.lens == nullptr || d.offsets == nullptr) return GBA_EINVAL;
     if (d.width > 0 && d.table == nullptr) return GBA_EINVAL;
     // (a stride of a dimension of one element is not used)
