@@ -143,8 +143,9 @@ struct Run {
 // factor covers its rounding.
 //
 // With a window, a run that is all of a request's is that of the row tile: its
-// `rows` rows from row0 on alone say which keys it has.
-template <bool WINDOW, int TILE>
+// `rows` rows from row0 on alone say which keys it has.  Not BY_MEAN: runs, where
+// there are any, are of p.length.
+template <bool WINDOW, int TILE, bool BY_MEAN>
 __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, int step, int row0, int rows)
 {
     Run u;
@@ -164,7 +165,7 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
     }
     u.r = -1;
     if constexpr (WINDOW) {
-        if (p.length != 0) {
+        if (!BY_MEAN || p.length != 0) {
             const int r = x / p.each, i = x - r * p.each;
             Request q = request_of(p, r);
             if (q.fresh == 0) return u;
@@ -179,41 +180,43 @@ __device__ __forceinline__ Run run_of(const AttentionArgs &p, int x, int lane, i
             return u;
         }
     }
-    float keys = 0.f;
-    Request q = {0, 0, 0, 0, 0, 0};
-    auto look = [&](int r) {
-        q = request_of(p, r);
-        if constexpr (WINDOW) bound_keys<TILE>(p, 0, q.fresh - 1, q);
-    };
-    for (int r = lane; r < p.requests; r += 64) {
-        look(r);
-        if (q.fresh > 0) keys += (float)q.end;
-    }
-    const float mean = wave_total(keys) / (float)p.target * 1.00001f;
-    int length = mean < (float)(INT_MAX / step * step - step) ? ((int)mean / step + 1) * step : INT_MAX;
-    if (length < SHORTEST) length = SHORTEST;
-    length = uniform(length);
-    int before = 0;
-    for (int base = 0; base < p.requests; base += 64) {
-        const int r = base + lane;
-        if (p.requests > 64 && r < p.requests) look(r);
-        int n = 0;
-        if (r < p.requests && q.fresh > 0) n = q.end > length ? (q.end - 1) / length + 1 : 1;
-        const int upto = wave_sums(n);
-        const uint64_t past = __ballot(before + upto > x);
-        if (past != 0) {
-            const int l = __ffsll((unsigned long long)past) - 1;
-            u.r = base + l;
-            u.n = __builtin_amdgcn_readlane(n, l);
-            u.first = before + __builtin_amdgcn_readlane(upto, l) - u.n;
-            u.from = (x - u.first) * length;
-            u.q = {__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.fresh, l), __builtin_amdgcn_readlane(q.kept, l),
-                   __builtin_amdgcn_readlane(q.end, l), WINDOW ? __builtin_amdgcn_readlane(q.split, l) : 0,
-                   WINDOW ? __builtin_amdgcn_readlane(q.gap, l) : 0};
-            u.to = u.q.end - u.from > length ? u.from + length : u.q.end;
-            return u;
+    if constexpr (BY_MEAN) {
+        float keys = 0.f;
+        Request q = {0, 0, 0, 0, 0, 0};
+        auto look = [&](int r) {
+            q = request_of(p, r);
+            if constexpr (WINDOW) bound_keys<TILE>(p, 0, q.fresh - 1, q);
+        };
+        for (int r = lane; r < p.requests; r += 64) {
+            look(r);
+            if (q.fresh > 0) keys += (float)q.end;
         }
-        before += __builtin_amdgcn_readlane(upto, 63);
+        const float mean = wave_total(keys) / (float)p.target * 1.00001f;
+        int length = mean < (float)(INT_MAX / step * step - step) ? ((int)mean / step + 1) * step : INT_MAX;
+        if (length < SHORTEST) length = SHORTEST;
+        length = uniform(length);
+        int before = 0;
+        for (int base = 0; base < p.requests; base += 64) {
+            const int r = base + lane;
+            if (p.requests > 64 && r < p.requests) look(r);
+            int n = 0;
+            if (r < p.requests && q.fresh > 0) n = q.end > length ? (q.end - 1) / length + 1 : 1;
+            const int upto = wave_sums(n);
+            const uint64_t past = __ballot(before + upto > x);
+            if (past != 0) {
+                const int l = __ffsll((unsigned long long)past) - 1;
+                u.r = base + l;
+                u.n = __builtin_amdgcn_readlane(n, l);
+                u.first = before + __builtin_amdgcn_readlane(upto, l) - u.n;
+                u.from = (x - u.first) * length;
+                u.q = {__builtin_amdgcn_readlane(q.first, l), __builtin_amdgcn_readlane(q.fresh, l), __builtin_amdgcn_readlane(q.kept, l),
+                       __builtin_amdgcn_readlane(q.end, l), WINDOW ? __builtin_amdgcn_readlane(q.split, l) : 0,
+                       WINDOW ? __builtin_amdgcn_readlane(q.gap, l) : 0};
+                u.to = u.q.end - u.from > length ? u.from + length : u.q.end;
+                return u;
+            }
+            before += __builtin_amdgcn_readlane(upto, 63);
+        }
     }
     return u;
 }
@@ -304,7 +307,7 @@ __device__ __forceinline__ void stores_arrive() { asm volatile("s_waitcnt vmcnt(
 // Four elements of a row of `n` runs, added in their order.  A run's maximum is
 // -infinity where the row sees none of its keys, and where all of its scores
 // are NaN: its sums, zeros or NaN, are added all the same.
-template <class T, bool OTHERS = false>
+template <class T, bool OTHERS>
 __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_at, const float *l_at, int64_t stride, int n, typename T::elem *to)
 {
     typedef typename T::elem elem;
@@ -346,23 +349,36 @@ __device__ __forceinline__ void join_runs(const float *sum_at, const float *top_
 }
 
 // A workgroup whose sums of one run, ROWS rows of `row_tile`, are written: the
-// one that is the request's last joins them all.  Every wave's stores are done
-// at the barrier; one thread's release makes them visible to other XCDs before
-// it counts the run, and who counts the last one acquires those of all others.
-template <class T, int DP, int ROWS, int THREADS>
+// one that is the request's last joins them all.  Every wave's stores are done at
+// the barrier.
+//
+// Not WRITTEN_THROUGH: one thread's release makes them visible to other XCDs
+// before it counts the run, and who counts the last one acquires those of all
+// others.
+//
+// WRITTEN_THROUGH, with to_other_xcds: the language orders nothing here, since the
+// count is relaxed: a release would write back the XCD's L2.  What is relied upon is
+// this hardware's: a store that writes through has arrived where every XCD reads it
+// when the wave's vmcnt no longer counts it, each wave waits for that before the
+// barrier, and so before the count; loads of agent scope are not served from an L2
+// that may be out of date.  To the compiler the assembly before the count and after
+// it is an order of memory.
+template <class T, int DP, int ROWS, int THREADS, bool WRITTEN_THROUGH>
 __device__ __forceinline__ void join_by_last(const AttentionArgs &p, const Run &run, const Request &rq, int head, int row_tile, int rows)
 {
     __shared__ int last;
-    wait_vm_lgkm0<0>();
+    if constexpr (WRITTEN_THROUGH) stores_arrive();
+    else wait_vm_lgkm0<0>();
     __syncthreads();
     const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
     if (threadIdx.x == 0) {
-        last = __hip_atomic_fetch_add(p.arrived + place, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
+        last = __hip_atomic_fetch_add(p.arrived + place, 1, WRITTEN_THROUGH ? __ATOMIC_RELAXED : __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
         if (last) __hip_atomic_store(p.arrived + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
     __syncthreads();
     if (!last) return;
-    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+    if constexpr (WRITTEN_THROUGH) asm volatile("" ::: "memory");
+    else __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
     const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
     const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
     constexpr int FOURS = DP / 4;
@@ -372,43 +388,8 @@ __device__ __forceinline__ void join_by_last(const AttentionArgs &p, const Run &
         if (row0 + row >= rows || d >= p.dim) continue;
         const float *top_at = first_part + ROWS * p.dim + row;
         const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
-        join_runs<T>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
-                     static_cast<typename T::elem *>(p.out) + token * p.out_token + h * p.out_head + d);
-    }
-}
-
-// The same where the sums were written with to_other_xcds.  The language orders
-// nothing here, since the count is relaxed: a release would write back the XCD's
-// L2.  What is relied upon is this hardware's: a store that writes through has
-// arrived where every XCD reads it when the wave's vmcnt no longer counts it, each
-// wave waits for that before the barrier, and so before the count; loads of agent
-// scope are not served from an L2 that may be out of date.  To the compiler the
-// assembly before the count and after it is an order of memory.
-template <class T, int DP, int ROWS, int THREADS>
-__device__ __forceinline__ void join_written_through(const AttentionArgs &p, const Run &run, const Request &rq, int head, int row_tile, int rows)
-{
-    __shared__ int last;
-    stores_arrive();
-    __syncthreads();
-    const int64_t place = ((int64_t)run.first * p.heads + head) * p.row_tiles + row_tile;
-    if (threadIdx.x == 0) {
-        last = __hip_atomic_fetch_add(p.arrived + place, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == run.n - 1;
-        if (last) __hip_atomic_store(p.arrived + place, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    }
-    __syncthreads();
-    if (!last) return;
-    asm volatile("" ::: "memory");
-    const int64_t stride = (int64_t)p.heads * p.row_tiles * ROWS * (p.dim + 2);
-    const float *first_part = p.part + place * ROWS * (int64_t)(p.dim + 2);
-    constexpr int FOURS = DP / 4;
-    const int row0 = row_tile * ROWS;
-    for (int j = threadIdx.x; j < ROWS * FOURS; j += THREADS) {
-        const int row = j / FOURS, d = 4 * (j % FOURS);
-        if (row0 + row >= rows || d >= p.dim) continue;
-        const float *top_at = first_part + ROWS * p.dim + row;
-        const int token = rq.first + (row0 + row) / p.share, h = head * p.share + (row0 + row) % p.share;
-        join_runs<T, true>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
-                     static_cast<typename T::elem *>(p.out) + token * p.out_token + h * p.out_head + d);
+        join_runs<T, WRITTEN_THROUGH>(first_part + row * p.dim + d, top_at, top_at + ROWS, stride, run.n,
+                                      static_cast<typename T::elem *>(p.out) + token * p.out_token + h * p.out_head + d);
     }
 }
 
@@ -443,7 +424,7 @@ __global__ void __launch_bounds__(512) join_rows_kernel(AttentionArgs p, int til
         const int head = j / fours, d = 4 * (j - head * fours), kv = head / p.share;
         const int row = (t - rq.first) * p.share + head - kv * p.share, tile = row / tile_rows, in_tile = row - tile * tile_rows;
         const float *part = p.part + (((int64_t)x0 * p.heads + kv) * p.row_tiles + tile) * tile_size, *top_at = part + tile_rows * p.dim + in_tile;
-        join_runs<T>(part + in_tile * p.dim + d, top_at, top_at + tile_rows, stride, n,
+        join_runs<T, false>(part + in_tile * p.dim + d, top_at, top_at + tile_rows, stride, n,
                      static_cast<typename T::elem *>(p.out) + t * p.out_token + head * p.out_head + d);
     }
 }

@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
         min((int64_t)p.width * p.block_size, p.window) >= Q4_SORTED_KEYS)
         x = nth_longest(p, x, lane);
     const int row0 = row_tile * ROWS;
-    const Run run = run_of<true, Q4_KEYS>(p, x, lane, Q4_KEYS * Q4_WAVES, row0, ROWS);
+    const Run run = run_of<true, Q4_KEYS, true>(p, x, lane, Q4_KEYS * Q4_WAVES, row0, ROWS);
     if (run.r < 0) return;
     const Request rq = run.q;
     const int rows = rq.fresh * p.share;
@@ -545,7 +545,7 @@ __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention
             }
         }
     }
-    if (!whole_request) join_written_through<T, DP, ROWS, 64 * Q4_WAVES>(p, run, rq, head, row_tile, rows);
+    if (!whole_request) join_by_last<T, DP, ROWS, 64 * Q4_WAVES, true>(p, run, rq, head, row_tile, rows);
 }
 
 }  // namespace

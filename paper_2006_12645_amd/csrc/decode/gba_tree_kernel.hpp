@@ -152,7 +152,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     const int head = item % p.heads, x = item / p.heads;
     if (x >= p.slots) return;
     const int row0 = row_tile * ROWS;
-    const Run run = run_of<WINDOW, KEYS>(p, x, lane, KEYS * KG, row0, ROWS);
+    const Run run = run_of<WINDOW, KEYS, !WINDOW>(p, x, lane, KEYS * KG, row0, ROWS);
     if (run.r < 0) return;
     const Request rq = run.q;
     const int rows = rq.fresh * p.share;
@@ -684,8 +684,7 @@ __global__ void __launch_bounds__((threads_of<DP, RG>()), (RG == 1 ? 1 : 2)) att
     }
     if constexpr (RG <= 2) {
         if (whole_request || p.arrived == nullptr) return;
-        if constexpr (WINDOW) join_written_through<T, DP, ROWS, 64 * WAVES>(p, run, rq, head, row_tile, rows);
-        else join_by_last<T, DP, ROWS, 64 * WAVES>(p, run, rq, head, row_tile, rows);
+        join_by_last<T, DP, ROWS, 64 * WAVES, WINDOW>(p, run, rq, head, row_tile, rows);
     }
 }
 
