@@ -224,14 +224,10 @@ class Q4Cache:
     """
 
     def __init__(self, k, v, k_scales, v_scales, *, dim, group=64):
-        if group not in (32, 64, 128):
-            raise ValueError("group must be 32, 64 or 128")
-        if dim % 8 or not 0 < dim <= 256:
-            raise ValueError("dim must be a multiple of 8 up to 256")
+        width = self._width(dim, group)
         _gpu("k", k, torch.uint8)
         if k_scales.dtype not in DTYPES:
             raise TypeError("k_scales must be a float16 or bfloat16 CUDA tensor")
-        width = 64 if dim <= 64 else 128 if dim <= 128 else 256
         if k.dim() != 4 or k.shape[2] == 0 or k.shape[2] % 16:
             raise ValueError(f"k must be (num_blocks, heads, a multiple of 16, {width // 2})")
         codes, scales = (*k.shape[:3], width // 2), (*k.shape[:3], max(1, width // group), 2)
@@ -248,10 +244,18 @@ class Q4Cache:
         self._at, self._index = ctypes.addressof(self._desc), k.device.index
         self._store, self._load, self._attend = _calls().store_q4, _calls().load_q4, _calls().attend_q4
 
+    @staticmethod
+    def _width(dim, group):
+        if group not in (32, 64, 128):
+            raise ValueError("group must be 32, 64 or 128")
+        if dim % 8 or not 0 < dim <= 256:
+            raise ValueError("dim must be a multiple of 8 up to 256")
+        return 64 if dim <= 64 else 128 if dim <= 128 else 256
+
     @classmethod
     def empty(cls, num_blocks, block_size, heads, dim, dtype, *, group=64, device="cuda"):
         """A cache that holds nothing yet."""
-        width = 64 if dim <= 64 else 128 if dim <= 128 else 256
+        width = cls._width(dim, group)
         lead = (num_blocks, heads, block_size)
         codes = [torch.empty((*lead, width // 2), dtype=torch.uint8, device=device) for _ in range(2)]
         scales = [torch.empty((*lead, max(1, width // group), 2), dtype=dtype, device=device) for _ in range(2)]
