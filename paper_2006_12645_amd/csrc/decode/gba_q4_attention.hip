@@ -45,6 +45,13 @@ gba_status validate(const gba_q4_attention &d)
 // heads (4236 keys, 512 pairs) is one run, 43 us; as three, 47.
 constexpr int64_t FIXED_KEYS = 512;
 
+// Workgroups that are counted as running at once when windows are cut: one a
+// compute unit.  All kernels but those of dim 256 have room for two or more, so
+// from 129 to 256 pairs of request and head this leaves half of it empty: 16
+// requests of 8 heads in a window of 4096 are two runs each, 24 us, and 24 requests
+// one, 36.5.
+constexpr int64_t WINDOW_ROOM = 256;
+
 struct Shape {
     int dp, groups, row_tiles, target, slots, length, each;
     size_t bytes;  // of the workspace: counters, then the sums
@@ -81,7 +88,7 @@ Shape shape_of(const gba_q4_attention &d)
     int64_t slots = 0;
     const int64_t sums = Q4_ROWS * (c.dim + 2) * (int64_t)sizeof(float);
     if (d.window != 0) {
-        const int64_t length = run_of_window(pairs, sums, most_keys, 256, FIXED_KEYS, Q4_KEYS * Q4_WAVES);
+        const int64_t length = run_of_window(pairs, sums, most_keys, WINDOW_ROOM, FIXED_KEYS, Q4_KEYS * Q4_WAVES);
         const int64_t each = div_up(most_keys, length);
         if (each == 1) return s;
         s.length = (int)length;

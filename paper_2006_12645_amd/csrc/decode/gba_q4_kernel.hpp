@@ -149,6 +149,9 @@ __device__ __forceinline__ void each(F f)
 // for the end: 16 trees of 64 tokens over 500 to 4096 keys, 2048 workgroups, 103 us
 // as they come and 83, of 36 tokens over 100 to 8000 keys 96 and 65; over 4000 keys
 // each 179 and 181; 64 trees of 64 over 100 to 4000 keys, 8192 workgroups, 271 and 285.
+// Below, the look at all lengths costs more: trees of 64 over 500 to 4096 keys, 768
+// workgroups 44 and 47, 1024 of them 75 and 66; 16 trees over up to 512 keys 37.1 and
+// 38.5, up to 1024 51.5 and 48.7, up to 2048 78 and 72.
 constexpr int64_t Q4_SORTED_FROM = 1024, Q4_SORTED_TO = 4096, Q4_SORTED_KEYS = 2048;
 
 // The x-th longest of up to 64 requests, in steps of 64 keys; of equal ones, the
@@ -172,10 +175,10 @@ __device__ __forceinline__ int nth_longest(const Q4Args &p, int x, int lane)
 // TB/s).  Else by vector instructions, about 740 a tile of dim 128 in two groups,
 // of which 224 unpack codes: 64 requests of up to 8192 keys, 79 MB, 32 us; 16 trees
 // of 64 tokens, four heads a key head, 83 us.  Two blocks of 16 rows a wave would
-// share what is unpacked, but leave one wave a SIMD: 124 us.  With rows and keys
-// exchanged in the first product a lane has one key, and scales need no
-// broadcasts, but weights go through LDS to the second: 33 us and, of 128 windows
-// of 4096 keys for 16 rows, 51 in place of 43.
+// share what is unpacked, but leave one wave a SIMD: 124 us, where these took 103
+// with requests as they come.  With rows and keys exchanged in the first product a
+// lane has one key, and scales need no broadcasts, but weights go through LDS to the
+// second: 33 us and, of 128 windows of 4096 keys for 16 rows, 51 in place of 43.
 template <class T, int DP, int G>
 __global__ void __launch_bounds__(64 * Q4_WAVES, DP <= 128 ? 2 : 1) q4_attention_kernel(Q4Args p)
 {
